@@ -155,6 +155,34 @@ int adaspec_verify_attn(const void *q, const void *k_pages, const void *v_pages,
                         void *workspace, size_t workspace_bytes, void *stream);
 
 /* ------------------------------------------------------------------------
+ * adaspec_verify_attn_window - verification attention with a sliding window and
+ * first tokens that stay visible (sinks), for targets whose layers attend that
+ * way.  As adaspec_verify_attn, except for what a row sees: row j of request i,
+ * at position pos = ctx_lens[i] - n_i + j, attends to token t iff
+ *     t <= pos  and  (t > pos - window  or  t < sinks).
+ * window >= 1 (a row always sees itself), sinks >= 0; a window of at least the
+ * longest context is plain causal attention.
+ *   - Pages that no row of a request looks at, those whose tokens all lie in
+ *     [sinks, ctx_lens[i] - n_i - window], are never read, and neither are their
+ *     block_table entries: they may have been given back (adaspec_kv_remap).
+ *   - A token influences only rows that see it, whatever it holds (NaN and
+ *     infinities too).
+ *   - Same dims as adaspec_verify_attn, but at most 2^30 tokens per block table
+ *     row, and batch * n_kv_heads * row groups below 2^31.  path: FAST is the
+ *     matrix-core form (head_dim 64 or 128), VECTOR the portable one, AUTO the
+ *     former where it fits.
+ *   - There is no metadata: a PLAN_BUILD_ONLY call checks its arguments and
+ *     enqueues nothing, a PLAN_REUSE call is a PLAN_BUILD_AND_RUN call.
+ * ---------------------------------------------------------------------- */
+size_t adaspec_verify_attn_window_workspace_bytes(const adaspec_attn_dims *dims, int32_t window, int32_t sinks);
+
+int adaspec_verify_attn_window(const void *q, const void *k_pages, const void *v_pages,
+                               const int32_t *block_table, const int32_t *ctx_lens,
+                               const int32_t *spec_lens, void *out,
+                               const adaspec_attn_dims *dims, int32_t window, int32_t sinks,
+                               void *workspace, size_t workspace_bytes, void *stream);
+
+/* ------------------------------------------------------------------------
  * Acceptance (paper Sec. 2.2 and Fig. 1 for the greedy form: accept a draft
  * while it equals the target's choice, stop at the first mismatch, emit the
  * target's token there; Sec. 4.2: one bonus token is always produced.  The
@@ -273,6 +301,11 @@ int adaspec_accept_resolved_path(const void *target_logits, const void *draft_pr
 int adaspec_check_ragged_inputs(const int32_t *block_table, const int32_t *ctx_lens,
                                 const int32_t *spec_lens, const adaspec_attn_dims *dims,
                                 int32_t *err_flags, void *stream);
+
+/* The same for a windowed call: entries of pages that it never reads are not looked at. */
+int adaspec_check_window_inputs(const int32_t *block_table, const int32_t *ctx_lens,
+                                const int32_t *spec_lens, const adaspec_attn_dims *dims,
+                                int32_t window, int32_t sinks, int32_t *err_flags, void *stream);
 
 /* ------------------------------------------------------------------------
  * The two steps on either side of a verification step (paper Sec. 6: the

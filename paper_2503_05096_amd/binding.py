@@ -26,6 +26,7 @@ EXPORTS = (
     "adaspec_accept_workspace_bytes", "adaspec_accept", "adaspec_accept_noalloc", "adaspec_accept_resolved_path",
     "adaspec_verify_attn_tree", "adaspec_accept_tree", "adaspec_kv_compact_path", "adaspec_check_tree_parents", "adaspec_check_accept_inputs",
     "adaspec_check_ragged_inputs", "adaspec_kv_append", "adaspec_commit",
+    "adaspec_verify_attn_window_workspace_bytes", "adaspec_verify_attn_window", "adaspec_check_window_inputs",
     "adaspec_draft_sample_workspace_bytes", "adaspec_draft_sample",
     "adaspec_status_string", "adaspec_version",
 )
@@ -132,6 +133,12 @@ def _open(path: str) -> C.CDLL:
     L.adaspec_verify_attn_workspace_bytes.argtypes = [C.POINTER(AttnDims)]
     L.adaspec_verify_attn.restype = C.c_int
     L.adaspec_verify_attn.argtypes = [vp] * 7 + [C.POINTER(AttnDims), vp, C.c_size_t, vp]
+    L.adaspec_verify_attn_window_workspace_bytes.restype = C.c_size_t
+    L.adaspec_verify_attn_window_workspace_bytes.argtypes = [C.POINTER(AttnDims), C.c_int32, C.c_int32]
+    L.adaspec_verify_attn_window.restype = C.c_int
+    L.adaspec_verify_attn_window.argtypes = [vp] * 7 + [C.POINTER(AttnDims), C.c_int32, C.c_int32, vp, C.c_size_t, vp]
+    L.adaspec_check_window_inputs.restype = C.c_int
+    L.adaspec_check_window_inputs.argtypes = [vp, vp, vp, C.POINTER(AttnDims), C.c_int32, C.c_int32, vp, vp]
     L.adaspec_accept_workspace_bytes.restype = C.c_size_t
     L.adaspec_accept_workspace_bytes.argtypes = [C.POINTER(AcceptDims)]
     L.adaspec_accept.restype = C.c_int
@@ -250,15 +257,23 @@ def attn_dims(q, k_pages, block_table, *, max_spec_len: int, scale: float = 0.0,
 
 def verify_attn(q, k_pages, v_pages, block_table, ctx_lens, spec_lens, out=None, *,
                 max_spec_len: int, scale: float = 0.0, out_dtype: Optional[int] = None,
-                path: str = "auto", plan: str = "run", workspace=None, stream=None, parents=None, timing=None):
+                path: str = "auto", plan: str = "run", workspace=None, stream=None, parents=None, timing=None,
+                window: Optional[int] = None, sinks: int = 0):
     """adaspec_verify_attn on device tensors; returns `out` [TQ][Hq][d].
 
     plan: "run" (build the ragged metadata, then run), "build" (metadata only; returns None) or
     "reuse" (run with the metadata a previous call left in the same workspace).  "build" and "reuse"
     require `workspace`: a tensor of at least adaspec_verify_attn_workspace_bytes that the caller owns
     and that no other call touches between the build and the last reuse.
-    parents [TQ] int32 (a draft tree): adaspec_verify_attn_tree instead."""
-    if path == "auto" and timing is None:
+    parents [TQ] int32 (a draft tree): adaspec_verify_attn_tree instead.
+    window, sinks: adaspec_verify_attn_window instead: a row sees the last `window` tokens up to its own and the request's
+    first `sinks`; block_table entries of pages that no row sees are never read.  Not with parents."""
+    if window is not None or sinks != 0:
+        if window is None:
+            raise ValueError("verify_attn(sinks=...) needs a window: without one every token is visible")
+        if parents is not None:
+            raise ValueError("verify_attn(window=...) takes chains of drafts, not trees (parents=)")
+    elif path == "auto" and timing is None:
         r = (_fast or _native()).verify_attn(q, k_pages, v_pages, block_table, ctx_lens, spec_lens, out, max_spec_len,
                                              scale, out_dtype, plan, workspace, stream, parents)
         if r is not NotImplemented:
@@ -273,6 +288,9 @@ def verify_attn(q, k_pages, v_pages, block_table, ctx_lens, spec_lens, out=None,
     if out is None and plan != "build":
         out = torch.empty(q.shape, dtype=_torch_dtype(dims.out_dtype), device=q.device)
     L = lib()
+    if window is not None:
+        return _verify_attn_window(q, k_pages, v_pages, block_table, ctx_lens, spec_lens, out, dims, int(window), int(sinks), plan,
+                                   workspace, stream)
     need = L.adaspec_verify_attn_workspace_bytes(C.byref(dims))
     if need == 0 and dims.batch > 0:
         raise AdaspecError(L.adaspec_verify_attn(None, None, None, None, None, None, None, C.byref(dims),
@@ -299,6 +317,25 @@ def verify_attn(q, k_pages, v_pages, block_table, ctx_lens, spec_lens, out=None,
                                _stream_ptr(stream))
     if rc != 0:
         raise AdaspecError(rc, "adaspec_verify_attn")
+    return out
+
+
+def _verify_attn_window(q, k_pages, v_pages, block_table, ctx_lens, spec_lens, out, dims, window, sinks, plan, workspace, stream):
+    """the windowed call of verify_attn, whose checks have been made"""
+    L = lib()
+    need = L.adaspec_verify_attn_window_workspace_bytes(C.byref(dims), window, sinks)
+    if need == 0 and dims.batch > 0:
+        raise AdaspecError(L.adaspec_verify_attn_window(None, None, None, None, None, None, None, C.byref(dims), window, sinks, None,
+                                                        0, None) or -2, "adaspec_verify_attn_window (dims)")
+    if plan != "run" and workspace is None:
+        raise ValueError("verify_attn(plan='build' / 'reuse') needs an explicit workspace= tensor that the "
+                         "caller keeps for the whole pass")
+    ws = _workspace(need, q.device, workspace, "attn")
+    rc = L.adaspec_verify_attn_window(q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), block_table.data_ptr(),
+                                      ctx_lens.data_ptr(), spec_lens.data_ptr(), None if out is None else out.data_ptr(),
+                                      C.byref(dims), window, sinks, ws.data_ptr(), ws.numel(), _stream_ptr(stream))
+    if rc != 0:
+        raise AdaspecError(rc, "adaspec_verify_attn_window")
     return out
 
 
@@ -478,10 +515,18 @@ def check_tree_parents(parents, spec_lens, *, max_spec_len: int, stream=None) ->
     return int(flags.item())
 
 
-def check_ragged_inputs(block_table, ctx_lens, spec_lens, dims: AttnDims, stream=None) -> int:
-    """Runs the device-side metadata check and returns the flag word (synchronises)."""
+def check_ragged_inputs(block_table, ctx_lens, spec_lens, dims: AttnDims, stream=None, *, window: Optional[int] = None,
+                        sinks: int = 0) -> int:
+    """Runs the device-side metadata check and returns the flag word (synchronises).  window, sinks: the check of a windowed
+    call, which leaves out the entries that such a call never reads."""
     import torch
     flags = torch.zeros(1, dtype=torch.int32, device=block_table.device)
+    if window is not None:
+        rc = lib().adaspec_check_window_inputs(block_table.data_ptr(), ctx_lens.data_ptr(), spec_lens.data_ptr(), C.byref(dims),
+                                               int(window), int(sinks), flags.data_ptr(), _stream_ptr(stream))
+        if rc != 0:
+            raise AdaspecError(rc, "adaspec_check_window_inputs")
+        return int(flags.item())
     rc = lib().adaspec_check_ragged_inputs(block_table.data_ptr(), ctx_lens.data_ptr(),
                                            spec_lens.data_ptr(), C.byref(dims), flags.data_ptr(),
                                            _stream_ptr(stream))

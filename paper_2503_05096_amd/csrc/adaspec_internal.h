@@ -193,6 +193,26 @@ int attn_f32_grid_slots(const AttnArgs &a, int cus);
 hipError_t launch_attn_combine(const AttnArgs &a);
 int attn_combine_waves(const AttnPlan &p, const adaspec_attn_dims &d);   // wavefronts per (row, head) of the combine kernel
 
+// ---- windowed attention (attn_window.hip) --------------------------------------
+struct WindowPlan {
+    int groups, rows_per_group;     // row groups of a request with max_spec_len + 1 rows, query rows (times G) in one
+    int64_t units;                  // batch * n_kv_heads * groups
+    size_t total_bytes;
+};
+struct WindowArgs {
+    const void *q, *k_pages, *v_pages;
+    const int32_t *block_table, *ctx_lens, *spec_lens;
+    void *out;
+    adaspec_attn_dims dims;
+    int window, sinks;              // at most 16 max_pages_per_req each
+    float scale_log2;
+    WindowPlan plan;
+    char *ws;
+    hipStream_t stream;
+};
+WindowPlan make_window_plan(const adaspec_attn_dims &d, int window, int sinks);
+hipError_t launch_attn_window(const WindowArgs &a);
+
 // ---- accept workspace ------------------------------------------------------
 struct AcceptPlan {
     size_t off_cu_q;        // int32[B + 1]
@@ -273,7 +293,7 @@ hipError_t launch_check_accept_inputs(const int32_t *draft_tokens, const int32_t
 hipError_t launch_check_tree_parents(const int32_t *parents, const int32_t *spec_lens, int B, int total_q,
                                      int max_spec_len, int32_t *err_flags, hipStream_t stream);
 hipError_t launch_check_ragged(const int32_t *block_table, const int32_t *ctx_lens,
-                               const int32_t *spec_lens, const adaspec_attn_dims &d,
+                               const int32_t *spec_lens, const adaspec_attn_dims &d, int window, int sinks,
                                int32_t *err_flags, hipStream_t stream);
 
 bool draft_sample_supported(const adaspec_draft_dims &d, const void *logits, const void *probs);

@@ -413,6 +413,57 @@ int adaspec_verify_attn_tree(const void *q, const void *k_pages, const void *v_p
                             workspace, workspace_bytes, stream);
 }
 
+// dims of a windowed call; window and sinks are cut to what a block table can hold
+static int validate_window(const adaspec_attn_dims *d, int32_t &window, int32_t &sinks)
+{
+    const int rc = validate_attn_dims(d);
+    if (rc != ADASPEC_OK) return rc;
+    if (window < 1 || sinks < 0) return ADASPEC_ERR_DIM;
+    const int64_t tokens = (int64_t)d->max_pages_per_req * d->page_size;
+    if (tokens > (1 << 30)) return ADASPEC_ERR_UNSUPPORTED;
+    if (window > tokens) window = (int32_t)tokens;
+    if (sinks > tokens) sinks = (int32_t)tokens;
+    if (make_window_plan(*d, window, sinks).units > INT32_MAX) return ADASPEC_ERR_UNSUPPORTED;
+    return ADASPEC_OK;
+}
+
+size_t adaspec_verify_attn_window_workspace_bytes(const adaspec_attn_dims *dims, int32_t window, int32_t sinks)
+{
+    if (validate_window(dims, window, sinks) != ADASPEC_OK) return 0;
+    return make_window_plan(*dims, window, sinks).total_bytes;
+}
+
+int adaspec_verify_attn_window(const void *q, const void *k_pages, const void *v_pages,
+                               const int32_t *block_table, const int32_t *ctx_lens,
+                               const int32_t *spec_lens, void *out, const adaspec_attn_dims *dims,
+                               int32_t window, int32_t sinks,
+                               void *workspace, size_t workspace_bytes, void *stream)
+{
+    const int rc = validate_window(dims, window, sinks);
+    if (rc != ADASPEC_OK) return rc;
+    if (dims->batch == 0) return ADASPEC_OK;
+    const bool plan_only = dims->plan_mode == ADASPEC_PLAN_BUILD_ONLY;
+    if (!block_table || !ctx_lens || !spec_lens || !workspace) return ADASPEC_ERR_NULL;
+    if (!plan_only && (!q || !k_pages || !v_pages || !out)) return ADASPEC_ERR_NULL;
+    if (reinterpret_cast<uintptr_t>(workspace) & 255u) return ADASPEC_ERR_ALIGN;
+    if (!plan_only && (!aligned16(q) || !aligned16(k_pages) || !aligned16(v_pages) || !aligned16(out)))
+        return ADASPEC_ERR_ALIGN;
+    WindowArgs a;
+    a.plan = make_window_plan(*dims, window, sinks);
+    if (workspace_bytes < a.plan.total_bytes) return ADASPEC_ERR_WORKSPACE;
+    if (plan_only) return ADASPEC_OK;                               // (the units follow from the bounds: no metadata)
+    a.q = q; a.k_pages = k_pages; a.v_pages = v_pages;
+    a.block_table = block_table; a.ctx_lens = ctx_lens; a.spec_lens = spec_lens;
+    a.out = out; a.dims = *dims; a.window = window; a.sinks = sinks;
+    a.ws = static_cast<char *>(workspace);
+    a.stream = static_cast<hipStream_t>(stream);
+    a.scale_log2 = (dims->scale > 0.0f ? dims->scale : 1.0f / sqrtf((float)dims->head_dim)) * 1.4426950408889634f;
+    if (!record_event(dims->timing_start, dims->timing_stop, true, a.stream)) return ADASPEC_ERR_HIP;
+    if (launch_attn_window(a) != hipSuccess) return ADASPEC_ERR_HIP;
+    if (!record_event(dims->timing_start, dims->timing_stop, false, a.stream)) return ADASPEC_ERR_HIP;
+    return ADASPEC_OK;
+}
+
 size_t adaspec_accept_workspace_bytes(const adaspec_accept_dims *dims)
 {
     if (validate_accept_dims(dims) != ADASPEC_OK) return 0;
@@ -613,7 +664,20 @@ int adaspec_check_ragged_inputs(const int32_t *block_table, const int32_t *ctx_l
     int rc = validate_attn_dims(dims);
     if (rc != ADASPEC_OK) return rc;
     if (!block_table || !ctx_lens || !spec_lens || !err_flags) return ADASPEC_ERR_NULL;
-    if (launch_check_ragged(block_table, ctx_lens, spec_lens, *dims, err_flags,
+    if (launch_check_ragged(block_table, ctx_lens, spec_lens, *dims, INT32_MAX, 0, err_flags,
+                            static_cast<hipStream_t>(stream)) != hipSuccess)
+        return ADASPEC_ERR_HIP;
+    return ADASPEC_OK;
+}
+
+int adaspec_check_window_inputs(const int32_t *block_table, const int32_t *ctx_lens,
+                                const int32_t *spec_lens, const adaspec_attn_dims *dims,
+                                int32_t window, int32_t sinks, int32_t *err_flags, void *stream)
+{
+    const int rc = validate_window(dims, window, sinks);
+    if (rc != ADASPEC_OK) return rc;
+    if (!block_table || !ctx_lens || !spec_lens || !err_flags) return ADASPEC_ERR_NULL;
+    if (launch_check_ragged(block_table, ctx_lens, spec_lens, *dims, window, sinks, err_flags,
                             static_cast<hipStream_t>(stream)) != hipSuccess)
         return ADASPEC_ERR_HIP;
     return ADASPEC_OK;

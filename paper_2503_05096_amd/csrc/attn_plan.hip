@@ -603,7 +603,7 @@ hipError_t launch_attn_combine(const AttnArgs &a)
 __global__ __launch_bounds__(256) void check_ragged_kernel(
     const int32_t *__restrict__ block_table, const int32_t *__restrict__ ctx_lens,
     const int32_t *__restrict__ spec_lens, int B, int total_q, int max_spec_len, int page_size,
-    int num_pages, int max_pages_per_req, int32_t *__restrict__ err_flags)
+    int num_pages, int max_pages_per_req, int window, int sinks, int32_t *__restrict__ err_flags)
 {
     __shared__ int s_flags, s_rows;
     if (threadIdx.x == 0) { s_flags = 0; s_rows = 0; }
@@ -616,7 +616,9 @@ __global__ __launch_bounds__(256) void check_ragged_kernel(
         rows += n;
         const int pages = L > 0 ? ceil_div(L, page_size) : 0;
         if (L < n || pages > max_pages_per_req) { flags |= 2; continue; }
+        const int first = ceil_div(sinks, page_size), low = max(L - n - window + 1, 0) / page_size;
         for (int pg = 0; pg < pages; ++pg) {
+            if (pg >= first && pg < low) { pg = low - 1; continue; }        // behind every row's window
             const int id = block_table[(int64_t)i * max_pages_per_req + pg];
             if (id < 0 || id >= num_pages) flags |= 4;
         }
@@ -628,12 +630,12 @@ __global__ __launch_bounds__(256) void check_ragged_kernel(
 }
 
 hipError_t launch_check_ragged(const int32_t *block_table, const int32_t *ctx_lens,
-                               const int32_t *spec_lens, const adaspec_attn_dims &d,
+                               const int32_t *spec_lens, const adaspec_attn_dims &d, int window, int sinks,
                                int32_t *err_flags, hipStream_t stream)
 {
     hipLaunchKernelGGL(check_ragged_kernel, dim3(1), dim3(256), 0, stream, block_table, ctx_lens,
                        spec_lens, d.batch, d.total_q, d.max_spec_len, d.page_size, d.num_pages,
-                       d.max_pages_per_req, err_flags);
+                       d.max_pages_per_req, window, sinks, err_flags);
     return hipGetLastError();
 }
 

@@ -1,0 +1,142 @@
+// Windowed verification attention, portable form: any of the three storage types, any head_dim that is a multiple of 8 up
+// to 256.  One wavefront per (request, kv head, chunk of 8 query rows).
+//
+// Per 64 tokens: lane <-> token for the scores (each lane walks its key row, the query rows are broadcast from LDS),
+// wavefront reductions for the online softmax, then lane <-> channel for P.V.  A token that a row does not see has a weight
+// below zero in LDS and is left out of that row's sum, not multiplied by zero: whatever it holds cannot reach the row.
+#include "attn_window.h"
+
+namespace adaspec {
+
+constexpr int kWinRows = 8;
+constexpr int kWinMaxD = 256;
+
+template <class T>
+__global__ __launch_bounds__(64) void attn_window_vector_kernel(WindowDims dims, const void *__restrict__ q,
+                                                                const void *__restrict__ k_pages, const void *__restrict__ v_pages,
+                                                                void *__restrict__ out, int d, float scale_log2, int out_dtype)
+{
+    __shared__ float qs[kWinRows][kWinMaxD];
+    __shared__ float ps[kWinRows][64];
+    const int lane = threadIdx.x;
+    const int G = dims.Hq / dims.Hkv;
+    const int gkv = blockIdx.x % dims.Hkv, rest = blockIdx.x / dims.Hkv;
+    WindowUnit u;
+    if (!window_unit(u, dims, rest / dims.groups, rest % dims.groups, gkv, lane)) return;
+
+    for (int idx = lane; idx < kWinRows * d; idx += 64) {
+        const int r = u.r0 + idx / d, c = idx % d;
+        qs[idx / d][c] = r < u.rows ? load_as_float<T>(q, ((u.qrow0 + r / G) * dims.Hq + gkv * G + r % G) * d + c) : 0.f;
+    }
+    __syncthreads();
+
+    float m[kWinRows], l[kWinRows], acc[kWinRows][4];
+#pragma unroll
+    for (int r = 0; r < kWinRows; ++r) {
+        m[r] = -INFINITY; l[r] = 0.f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[r][e] = 0.f;
+    }
+    for (int v0 = 0; v0 < u.pages; v0 += 4) {
+        const int v = v0 + (lane >> 4);
+        const int pg = u.page_of(min(v, u.pages - 1)), t = pg * 16 + (lane & 15);
+        const bool valid = v < u.pages && t < u.L;
+        float sc[kWinRows];
+#pragma unroll
+        for (int r = 0; r < kWinRows; ++r) sc[r] = 0.f;
+        if (valid) {
+            const int64_t page = dims.block_table[u.bt_off + pg];
+            const int64_t koff = ((page * dims.Hkv + gkv) * 16 + (lane & 15)) * (int64_t)d;
+            for (int c = 0; c < d; c += 8) {
+                float kv[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) kv[e] = load_as_float<T>(k_pages, koff + c + e);
+#pragma unroll
+                for (int r = 0; r < kWinRows; ++r)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) sc[r] = fmaf(qs[r][c + e], kv[e], sc[r]);
+            }
+        }
+        __syncthreads();                                            // the last 64 tokens' weights have been read
+#pragma unroll
+        for (int r = 0; r < kWinRows; ++r) {
+            const int row = u.r0 + r;
+            const bool vis = valid && row < u.rows && window_sees(u, u.first_pos + row / G, t);
+            const float sv = vis ? sc[r] * scale_log2 : -INFINITY;
+            const float mn = fmaxf(m[r], wave_max(sv));
+            float p = 0.f, alpha = 1.f;
+            if (mn > -INFINITY) {
+                alpha = __builtin_amdgcn_exp2f(m[r] - mn);
+                p = vis ? __builtin_amdgcn_exp2f(sv - mn) : 0.f;
+            } else if (vis) {
+                p = sv == sv ? 0.f : sv;                            // (every score so far is -inf or NaN)
+            }
+            l[r] = l[r] * alpha + wave_sum(p);
+            m[r] = mn;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[r][e] *= alpha;
+            ps[r][lane] = vis ? p : -1.f;
+        }
+        __syncthreads();
+        const int most = min(4, u.pages - v0) * 16;
+        for (int tt = 0; tt < most; ++tt) {
+            const int pv = u.page_of(v0 + (tt >> 4));
+            if (pv * 16 + (tt & 15) >= u.L) break;                  // (the last page of the list is the newest)
+            const int64_t page = dims.block_table[u.bt_off + pv];
+            const int64_t voff = ((page * dims.Hkv + gkv) * 16 + (tt & 15)) * (int64_t)d;
+            float vv[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int c = lane + 64 * e;
+                vv[e] = c < d ? load_as_float<T>(v_pages, voff + c) : 0.f;
+            }
+#pragma unroll
+            for (int r = 0; r < kWinRows; ++r) {
+                const float p = ps[r][tt];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[r][e] = p < 0.f ? acc[r][e] : fmaf(p, vv[e], acc[r][e]);
+            }
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < kWinRows; ++r) {
+        const int row = u.r0 + r;
+        if (row >= u.rows) continue;
+        const float inv = 1.0f / l[r];
+        const int64_t obase = ((u.qrow0 + row / G) * dims.Hq + gkv * G + row % G) * (int64_t)d;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int c = lane + 64 * e;
+            if (c < d) store_out(out, obase + c, acc[r][e] * inv, out_dtype);
+        }
+    }
+}
+
+WindowPlan make_window_plan(const adaspec_attn_dims &d, int window, int sinks)
+{
+    (void)window; (void)sinks;
+    WindowPlan p;
+    const int rows = (d.max_spec_len + 1) * (d.n_q_heads / d.n_kv_heads);
+    p.rows_per_group = kWinRows;
+    p.groups = ceil_div(rows, p.rows_per_group);
+    p.units = (int64_t)d.batch * d.n_kv_heads * p.groups;
+    p.total_bytes = 256;
+    return p;
+}
+
+hipError_t launch_attn_window(const WindowArgs &a)
+{
+    const adaspec_attn_dims &d = a.dims;
+    const WindowDims w{a.block_table, a.ctx_lens, a.spec_lens, d.total_q, d.max_spec_len, d.max_pages_per_req, d.n_q_heads,
+                       d.n_kv_heads, a.window, a.sinks, a.plan.groups, a.plan.rows_per_group};
+    auto launch = [&](auto tag) {
+        hipLaunchKernelGGL(attn_window_vector_kernel<decltype(tag)>, dim3((unsigned)a.plan.units), dim3(64), 0, a.stream, w, a.q,
+                           a.k_pages, a.v_pages, a.out, d.head_dim, a.scale_log2, d.out_dtype);
+    };
+    if (d.dtype == ADASPEC_F32) launch(F32{});
+    else if (d.dtype == ADASPEC_F16) launch(F16{});
+    else launch(BF16{});
+    return hipGetLastError();
+}
+
+}  // namespace adaspec
