@@ -362,6 +362,113 @@ int adaspec_commit(const int32_t *out_tokens, const int32_t *out_accept_len,
                    const adaspec_commit_dims *dims, void *stream);
 
 /* ------------------------------------------------------------------------
+ * The pages of the cache: which request holds which.  A pool of num_pages pages
+ * is shared by all requests of a block table, and by several requests at once
+ * where they begin alike.  Its state is two device arrays that the caller owns:
+ *   block_table [rows][max_pages_per_req]  page ids; a negative entry holds none
+ *   page_refs   [num_pages]                holders of every page: entries of the
+ *                                          block table, and whatever else keeps one
+ *                                          (a cache of prompts, another table); 0 = free
+ * Both start out as -1 and 0.  One set serves all layers of a model: the calls
+ * below move ids, adaspec_kv_copy_pages then moves the K/V of every layer.
+ *
+ * adaspec_kv_remap - between steps: the block table of the next batch.  In one
+ * call requests end, start, fork (parallel samples, beams), change places, get
+ * room for their next tokens, give back what rejected drafts had reserved and
+ * what has left their window.
+ *   sources  [batch]      row of the old table that row i continues; outside
+ *                         [0, old_batch): a new request that starts empty.  An
+ *                         old row may be named by any number of rows, or by none
+ *                         (then it has ended)
+ *   lens     [old_batch]  tokens of every old row that are kept, e.g. the
+ *                         committed_lens of adaspec_commit
+ *   new_lens [batch]      tokens that row i needs room for, e.g. next_ctx_lens
+ * What happens, as if in this order (P = page_size, n = lens[sources[i]], or 0):
+ *   1. every entry of the old table is released: its page's count falls by one;
+ *   2. row i holds the first ceil(n / P) entries of its source again, except
+ *      those whose tokens all lie in [sinks, n - window] where window > 0: no
+ *      later row of adaspec_verify_attn_window sees them;
+ *   3. in the order of rows: where new_lens[i] > n and the page of token n has
+ *      earlier tokens in it (n % P != 0) and other holders too, row i wants a
+ *      page of its own for it and lets go of the shared one (so of several rows
+ *      that share such a page among themselves only, the last keeps it);
+ *   4. wants - row by row, in a row the page of step 3 first, then entries
+ *      ceil(n / P) .. ceil(new_lens[i] / P) - 1 - are served with the pages that
+ *      are free after step 2, lowest id first.
+ * Outputs (overwritten; entries that hold nothing are -1):
+ *   out_table [batch][max_pages_per_req]   must not overlap block_table
+ *   out_refs  [num_pages]                  the counts; may be page_refs itself
+ *   copy_src, copy_dst [batch]             the pages of step 3: copy_dst[i] has to
+ *                                          become a copy of copy_src[i] before it
+ *                                          is written (adaspec_kv_copy_pages), or -1
+ *   status [2]                             free pages left; wants that could not
+ *                                          be served
+ * Where wants are left over, their entries stay -1 and pages of step 3 stay
+ * shared: the caller makes room and calls again with the new table, every row
+ * its own source.  Such a row must not be written to meanwhile.
+ * Lengths are cut to [0, max_pages_per_req * page_size], at most 2^30; ids outside
+ * the pool hold nothing.  batch + old_batch <= 65535.  No call reads K or V.
+ * ---------------------------------------------------------------------- */
+typedef struct {
+    int32_t batch;              /* rows of the new table (adaspec_kv_remap)             */
+    int32_t old_batch;          /* rows of block_table                                  */
+    int32_t max_pages_per_req;  /* row stride of both tables                            */
+    int32_t num_pages;          /* pages of the pool                                    */
+    int32_t page_size;          /* tokens per page                                      */
+    int32_t window;             /* adaspec_kv_remap: 0 = no window                      */
+    int32_t sinks;              /* adaspec_kv_remap, with a window                      */
+    int32_t max_moves;          /* adaspec_kv_compact_pages: 1 .. num_pages             */
+} adaspec_pages_dims;
+
+size_t adaspec_kv_remap_workspace_bytes(const adaspec_pages_dims *dims);
+
+int adaspec_kv_remap(const int32_t *block_table, const int32_t *page_refs, const int32_t *sources,
+                     const int32_t *lens, const int32_t *new_lens,
+                     int32_t *out_table, int32_t *out_refs, int32_t *copy_src, int32_t *copy_dst,
+                     int32_t *status, const adaspec_pages_dims *dims,
+                     void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * adaspec_kv_compact_pages - used pages (page_refs > 0) to the front of the pool,
+ * so that what lies behind can be given away.  With N used pages, the m-th used
+ * page at or behind N moves to the m-th free page below N, for the first
+ * max_moves of them; later calls go on from there.
+ *   out_table [old_batch][max_pages_per_req]  block_table with the new ids; may be
+ *                                             block_table itself, must not overlap it otherwise
+ *   out_refs  [num_pages]                     the counts at the new ids; may be page_refs itself
+ *   page_map  [num_pages]                     new id of every used page, -1 for free ones:
+ *                                             for holders outside the table
+ *   copy_src, copy_dst [max_moves]            the moves, then -1: for adaspec_kv_copy_pages
+ *   status [2]                                N; moves that the pool takes altogether
+ */
+size_t adaspec_kv_compact_pages_workspace_bytes(const adaspec_pages_dims *dims);
+
+int adaspec_kv_compact_pages(const int32_t *block_table, const int32_t *page_refs,
+                             int32_t *out_table, int32_t *out_refs, int32_t *page_map,
+                             int32_t *copy_src, int32_t *copy_dst, int32_t *status,
+                             const adaspec_pages_dims *dims,
+                             void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * adaspec_kv_copy_pages - page copy_dst[c] of K and of V becomes a copy of page
+ * copy_src[c], all kv heads, in every layer, for c < n_copies.  Pairs with an id
+ * outside [0, num_pages) are left out.  No page may be a destination twice, or a
+ * destination and a source (the lists of the two calls above never have such):
+ * what it would hold is undefined.
+ *   k_pages, v_pages [layers][num_pages][n_kv_heads][page_size][head_dim], contiguous
+ * head_dim a multiple of 8 for 16-bit types, of 4 for fp32; both tensors 16-byte
+ * aligned.  Needs no workspace.
+ */
+typedef struct {
+    int32_t layers;             /* 1 for the pages of one layer        */
+    int32_t num_pages, n_kv_heads, page_size, head_dim;
+    int32_t dtype;              /* adaspec_dtype of k_pages, v_pages   */
+} adaspec_copy_dims;
+
+int adaspec_kv_copy_pages(void *k_pages, void *v_pages, const int32_t *copy_src, const int32_t *copy_dst,
+                          int32_t n_copies, const adaspec_copy_dims *dims, void *stream);
+
+/* ------------------------------------------------------------------------
  * Tree verification: the drafts of a request form a token TREE instead of a
  * chain.  The paper verifies chains and runs the tree-based system it compares
  * with at tree width 1 (Sec. 7.1, baselines; Sec. 8 names tree-based

@@ -27,6 +27,8 @@ EXPORTS = (
     "adaspec_verify_attn_tree", "adaspec_accept_tree", "adaspec_kv_compact_path", "adaspec_check_tree_parents", "adaspec_check_accept_inputs",
     "adaspec_check_ragged_inputs", "adaspec_kv_append", "adaspec_commit",
     "adaspec_verify_attn_window_workspace_bytes", "adaspec_verify_attn_window", "adaspec_check_window_inputs",
+    "adaspec_kv_remap_workspace_bytes", "adaspec_kv_remap", "adaspec_kv_compact_pages_workspace_bytes", "adaspec_kv_compact_pages",
+    "adaspec_kv_copy_pages",
     "adaspec_draft_sample_workspace_bytes", "adaspec_draft_sample",
     "adaspec_status_string", "adaspec_version",
 )
@@ -60,6 +62,16 @@ class DraftDims(C.Structure):
                 ("probs_dtype", C.c_int32), ("logits_row_stride", C.c_int64), ("probs_row_stride", C.c_int64),
                 ("path", C.c_int32), ("reserved", C.c_int32),
                 ("timing_start", C.c_void_p), ("timing_stop", C.c_void_p)]
+
+
+class PagesDims(C.Structure):
+    _fields_ = [("batch", C.c_int32), ("old_batch", C.c_int32), ("max_pages_per_req", C.c_int32), ("num_pages", C.c_int32),
+                ("page_size", C.c_int32), ("window", C.c_int32), ("sinks", C.c_int32), ("max_moves", C.c_int32)]
+
+
+class CopyDims(C.Structure):
+    _fields_ = [("layers", C.c_int32), ("num_pages", C.c_int32), ("n_kv_heads", C.c_int32), ("page_size", C.c_int32),
+                ("head_dim", C.c_int32), ("dtype", C.c_int32)]
 
 
 class AdaspecError(RuntimeError):
@@ -167,6 +179,16 @@ def _open(path: str) -> C.CDLL:
     L.adaspec_draft_sample.argtypes = [vp] * 7 + [C.POINTER(DraftDims), vp, C.c_size_t, vp]
     L.adaspec_draft_sample_workspace_bytes.restype = C.c_size_t
     L.adaspec_draft_sample_workspace_bytes.argtypes = [C.POINTER(DraftDims)]
+    L.adaspec_kv_remap_workspace_bytes.restype = C.c_size_t
+    L.adaspec_kv_remap_workspace_bytes.argtypes = [C.POINTER(PagesDims)]
+    L.adaspec_kv_remap.restype = C.c_int
+    L.adaspec_kv_remap.argtypes = [vp] * 10 + [C.POINTER(PagesDims), vp, C.c_size_t, vp]
+    L.adaspec_kv_compact_pages_workspace_bytes.restype = C.c_size_t
+    L.adaspec_kv_compact_pages_workspace_bytes.argtypes = [C.POINTER(PagesDims)]
+    L.adaspec_kv_compact_pages.restype = C.c_int
+    L.adaspec_kv_compact_pages.argtypes = [vp] * 8 + [C.POINTER(PagesDims), vp, C.c_size_t, vp]
+    L.adaspec_kv_copy_pages.restype = C.c_int
+    L.adaspec_kv_copy_pages.argtypes = [vp] * 4 + [C.c_int32, C.POINTER(CopyDims), vp]
     L.adaspec_status_string.restype = C.c_char_p
     L.adaspec_status_string.argtypes = [C.c_int]
     L.adaspec_version.restype = C.c_int
@@ -323,6 +345,10 @@ def verify_attn(q, k_pages, v_pages, block_table, ctx_lens, spec_lens, out=None,
 def _verify_attn_window(q, k_pages, v_pages, block_table, ctx_lens, spec_lens, out, dims, window, sinks, plan, workspace, stream):
     """the windowed call of verify_attn, whose checks have been made"""
     L = lib()
+    _on_current_device(q)
+    assert all(t.device == q.device for t in (k_pages, v_pages, block_table, ctx_lens, spec_lens))
+    assert ctx_lens.shape == spec_lens.shape == (dims.batch,)
+    assert out is None or (out.is_contiguous() and out.shape == q.shape and _dtype_code(out) == dims.out_dtype)
     need = L.adaspec_verify_attn_window_workspace_bytes(C.byref(dims), window, sinks)
     if need == 0 and dims.batch > 0:
         raise AdaspecError(L.adaspec_verify_attn_window(None, None, None, None, None, None, None, C.byref(dims), window, sinks, None,
@@ -592,6 +618,111 @@ def commit(out_tokens, out_accept_len, spec_lens, ctx_lens, *, max_spec_len: int
     if rc != 0:
         raise AdaspecError(rc, "adaspec_commit")
     return committed_lens, next_ctx_lens, last_token
+
+
+def _on_current_device(t) -> None:
+    import torch
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"tensors on {t.device}, but the current device is cuda:{torch.cuda.current_device()}: make the call under "
+                         f"torch.cuda.device({t.device.index})")
+
+
+def _dense_ints(*tensors):
+    import torch
+    for t in tensors:
+        assert t.is_cuda and t.is_contiguous() and t.dtype == torch.int32 and t.device == tensors[0].device
+
+
+def _ints_like(given, shape, like):
+    """the caller's output tensor, or a new one"""
+    import torch
+    if given is None:
+        return torch.empty(shape, dtype=torch.int32, device=like.device)
+    _dense_ints(like, given)
+    assert tuple(given.shape) == tuple(shape)
+    return given
+
+
+def kv_remap(block_table, page_refs, sources, lens, new_lens, *, window: Optional[int] = None, sinks: int = 0, page_size: int = 16,
+             out_table=None, out_refs=None, copy_src=None, copy_dst=None, status=None, workspace=None, stream=None):
+    """adaspec_kv_remap: the block table of the next batch; returns (out_table [batch][max_pages], out_refs [num_pages],
+    copy_src [batch], copy_dst [batch], status [2]).
+
+    block_table [old_batch][max_pages], page_refs [num_pages], sources [batch], lens [old_batch], new_lens [batch], all int32.
+    window, sinks: pages that no later row of verify_attn(window=, sinks=) sees are given back as well.  out_refs may be
+    page_refs; out_table must not overlap block_table."""
+    if window is None and sinks != 0:
+        raise ValueError("kv_remap(sinks=...) needs a window: without one every token is visible")
+    if window is not None and window < 1:
+        raise ValueError("kv_remap(window=...) is at least 1 (None: no window)")
+    old_batch, max_pages = block_table.shape
+    batch, num_pages = sources.shape[0], page_refs.shape[0]
+    _dense_ints(block_table, page_refs, sources, lens, new_lens)
+    _on_current_device(block_table)
+    assert sources.shape == new_lens.shape == (batch,) and lens.shape == (old_batch,) and page_refs.shape == (num_pages,)
+    out_table = _ints_like(out_table, (batch, max_pages), block_table)
+    out_refs = _ints_like(out_refs, (num_pages,), block_table)
+    copy_src = _ints_like(copy_src, (batch,), block_table)
+    copy_dst = _ints_like(copy_dst, (batch,), block_table)
+    status = _ints_like(status, (2,), block_table)
+    dims = PagesDims(batch, old_batch, max_pages, num_pages, int(page_size), 0 if window is None else int(window), int(sinks), 0)
+    L = lib()
+    ws = _workspace(L.adaspec_kv_remap_workspace_bytes(C.byref(dims)), block_table.device, workspace, "pages")
+    rc = L.adaspec_kv_remap(block_table.data_ptr(), page_refs.data_ptr(), sources.data_ptr(), lens.data_ptr(), new_lens.data_ptr(),
+                            out_table.data_ptr(), out_refs.data_ptr(), copy_src.data_ptr(), copy_dst.data_ptr(), status.data_ptr(),
+                            C.byref(dims), ws.data_ptr(), ws.numel(), _stream_ptr(stream))
+    if rc != 0:
+        raise AdaspecError(rc, "adaspec_kv_remap")
+    return out_table, out_refs, copy_src, copy_dst, status
+
+
+def kv_compact_pages(block_table, page_refs, *, max_moves: Optional[int] = None, out_table=None, out_refs=None, page_map=None,
+                     copy_src=None, copy_dst=None, status=None, page_size: int = 16, workspace=None, stream=None):
+    """adaspec_kv_compact_pages: used pages to the front of the pool; returns (out_table, out_refs, page_map [num_pages],
+    copy_src [max_moves], copy_dst [max_moves], status [2]).  max_moves: half of the pool's pages unless given, which is always
+    enough.  out_table may be block_table, out_refs may be page_refs."""
+    batch, max_pages = block_table.shape
+    num_pages = page_refs.shape[0]
+    _dense_ints(block_table, page_refs)
+    _on_current_device(block_table)
+    assert page_refs.shape == (num_pages,)
+    max_moves = max(1, num_pages // 2) if max_moves is None else int(max_moves)
+    if max_moves < 1:
+        raise ValueError("kv_compact_pages(max_moves=...) is at least 1")
+    out_table = _ints_like(out_table, (batch, max_pages), block_table)
+    out_refs = _ints_like(out_refs, (num_pages,), block_table)
+    page_map = _ints_like(page_map, (num_pages,), block_table)
+    copy_src = _ints_like(copy_src, (max_moves,), block_table)
+    copy_dst = _ints_like(copy_dst, (max_moves,), block_table)
+    status = _ints_like(status, (2,), block_table)
+    dims = PagesDims(0, batch, max_pages, num_pages, int(page_size), 0, 0, max_moves)
+    L = lib()
+    ws = _workspace(L.adaspec_kv_compact_pages_workspace_bytes(C.byref(dims)), block_table.device, workspace, "pages")
+    rc = L.adaspec_kv_compact_pages(block_table.data_ptr(), page_refs.data_ptr(), out_table.data_ptr(), out_refs.data_ptr(),
+                                    page_map.data_ptr(), copy_src.data_ptr(), copy_dst.data_ptr(), status.data_ptr(), C.byref(dims),
+                                    ws.data_ptr(), ws.numel(), _stream_ptr(stream))
+    if rc != 0:
+        raise AdaspecError(rc, "adaspec_kv_compact_pages")
+    return out_table, out_refs, page_map, copy_src, copy_dst, status
+
+
+def kv_copy_pages(k_pages, v_pages, copy_src, copy_dst, *, stream=None) -> None:
+    """adaspec_kv_copy_pages: pages copy_src[c] -> copy_dst[c] of K and V, in place; pairs with -1 are left out.
+    k_pages, v_pages: the pages of one layer [num_pages][Hkv][P][d], or of several [layers][num_pages][Hkv][P][d]."""
+    assert k_pages.dim() in (4, 5)
+    layers = k_pages.shape[0] if k_pages.dim() == 5 else 1
+    num_pages, Hkv, P, d = k_pages.shape[-4:]
+    assert k_pages.is_cuda and k_pages.is_contiguous() and v_pages.is_cuda and v_pages.is_contiguous()
+    assert v_pages.shape == k_pages.shape and v_pages.dtype == k_pages.dtype
+    _dense_ints(copy_src, copy_dst)
+    _on_current_device(k_pages)
+    assert v_pages.device == copy_src.device == k_pages.device
+    assert copy_src.dim() == 1 and copy_dst.shape == copy_src.shape
+    dims = CopyDims(layers, num_pages, Hkv, P, d, _dtype_code(k_pages))
+    rc = lib().adaspec_kv_copy_pages(k_pages.data_ptr(), v_pages.data_ptr(), copy_src.data_ptr(), copy_dst.data_ptr(),
+                                     copy_src.shape[0], C.byref(dims), _stream_ptr(stream))
+    if rc != 0:
+        raise AdaspecError(rc, "adaspec_kv_copy_pages")
 
 
 def draft_sample(draft_logits, temperature, uniforms, *, probs_dtype=None, draft_probs=None, out_rows=None,

@@ -296,6 +296,29 @@ hipError_t launch_check_ragged(const int32_t *block_table, const int32_t *ctx_le
                                const int32_t *spec_lens, const adaspec_attn_dims &d, int window, int sinks,
                                int32_t *err_flags, hipStream_t stream);
 
+// ---- the pages of the cache (kv_pages.hip) -----------------------------------------------------------------------------
+struct RemapArgs {
+    const int32_t *block_table, *page_refs, *sources, *lens, *new_lens;
+    int32_t *out_table, *out_refs, *copy_src, *copy_dst, *status;
+    adaspec_pages_dims dims;
+    int chunks;                                                     // of the pool's pages
+    int32_t *chunk_free, *part, *want_base, *copies;                // workspace: [chunks], [batch], [batch + 1], [batch]
+};
+struct CompactArgs {
+    const int32_t *block_table, *page_refs;
+    int32_t *out_table, *out_refs, *page_map, *copy_src, *copy_dst, *status;
+    adaspec_pages_dims dims;
+    int chunks, table_groups;                                       // workgroups for the pages, for the table
+    int32_t *chunk_used, *rank;                                     // workspace: [chunks], [num_pages]
+};
+// bytes of workspace; fills in its pointers where `a` is given
+size_t remap_workspace(const adaspec_pages_dims &d, RemapArgs *a, char *ws);
+size_t compact_workspace(const adaspec_pages_dims &d, CompactArgs *a, char *ws);
+hipError_t launch_kv_remap(const RemapArgs &a, hipStream_t stream);
+hipError_t launch_kv_compact_pages(const CompactArgs &a, hipStream_t stream);
+hipError_t launch_kv_copy_pages(void *k_pages, void *v_pages, const int32_t *copy_src, const int32_t *copy_dst, int n_copies,
+                                const adaspec_copy_dims &d, hipStream_t stream);
+
 bool draft_sample_supported(const adaspec_draft_dims &d, const void *logits, const void *probs);
 hipError_t launch_draft_sample(const void *logits, const float *temperature, const float *uniforms,
                                const int32_t *out_rows, void *probs, int32_t *tokens, float *confidence,

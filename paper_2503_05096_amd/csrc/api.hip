@@ -753,6 +753,92 @@ int adaspec_commit(const int32_t *out_tokens, const int32_t *out_accept_len,
     return ADASPEC_OK;
 }
 
+static int validate_pages_dims(const adaspec_pages_dims *d, bool remap)
+{
+    if (!d) return ADASPEC_ERR_NULL;
+    if (d->old_batch < 0 || d->max_pages_per_req <= 0 || d->num_pages <= 0 || d->page_size <= 0) return ADASPEC_ERR_DIM;
+    if (remap && (d->batch < 0 || d->window < 0 || d->sinks < 0)) return ADASPEC_ERR_DIM;
+    if (!remap && (d->max_moves < 1 || d->max_moves > d->num_pages)) return ADASPEC_ERR_DIM;
+    if ((int64_t)d->max_pages_per_req * d->page_size > (1 << 30)) return ADASPEC_ERR_UNSUPPORTED;
+    if (remap && (int64_t)d->old_batch + d->batch > 65535) return ADASPEC_ERR_UNSUPPORTED;
+    return ADASPEC_OK;
+}
+
+static bool overlap(const void *a, size_t na, const void *b, size_t nb)
+{
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return na > 0 && nb > 0 && x < y + nb && y < x + na;
+}
+
+size_t adaspec_kv_remap_workspace_bytes(const adaspec_pages_dims *dims)
+{
+    return validate_pages_dims(dims, true) == ADASPEC_OK ? remap_workspace(*dims, nullptr, nullptr) : 0;
+}
+
+int adaspec_kv_remap(const int32_t *block_table, const int32_t *page_refs, const int32_t *sources,
+                     const int32_t *lens, const int32_t *new_lens,
+                     int32_t *out_table, int32_t *out_refs, int32_t *copy_src, int32_t *copy_dst,
+                     int32_t *status, const adaspec_pages_dims *dims,
+                     void *workspace, size_t workspace_bytes, void *stream)
+{
+    const int rc = validate_pages_dims(dims, true);
+    if (rc != ADASPEC_OK) return rc;
+    if (!page_refs || !out_refs || !status || !workspace) return ADASPEC_ERR_NULL;
+    if (dims->old_batch > 0 && (!block_table || !lens)) return ADASPEC_ERR_NULL;
+    if (dims->batch > 0 && (!sources || !new_lens || !out_table || !copy_src || !copy_dst)) return ADASPEC_ERR_NULL;
+    if (reinterpret_cast<uintptr_t>(workspace) & 255u) return ADASPEC_ERR_ALIGN;
+    const size_t row = (size_t)dims->max_pages_per_req * 4, pool = (size_t)dims->num_pages * 4;
+    if (overlap(block_table, dims->old_batch * row, out_table, dims->batch * row)) return ADASPEC_ERR_DIM;
+    if (page_refs != out_refs && overlap(page_refs, pool, out_refs, pool)) return ADASPEC_ERR_DIM;
+    RemapArgs a{block_table, page_refs, sources, lens, new_lens, out_table, out_refs, copy_src, copy_dst, status, *dims,
+                0, nullptr, nullptr, nullptr, nullptr};
+    if (a.dims.sinks > (1 << 30)) a.dims.sinks = 1 << 30;
+    if (workspace_bytes < remap_workspace(*dims, &a, static_cast<char *>(workspace))) return ADASPEC_ERR_WORKSPACE;
+    return launch_kv_remap(a, static_cast<hipStream_t>(stream)) == hipSuccess ? ADASPEC_OK : ADASPEC_ERR_HIP;
+}
+
+size_t adaspec_kv_compact_pages_workspace_bytes(const adaspec_pages_dims *dims)
+{
+    return validate_pages_dims(dims, false) == ADASPEC_OK ? compact_workspace(*dims, nullptr, nullptr) : 0;
+}
+
+int adaspec_kv_compact_pages(const int32_t *block_table, const int32_t *page_refs,
+                             int32_t *out_table, int32_t *out_refs, int32_t *page_map,
+                             int32_t *copy_src, int32_t *copy_dst, int32_t *status,
+                             const adaspec_pages_dims *dims,
+                             void *workspace, size_t workspace_bytes, void *stream)
+{
+    const int rc = validate_pages_dims(dims, false);
+    if (rc != ADASPEC_OK) return rc;
+    if (!page_refs || !out_refs || !page_map || !copy_src || !copy_dst || !status || !workspace) return ADASPEC_ERR_NULL;
+    if (dims->old_batch > 0 && (!block_table || !out_table)) return ADASPEC_ERR_NULL;
+    if (reinterpret_cast<uintptr_t>(workspace) & 255u) return ADASPEC_ERR_ALIGN;
+    const size_t table = (size_t)dims->old_batch * dims->max_pages_per_req * 4, pool = (size_t)dims->num_pages * 4;
+    if (block_table != out_table && overlap(block_table, table, out_table, table)) return ADASPEC_ERR_DIM;
+    if (page_refs != out_refs && overlap(page_refs, pool, out_refs, pool)) return ADASPEC_ERR_DIM;
+    CompactArgs a{block_table, page_refs, out_table, out_refs, page_map, copy_src, copy_dst, status, *dims, 0, 0, nullptr, nullptr};
+    if (workspace_bytes < compact_workspace(*dims, &a, static_cast<char *>(workspace))) return ADASPEC_ERR_WORKSPACE;
+    return launch_kv_compact_pages(a, static_cast<hipStream_t>(stream)) == hipSuccess ? ADASPEC_OK : ADASPEC_ERR_HIP;
+}
+
+int adaspec_kv_copy_pages(void *k_pages, void *v_pages, const int32_t *copy_src, const int32_t *copy_dst,
+                          int32_t n_copies, const adaspec_copy_dims *d, void *stream)
+{
+    if (!d) return ADASPEC_ERR_NULL;
+    if (n_copies < 0 || d->layers < 0 || d->num_pages <= 0 || d->n_kv_heads <= 0 || d->page_size <= 0 || d->head_dim <= 0)
+        return ADASPEC_ERR_DIM;
+    if (!dtype_ok(d->dtype)) return ADASPEC_ERR_DTYPE;
+    const int esize = d->dtype == ADASPEC_F32 ? 4 : 2;
+    if ((int64_t)d->head_dim * esize % 16) return ADASPEC_ERR_UNSUPPORTED;
+    // (a page below 2 GB: offsets inside it have 32 bits)
+    if ((double)d->n_kv_heads * d->page_size * d->head_dim * esize >= 2147483648.0) return ADASPEC_ERR_UNSUPPORTED;
+    if (n_copies == 0 || d->layers == 0) return ADASPEC_OK;
+    if (!k_pages || !v_pages || !copy_src || !copy_dst) return ADASPEC_ERR_NULL;
+    if (!aligned16(k_pages) || !aligned16(v_pages)) return ADASPEC_ERR_ALIGN;
+    return launch_kv_copy_pages(k_pages, v_pages, copy_src, copy_dst, n_copies, *d, static_cast<hipStream_t>(stream)) == hipSuccess
+               ? ADASPEC_OK : ADASPEC_ERR_HIP;
+}
+
 static int validate_draft_dims(const adaspec_draft_dims *d)
 {
     if (!d) return ADASPEC_ERR_NULL;
