@@ -194,9 +194,13 @@ hipError_t launch_attn_combine(const AttnArgs &a);
 int attn_combine_waves(const AttnPlan &p, const adaspec_attn_dims &d);   // wavefronts per (row, head) of the combine kernel
 
 // ---- windowed attention (attn_window.hip) --------------------------------------
+enum class WindowKind { kVector, kMfma };
 struct WindowPlan {
+    WindowKind kind;
     int groups, rows_per_group;     // row groups of a request with max_spec_len + 1 rows, query rows (times G) in one
     int64_t units;                  // batch * n_kv_heads * groups
+    int splits, block_pages;        // parts that the blocks of a unit's pages are cut into at most; pages per block
+    size_t off_part_ml, off_part_o; // float[units][splits][rows_per_group][2], [d]: states of the parts
     size_t total_bytes;
 };
 struct WindowArgs {
@@ -211,6 +215,7 @@ struct WindowArgs {
     hipStream_t stream;
 };
 WindowPlan make_window_plan(const adaspec_attn_dims &d, int window, int sinks);
+bool window_fast_supported(const adaspec_attn_dims &d);
 hipError_t launch_attn_window(const WindowArgs &a);
 
 // ---- accept workspace ------------------------------------------------------

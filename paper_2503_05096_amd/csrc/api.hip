@@ -416,14 +416,19 @@ int adaspec_verify_attn_tree(const void *q, const void *k_pages, const void *v_p
 // dims of a windowed call; window and sinks are cut to what a block table can hold
 static int validate_window(const adaspec_attn_dims *d, int32_t &window, int32_t &sinks)
 {
-    const int rc = validate_attn_dims(d);
+    if (!d) return ADASPEC_ERR_NULL;
+    adaspec_attn_dims any = *d;                                     // (FAST has other shapes here)
+    if (any.path == ADASPEC_PATH_FAST) any.path = ADASPEC_PATH_AUTO;
+    const int rc = validate_attn_dims(&any);
     if (rc != ADASPEC_OK) return rc;
     if (window < 1 || sinks < 0) return ADASPEC_ERR_DIM;
+    if (d->path == ADASPEC_PATH_FAST && !window_fast_supported(*d)) return ADASPEC_ERR_UNSUPPORTED;
     const int64_t tokens = (int64_t)d->max_pages_per_req * d->page_size;
     if (tokens > (1 << 30)) return ADASPEC_ERR_UNSUPPORTED;
     if (window > tokens) window = (int32_t)tokens;
     if (sinks > tokens) sinks = (int32_t)tokens;
-    if (make_window_plan(*d, window, sinks).units > INT32_MAX) return ADASPEC_ERR_UNSUPPORTED;
+    const WindowPlan p = make_window_plan(*d, window, sinks);
+    if (p.units * p.splits > INT32_MAX) return ADASPEC_ERR_UNSUPPORTED;
     return ADASPEC_OK;
 }
 

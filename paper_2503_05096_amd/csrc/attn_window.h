@@ -54,4 +54,6 @@ __device__ __forceinline__ bool window_sees(const WindowUnit &u, int pos, int t)
     return t <= pos && (pos - t < u.window || t < u.sinks);
 }
 
+hipError_t launch_attn_window_mfma(const WindowArgs &a, const WindowDims &w);
+
 }  // namespace adaspec

@@ -112,15 +112,38 @@ __global__ __launch_bounds__(64) void attn_window_vector_kernel(WindowDims dims,
     }
 }
 
+bool window_fast_supported(const adaspec_attn_dims &d)
+{
+    return d.dtype != ADASPEC_F32 && (d.head_dim == 64 || d.head_dim == 128);
+}
+
 WindowPlan make_window_plan(const adaspec_attn_dims &d, int window, int sinks)
 {
-    (void)window; (void)sinks;
     WindowPlan p;
-    const int rows = (d.max_spec_len + 1) * (d.n_q_heads / d.n_kv_heads);
-    p.rows_per_group = kWinRows;
-    p.groups = ceil_div(rows, p.rows_per_group);
+    const int G = d.n_q_heads / d.n_kv_heads;
+    const int64_t rows = (int64_t)(d.max_spec_len + 1) * G;
+    p.kind = d.path != ADASPEC_PATH_VECTOR && window_fast_supported(d) ? WindowKind::kMfma : WindowKind::kVector;
+    p.rows_per_group = p.kind == WindowKind::kVector ? kWinRows : 16 * (int)(rows < 64 ? (rows + 15) / 16 : 4);
+    p.groups = (int)((rows + p.rows_per_group - 1) / p.rows_per_group);
     p.units = (int64_t)d.batch * d.n_kv_heads * p.groups;
-    p.total_bytes = 256;
+    p.splits = 1;
+    p.block_pages = d.head_dim == 64 ? 4 : 2;
+    if (p.kind == WindowKind::kMfma) {
+        // entries of a unit's list of pages at most: a row group spans this many positions
+        const int64_t span = (p.rows_per_group - 1) / G + 2 < d.max_spec_len + 1 ? (p.rows_per_group - 1) / G + 2 : d.max_spec_len + 1;
+        int64_t pages = ((int64_t)sinks + 15) / 16 + ((int64_t)window + span + 14) / 16 + 1;
+        if (pages > d.max_pages_per_req) pages = d.max_pages_per_req;
+        const int64_t turns = (pages + 4 * p.block_pages - 1) / (4 * p.block_pages);       // of the four wavefronts
+        int64_t want = p.units > 0 ? 512 / p.units : 1;
+        if (want > turns / 2) want = turns / 2;
+        p.splits = (int)(want > 1 ? want : 1);
+    }
+    size_t off = 0;
+    p.off_part_ml = off;
+    if (p.splits > 1) off = align_up(off + (size_t)p.units * p.splits * p.rows_per_group * 2 * sizeof(float), 256);
+    p.off_part_o = off;
+    if (p.splits > 1) off = align_up(off + (size_t)p.units * p.splits * p.rows_per_group * d.head_dim * sizeof(float), 256);
+    p.total_bytes = off > 0 ? off : 256;
     return p;
 }
 
@@ -129,6 +152,7 @@ hipError_t launch_attn_window(const WindowArgs &a)
     const adaspec_attn_dims &d = a.dims;
     const WindowDims w{a.block_table, a.ctx_lens, a.spec_lens, d.total_q, d.max_spec_len, d.max_pages_per_req, d.n_q_heads,
                        d.n_kv_heads, a.window, a.sinks, a.plan.groups, a.plan.rows_per_group};
+    if (a.plan.kind == WindowKind::kMfma) return launch_attn_window_mfma(a, w);
     auto launch = [&](auto tag) {
         hipLaunchKernelGGL(attn_window_vector_kernel<decltype(tag)>, dim3((unsigned)a.plan.units), dim3(64), 0, a.stream, w, a.q,
                            a.k_pages, a.v_pages, a.out, d.head_dim, a.scale_log2, d.out_dtype);

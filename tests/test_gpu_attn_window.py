@@ -111,8 +111,11 @@ def test_long_drafts(dtype, d, pkg):  # noqa: F811
 @pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
 @pytest.mark.parametrize("path", ["auto", "vector"])
 def test_what_a_row_does_not_see_cannot_reach_it(dtype, path, pkg):  # noqa: F811
-    """NaN and infinities in tokens that some rows of a request see and others do not."""
+    """NaN and infinities in tokens that some rows of a request see and others do not.  Rows that see none of them are worked
+out in another way than without them: both are fp32 (2e-6), but the matrix cores take bf16 weights in two pieces, of which the
+first is off by at most 2^-9 of the weight and the second by at most 2^-9 of that: 2^-18 of a mean of values below 5."""
     window, sinks = 20, 2
+    tol = 2e-6 + (5 * 2.0 ** -18 if dtype == "bf16" else 0.0)
     for d in (64, 128):
         for bad in (np.nan, np.inf, -np.inf):
             st = step(1000, [50, 90], [5, 7], 8, 2, d, dtype)
@@ -133,7 +136,7 @@ def test_what_a_row_does_not_see_cannot_reach_it(dtype, path, pkg):  # noqa: F81
                     if any(t <= pos and pos - t < window for t in (L - n - window + 3, L - 2)):
                         assert not np.isfinite(out[row]).all(), (d, bad, i, j)
                     else:
-                        assert np.abs(out[row] - clean[row]).max() <= 2e-6, (d, bad, i, j)
+                        assert float(np.abs(out[row] - clean[row]).max()) <= tol, (d, bad, i, j)
                     row += 1
 
 
