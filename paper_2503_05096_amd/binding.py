@@ -87,7 +87,9 @@ _fast = None        # the _fastcall module once the library is loaded
 _FAST_ENTRIES = ("adaspec_verify_attn_workspace_bytes", "adaspec_verify_attn", "adaspec_verify_attn_tree",
                  "adaspec_accept_workspace_bytes", "adaspec_accept", "adaspec_accept_tree", "adaspec_kv_append",
                  "adaspec_kv_compact_path", "adaspec_commit", "adaspec_draft_sample_workspace_bytes",
-                 "adaspec_draft_sample")
+                 "adaspec_draft_sample",
+                 "adaspec_verify_attn_window_workspace_bytes", "adaspec_verify_attn_window", "adaspec_kv_remap_workspace_bytes",
+                 "adaspec_kv_remap", "adaspec_kv_compact_pages_workspace_bytes", "adaspec_kv_compact_pages", "adaspec_kv_copy_pages")
 
 
 def _native():
@@ -118,6 +120,7 @@ class _PythonOnly:
     def _decline(*args):
         return NotImplemented
     verify_attn = accept = accept_tree = kv_append = kv_compact_path = commit = draft_sample = _decline
+    verify_attn_window = kv_remap = kv_compact_pages = kv_copy_pages = _decline
 
 
 def lib() -> C.CDLL:
@@ -217,6 +220,11 @@ def version() -> int:
 # --------------------------------------------------------------------------
 # torch-facing wrappers
 # --------------------------------------------------------------------------
+def _int32(n) -> int:
+    """n, cut to 32 bits: a window of more tokens than there are"""
+    return max(min(int(n), 2 ** 31 - 1), -2 ** 31)
+
+
 def _dtype_code(t) -> int:
     import torch
     return {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}[t.dtype]
@@ -295,6 +303,12 @@ def verify_attn(q, k_pages, v_pages, block_table, ctx_lens, spec_lens, out=None,
             raise ValueError("verify_attn(sinks=...) needs a window: without one every token is visible")
         if parents is not None:
             raise ValueError("verify_attn(window=...) takes chains of drafts, not trees (parents=)")
+        window, sinks = _int32(window), _int32(sinks)
+        if path == "auto" and timing is None:
+            r = (_fast or _native()).verify_attn_window(q, k_pages, v_pages, block_table, ctx_lens, spec_lens, out, max_spec_len,
+                                                        scale, out_dtype, plan, workspace, stream, window, sinks)
+            if r is not NotImplemented:
+                return r
     elif path == "auto" and timing is None:
         r = (_fast or _native()).verify_attn(q, k_pages, v_pages, block_table, ctx_lens, spec_lens, out, max_spec_len,
                                              scale, out_dtype, plan, workspace, stream, parents)
@@ -311,7 +325,7 @@ def verify_attn(q, k_pages, v_pages, block_table, ctx_lens, spec_lens, out=None,
         out = torch.empty(q.shape, dtype=_torch_dtype(dims.out_dtype), device=q.device)
     L = lib()
     if window is not None:
-        return _verify_attn_window(q, k_pages, v_pages, block_table, ctx_lens, spec_lens, out, dims, int(window), int(sinks), plan,
+        return _verify_attn_window(q, k_pages, v_pages, block_table, ctx_lens, spec_lens, out, dims, window, sinks, plan,
                                    workspace, stream)
     need = L.adaspec_verify_attn_workspace_bytes(C.byref(dims))
     if need == 0 and dims.batch > 0:
@@ -549,7 +563,7 @@ def check_ragged_inputs(block_table, ctx_lens, spec_lens, dims: AttnDims, stream
     flags = torch.zeros(1, dtype=torch.int32, device=block_table.device)
     if window is not None:
         rc = lib().adaspec_check_window_inputs(block_table.data_ptr(), ctx_lens.data_ptr(), spec_lens.data_ptr(), C.byref(dims),
-                                               int(window), int(sinks), flags.data_ptr(), _stream_ptr(stream))
+                                               _int32(window), _int32(sinks), flags.data_ptr(), _stream_ptr(stream))
         if rc != 0:
             raise AdaspecError(rc, "adaspec_check_window_inputs")
         return int(flags.item())
@@ -655,6 +669,11 @@ def kv_remap(block_table, page_refs, sources, lens, new_lens, *, window: Optiona
         raise ValueError("kv_remap(sinks=...) needs a window: without one every token is visible")
     if window is not None and window < 1:
         raise ValueError("kv_remap(window=...) is at least 1 (None: no window)")
+    window, sinks = 0 if window is None else _int32(window), _int32(sinks)
+    r = (_fast or _native()).kv_remap(block_table, page_refs, sources, lens, new_lens, window, sinks, page_size, out_table, out_refs,
+                                      copy_src, copy_dst, status, workspace, stream)
+    if r is not NotImplemented:
+        return r
     old_batch, max_pages = block_table.shape
     batch, num_pages = sources.shape[0], page_refs.shape[0]
     _dense_ints(block_table, page_refs, sources, lens, new_lens)
@@ -665,7 +684,7 @@ def kv_remap(block_table, page_refs, sources, lens, new_lens, *, window: Optiona
     copy_src = _ints_like(copy_src, (batch,), block_table)
     copy_dst = _ints_like(copy_dst, (batch,), block_table)
     status = _ints_like(status, (2,), block_table)
-    dims = PagesDims(batch, old_batch, max_pages, num_pages, int(page_size), 0 if window is None else int(window), int(sinks), 0)
+    dims = PagesDims(batch, old_batch, max_pages, num_pages, int(page_size), window, sinks, 0)
     L = lib()
     ws = _workspace(L.adaspec_kv_remap_workspace_bytes(C.byref(dims)), block_table.device, workspace, "pages")
     rc = L.adaspec_kv_remap(block_table.data_ptr(), page_refs.data_ptr(), sources.data_ptr(), lens.data_ptr(), new_lens.data_ptr(),
@@ -683,10 +702,14 @@ def kv_compact_pages(block_table, page_refs, *, max_moves: Optional[int] = None,
     enough.  out_table may be block_table, out_refs may be page_refs."""
     batch, max_pages = block_table.shape
     num_pages = page_refs.shape[0]
+    max_moves = max(1, num_pages // 2) if max_moves is None else int(max_moves)
+    r = (_fast or _native()).kv_compact_pages(block_table, page_refs, max_moves, page_size, out_table, out_refs, page_map, copy_src,
+                                              copy_dst, status, workspace, stream)
+    if r is not NotImplemented:
+        return r
     _dense_ints(block_table, page_refs)
     _on_current_device(block_table)
     assert page_refs.shape == (num_pages,)
-    max_moves = max(1, num_pages // 2) if max_moves is None else int(max_moves)
     if max_moves < 1:
         raise ValueError("kv_compact_pages(max_moves=...) is at least 1")
     out_table = _ints_like(out_table, (batch, max_pages), block_table)
@@ -709,6 +732,8 @@ def kv_compact_pages(block_table, page_refs, *, max_moves: Optional[int] = None,
 def kv_copy_pages(k_pages, v_pages, copy_src, copy_dst, *, stream=None) -> None:
     """adaspec_kv_copy_pages: pages copy_src[c] -> copy_dst[c] of K and V, in place; pairs with -1 are left out.
     k_pages, v_pages: the pages of one layer [num_pages][Hkv][P][d], or of several [layers][num_pages][Hkv][P][d]."""
+    if (_fast or _native()).kv_copy_pages(k_pages, v_pages, copy_src, copy_dst, stream) is not NotImplemented:
+        return
     assert k_pages.dim() in (4, 5)
     layers = k_pages.shape[0] if k_pages.dim() == 5 else 1
     num_pages, Hkv, P, d = k_pages.shape[-4:]

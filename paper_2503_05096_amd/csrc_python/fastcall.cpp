@@ -57,14 +57,23 @@ struct Api {
     decltype(&adaspec_commit) commit;
     decltype(&adaspec_draft_sample_workspace_bytes) draft_ws;
     decltype(&adaspec_draft_sample) draft;
+    // (from here on optional in setup(): a call whose entry point is not there is left to Python)
+    decltype(&adaspec_verify_attn_window_workspace_bytes) attn_window_ws;
+    decltype(&adaspec_verify_attn_window) attn_window;
+    decltype(&adaspec_kv_remap_workspace_bytes) remap_ws;
+    decltype(&adaspec_kv_remap) remap;
+    decltype(&adaspec_kv_compact_pages_workspace_bytes) compact_ws;
+    decltype(&adaspec_kv_compact_pages) compact;
+    decltype(&adaspec_kv_copy_pages) copy_pages;
 } api;
+constexpr Py_ssize_t kEntries = sizeof(Api) / sizeof(void *), kRequired = kEntries - 7;
 PyObject *get_workspace, *raw_stream, *current_device;   // binding._workspace, torch._C._cuda_getCurrentRawStream / _getDevice
 PyObject *error_class;                                   // binding.AdaspecError
 bool ready = false;
 
 // the default workspaces in use: [family][device], the tensors of binding._ws_cache
-enum Family { kAttn, kAccept, kDraft, kFamilies };
-const char *const kFamilyName[kFamilies] = {"attn", "accept", "draft"};
+enum Family { kAttn, kAccept, kDraft, kPages, kFamilies };
+const char *const kFamilyName[kFamilies] = {"attn", "accept", "draft", "pages"};
 // (never destroyed: at process exit the allocator may be gone before a static's destructor runs)
 auto &workspaces = *new std::array<std::vector<at::Tensor>, kFamilies>;
 
@@ -193,6 +202,16 @@ struct Output {
     PyObject *result() const { return Py_NewRef(object); }
 };
 
+// tensors of one device, which is the current one
+void on_current_device(std::initializer_list<const at::Tensor *> all)
+{
+    PyObject *dev = PyObject_CallNoArgs(current_device);
+    if (!dev) failed_in_python();
+    const long index = PyLong_Check(dev) ? PyLong_AsLong(dev) : -1;
+    Py_DECREF(dev);
+    for (const at::Tensor *t : all) need(device_index(*t) == index);
+}
+
 struct Unlocked {                                      // the interpreter lock is given up for the life of this object
     PyThreadState *state = PyEval_SaveThread();
     ~Unlocked() { PyEval_RestoreThread(state); }
@@ -283,6 +302,132 @@ PyObject *verify_attn(PyObject *, PyObject *const *a, Py_ssize_t nargs)
         const Output out(a[6], q.sizes(), scalar_type(d.out_dtype), q);
         run(ptr(out.t));
         return out.result();
+    });
+}
+
+// (q, k_pages, v_pages, block_table, ctx_lens, spec_lens, out, max_spec_len, scale, out_dtype, plan, workspace, stream, window, sinks)
+PyObject *verify_attn_window(PyObject *, PyObject *const *a, Py_ssize_t nargs)
+{
+    return guarded(nargs, 15, [&]() -> PyObject * {
+        need(api.attn_window && is_word(a[10], "run"));
+        const at::Tensor &q = tensor(a[0]), &k = tensor(a[1]), &v = tensor(a[2]);
+        const at::Tensor &bt = dense(a[3], at::kInt), &ctx = dense(a[4], at::kInt), &spec = dense(a[5], at::kInt);
+        need(q.dim() == 3 && k.dim() == 4 && bt.dim() == 2 && ctx.dim() == 1 && spec.dim() == 1);
+        need(q.is_contiguous() && k.is_contiguous() && v.is_contiguous() && ctx.size(0) == bt.size(0) && spec.size(0) == bt.size(0));
+        need(v.sizes() == k.sizes() && q.scalar_type() == k.scalar_type() && v.scalar_type() == k.scalar_type());
+        adaspec_attn_dims d = {};
+        d.batch = size32(bt.size(0));
+        d.total_q = size32(q.size(0));
+        d.max_spec_len = small_int(a[7]);
+        d.n_q_heads = size32(q.size(1));
+        d.n_kv_heads = size32(k.size(1));
+        d.head_dim = size32(q.size(2));
+        d.page_size = size32(k.size(2));
+        d.num_pages = size32(k.size(0));
+        d.max_pages_per_req = size32(bt.size(1));
+        d.dtype = dtype_code(q.scalar_type());
+        d.out_dtype = a[9] == Py_None ? d.dtype : small_int(a[9]);
+        need(PyFloat_CheckExact(a[8]));
+        d.scale = (float)PyFloat_AS_DOUBLE(a[8]);
+        const int32_t window = small_int(a[13]), sinks = small_int(a[14]);
+        const size_t nbytes = api.attn_window_ws(&d, window, sinks);
+        need(nbytes > 0);
+        on_current_device({&q, &k, &v, &bt, &ctx, &spec});
+        const Output out(a[6], q.sizes(), scalar_type(d.out_dtype), q);
+        need(out.t.is_contiguous() && out.t.sizes() == q.sizes() && out.t.scalar_type() == scalar_type(d.out_dtype));
+        const at::Tensor ws = workspace(a[11], nbytes, kAttn, q);
+        void *s = stream_of(a[12]);
+        call("adaspec_verify_attn_window", api.attn_window, ptr(q), ptr(k), ptr(v), ptr<int32_t>(bt), ptr<int32_t>(ctx), ptr<int32_t>(spec), ptr(out.t), &d,
+             window, sinks, ptr(ws), (size_t)ws.numel(), s);
+        return out.result();
+    });
+}
+
+// an integer output: the caller's tensor of exactly this shape, or a new one
+struct Ints : Output {
+    Ints(PyObject *given, at::IntArrayRef shape, const at::Tensor &like) : Output(given, shape, at::kInt, like)
+    {
+        need(t.scalar_type() == at::kInt && t.is_contiguous() && t.sizes() == shape && device_index(t) == device_index(like));
+    }
+};
+
+// (block_table, page_refs, sources, lens, new_lens, window or 0, sinks, page_size, out_table, out_refs, copy_src, copy_dst, status,
+//  workspace, stream)
+PyObject *kv_remap(PyObject *, PyObject *const *a, Py_ssize_t nargs)
+{
+    return guarded(nargs, 15, [&]() -> PyObject * {
+        need(api.remap != nullptr);
+        const at::Tensor &bt = dense(a[0], at::kInt), &refs = dense(a[1], at::kInt), &src = dense(a[2], at::kInt);
+        const at::Tensor &lens = dense(a[3], at::kInt), &more = dense(a[4], at::kInt);
+        need(bt.dim() == 2 && refs.dim() == 1 && src.dim() == 1 && lens.dim() == 1 && more.dim() == 1);
+        need(lens.size(0) == bt.size(0) && more.size(0) == src.size(0));
+        adaspec_pages_dims d = {};
+        d.batch = size32(src.size(0));
+        d.old_batch = size32(bt.size(0));
+        d.max_pages_per_req = size32(bt.size(1));
+        d.num_pages = size32(refs.size(0));
+        d.page_size = small_int(a[7]);
+        d.window = small_int(a[5]);
+        d.sinks = small_int(a[6]);
+        const size_t nbytes = api.remap_ws(&d);
+        need(nbytes > 0);
+        on_current_device({&bt, &refs, &src, &lens, &more});
+        const Ints table(a[8], {d.batch, d.max_pages_per_req}, bt), counts(a[9], {d.num_pages}, bt), cs(a[10], {d.batch}, bt), cd(a[11], {d.batch}, bt);
+        const Ints status(a[12], {2}, bt);
+        const at::Tensor ws = workspace(a[13], nbytes, kPages, bt);
+        void *s = stream_of(a[14]);
+        call("adaspec_kv_remap", api.remap, ptr<int32_t>(bt), ptr<int32_t>(refs), ptr<int32_t>(src), ptr<int32_t>(lens), ptr<int32_t>(more),
+             ptr<int32_t>(table.t), ptr<int32_t>(counts.t), ptr<int32_t>(cs.t), ptr<int32_t>(cd.t), ptr<int32_t>(status.t), &d, ptr(ws), (size_t)ws.numel(), s);
+        return Py_BuildValue("(NNNNN)", table.result(), counts.result(), cs.result(), cd.result(), status.result());
+    });
+}
+
+// (block_table, page_refs, max_moves, page_size, out_table, out_refs, page_map, copy_src, copy_dst, status, workspace, stream)
+PyObject *kv_compact_pages(PyObject *, PyObject *const *a, Py_ssize_t nargs)
+{
+    return guarded(nargs, 12, [&]() -> PyObject * {
+        need(api.compact != nullptr);
+        const at::Tensor &bt = dense(a[0], at::kInt), &refs = dense(a[1], at::kInt);
+        need(bt.dim() == 2 && refs.dim() == 1);
+        adaspec_pages_dims d = {};
+        d.old_batch = size32(bt.size(0));
+        d.max_pages_per_req = size32(bt.size(1));
+        d.num_pages = size32(refs.size(0));
+        d.max_moves = small_int(a[2]);
+        d.page_size = small_int(a[3]);
+        const size_t nbytes = api.compact_ws(&d);
+        need(nbytes > 0);
+        on_current_device({&bt, &refs});
+        const Ints table(a[4], bt.sizes(), bt), counts(a[5], {d.num_pages}, bt), map(a[6], {d.num_pages}, bt);
+        const Ints cs(a[7], {d.max_moves}, bt), cd(a[8], {d.max_moves}, bt), status(a[9], {2}, bt);
+        const at::Tensor ws = workspace(a[10], nbytes, kPages, bt);
+        void *s = stream_of(a[11]);
+        call("adaspec_kv_compact_pages", api.compact, ptr<int32_t>(bt), ptr<int32_t>(refs), ptr<int32_t>(table.t), ptr<int32_t>(counts.t), ptr<int32_t>(map.t),
+             ptr<int32_t>(cs.t), ptr<int32_t>(cd.t), ptr<int32_t>(status.t), &d, ptr(ws), (size_t)ws.numel(), s);
+        return Py_BuildValue("(NNNNNN)", table.result(), counts.result(), map.result(), cs.result(), cd.result(), status.result());
+    });
+}
+
+// (k_pages, v_pages, copy_src, copy_dst, stream)
+PyObject *kv_copy_pages(PyObject *, PyObject *const *a, Py_ssize_t nargs)
+{
+    return guarded(nargs, 5, [&]() -> PyObject * {
+        need(api.copy_pages != nullptr);
+        const at::Tensor &k = tensor(a[0]), &v = tensor(a[1]), &src = dense(a[2], at::kInt), &dst = dense(a[3], at::kInt);
+        const int64_t n = k.dim();
+        need((n == 4 || n == 5) && v.sizes() == k.sizes() && k.is_contiguous() && v.is_contiguous() && v.scalar_type() == k.scalar_type());
+        need(src.dim() == 1 && dst.sizes() == src.sizes());
+        adaspec_copy_dims d = {};
+        d.layers = n == 5 ? size32(k.size(0)) : 1;
+        d.num_pages = size32(k.size(n - 4));
+        d.n_kv_heads = size32(k.size(n - 3));
+        d.page_size = size32(k.size(n - 2));
+        d.head_dim = size32(k.size(n - 1));
+        d.dtype = dtype_code(k.scalar_type());
+        on_current_device({&k, &v, &src, &dst});
+        void *s = stream_of(a[4]);
+        call("adaspec_kv_copy_pages", api.copy_pages, ptr(k), ptr(v), ptr<int32_t>(src), ptr<int32_t>(dst), size32(src.size(0)), &d, s);
+        Py_RETURN_NONE;
     });
 }
 
@@ -471,11 +616,12 @@ PyObject *setup(PyObject *, PyObject *args)
     PyObject *table, *ws, *stream, *device, *error;
     if (!PyArg_ParseTuple(args, "O!OOOO", &PyTuple_Type, &table, &ws, &stream, &device, &error)) return nullptr;
     void **slot = reinterpret_cast<void **>(&api);
-    constexpr Py_ssize_t n = sizeof(Api) / sizeof(void *);
-    if (PyTuple_GET_SIZE(table) != n) {
-        PyErr_Format(PyExc_ValueError, "expected %zd entry points", n);
+    const Py_ssize_t n = PyTuple_GET_SIZE(table);
+    if (n != kRequired && n != kEntries) {
+        PyErr_Format(PyExc_ValueError, "expected %zd or %zd entry points", kRequired, kEntries);
         return nullptr;
     }
+    api = {};
     for (Py_ssize_t i = 0; i < n; ++i) {
         slot[i] = PyLong_AsVoidPtr(PyTuple_GET_ITEM(table, i));
         if (PyErr_Occurred()) return nullptr;
@@ -498,7 +644,8 @@ PyObject *set_meta_index(PyObject *, PyObject *i)
 
 #define FASTCALL(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FASTCALL(verify_attn), FASTCALL(accept), FASTCALL(accept_tree), FASTCALL(kv_append),
-                         FASTCALL(kv_compact_path), FASTCALL(commit), FASTCALL(draft_sample),
+                         FASTCALL(kv_compact_path), FASTCALL(commit), FASTCALL(draft_sample), FASTCALL(verify_attn_window),
+                         FASTCALL(kv_remap), FASTCALL(kv_compact_pages), FASTCALL(kv_copy_pages),
 #ifdef ADASPEC_FASTCALL_ON_META
                          {"set_meta_index", set_meta_index, METH_O, nullptr},
 #endif

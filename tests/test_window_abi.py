@@ -22,8 +22,8 @@ def _bytes(dims, window=100, sinks=4):
     (dict(out_dtype=1), -3), (dict(page_size=32), -6), (dict(head_dim=100), -6), (dict(head_dim=512), -6), (dict(path=3), -2),
     (dict(scale=-1.0), -2), (dict(plan_mode=3), -2), (dict(max_spec_len=-1), -2),
     (dict(max_pages_per_req=(1 << 26) + 1, batch=1, total_q=1, max_spec_len=0), -6),            # more than 2^30 tokens in a row
-    # units that do not fit the grid: 4096 requests of 8192 rows with 1024 kv heads
-    (dict(batch=1 << 13, total_q=1 << 13, max_spec_len=8191, n_q_heads=1024, n_kv_heads=1024, max_pages_per_req=1), -6),
+    # units that do not fit the grid: 16384 requests of 8192 rows with 1024 kv heads
+    (dict(batch=1 << 14, total_q=1 << 14, max_spec_len=8191, n_q_heads=1024, n_kv_heads=1024, max_pages_per_req=1), -6),
 ])
 def test_bad_dims(kw, code):
     d = _attn_dims(**kw)
