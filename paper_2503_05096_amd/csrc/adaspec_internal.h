@@ -306,8 +306,10 @@ struct RemapArgs {
     const int32_t *block_table, *page_refs, *sources, *lens, *new_lens;
     int32_t *out_table, *out_refs, *copy_src, *copy_dst, *status;
     adaspec_pages_dims dims;
-    int chunks;                                                     // of the pool's pages
-    int32_t *chunk_free, *part, *want_base, *copies;                // workspace: [chunks], [batch], [batch + 1], [batch]
+    int chunks, tiles;                                              // of the pool's pages, of the new rows
+    int32_t *chunk_free, *tile_wants;                               // workspace: [chunks], [tiles]
+    int4 *want;                                                     // workspace: [batch]
+    int2 *rows, *writers;                                           // workspace: [batch], [num_pages]
 };
 struct CompactArgs {
     const int32_t *block_table, *page_refs;

@@ -766,6 +766,7 @@ static int validate_pages_dims(const adaspec_pages_dims *d, bool remap)
     if (!remap && (d->max_moves < 1 || d->max_moves > d->num_pages)) return ADASPEC_ERR_DIM;
     if ((int64_t)d->max_pages_per_req * d->page_size > (1 << 30)) return ADASPEC_ERR_UNSUPPORTED;
     if (remap && (int64_t)d->old_batch + d->batch > 65535) return ADASPEC_ERR_UNSUPPORTED;
+    if (remap && d->batch * ((int64_t)d->max_pages_per_req + 1) >= (1 << 30)) return ADASPEC_ERR_UNSUPPORTED;       // (wants are counted in 32 bits)
     return ADASPEC_OK;
 }
 
@@ -796,7 +797,7 @@ int adaspec_kv_remap(const int32_t *block_table, const int32_t *page_refs, const
     if (overlap(block_table, dims->old_batch * row, out_table, dims->batch * row)) return ADASPEC_ERR_DIM;
     if (page_refs != out_refs && overlap(page_refs, pool, out_refs, pool)) return ADASPEC_ERR_DIM;
     RemapArgs a{block_table, page_refs, sources, lens, new_lens, out_table, out_refs, copy_src, copy_dst, status, *dims,
-                0, nullptr, nullptr, nullptr, nullptr};
+                0, 0, nullptr, nullptr, nullptr, nullptr, nullptr};
     if (a.dims.sinks > (1 << 30)) a.dims.sinks = 1 << 30;
     if (workspace_bytes < remap_workspace(*dims, &a, static_cast<char *>(workspace))) return ADASPEC_ERR_WORKSPACE;
     return launch_kv_remap(a, static_cast<hipStream_t>(stream)) == hipSuccess ? ADASPEC_OK : ADASPEC_ERR_HIP;

@@ -411,37 +411,49 @@ __global__ __launch_bounds__(256, 2) void attn_window_kernel(WindowDims dims, co
     }
 }
 
-// Rows of a unit whose pages were cut: out = sum_s 2^(m_s - m*) O_s / sum_s 2^(m_s - m*) l_s.  One wavefront per (row, head).
+// Rows of a unit whose pages were cut: out = sum_s 2^(m_s - m*) O_s / sum_s 2^(m_s - m*) l_s.  One wavefront per row, four
+// rows of a unit per workgroup; lane s looks at (m_s, l_s), the O_s are requested four at a time.
 template <int D>
 __global__ __launch_bounds__(256) void attn_window_combine_kernel(WindowDims dims, const float *__restrict__ part_ml,
                                                                   const float *__restrict__ part_o, void *__restrict__ out, int splits,
                                                                   int block_pages, int out_dtype)
 {
-    const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
-    const int unit = blockIdx.x;
+    constexpr int kE = D / 64;
+    const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int quads = dims.rows_per_group / 4, unit = blockIdx.x / quads, rl = 4 * (blockIdx.x % quads) + wv;
     WindowUnit u;
     if (!window_unit(u, dims, unit / (dims.Hkv * dims.groups), unit / dims.Hkv % dims.groups, unit % dims.Hkv, lane)) return;
+    const int row = u.r0 + rl;
     const int all_blocks = (u.pages + block_pages - 1) / block_pages, per = (all_blocks + splits - 1) / splits;
-    const int ns = per > 0 ? (all_blocks + per - 1) / per : 1;
-    if (ns == 1) return;
-    const int G = dims.Hq / dims.Hkv;
-    for (int rl = wv; rl < dims.rows_per_group && u.r0 + rl < u.rows; rl += 4) {
-        const int row = u.r0 + rl;
-        const int64_t first = (int64_t)unit * splits * dims.rows_per_group + rl;
-        float m = -INFINITY;
-        for (int s = 0; s < ns; ++s) m = fmaxf(m, part_ml[(first + (int64_t)s * dims.rows_per_group) * 2]);
-        float den = 0.f, acc[D / 64] = {};
-        for (int s = 0; s < ns; ++s) {
-            const int64_t at = first + (int64_t)s * dims.rows_per_group;
-            const float w = m > -INFINITY ? __builtin_amdgcn_exp2f(part_ml[at * 2] - m) : 1.f;
-            den += w * part_ml[at * 2 + 1];
+    const int ns = per > 0 ? (all_blocks + per - 1) / per : 1;      // (at most 64)
+    if (ns == 1 || row >= u.rows) return;
+    const int64_t first = (int64_t)unit * splits * dims.rows_per_group + rl;
+    float2 ml = make_float2(-INFINITY, 0.f);
+    if (lane < ns) ml = *reinterpret_cast<const float2 *>(part_ml + (first + (int64_t)lane * dims.rows_per_group) * 2);
+    const float m = wave_max(ml.x);
+    const float w = lane < ns ? (m > -INFINITY ? __builtin_amdgcn_exp2f(ml.x - m) : 1.f) : 0.f;
+    const float den = wave_sum(w * ml.y);
+    float acc[kE] = {};
+    const float *o = part_o + first * D + kE * lane;
+    for (int s0 = 0; s0 < ns; s0 += 4) {
+        float x[4][kE];
 #pragma unroll
-            for (int e = 0; e < D / 64; ++e) acc[e] += w * part_o[at * D + lane + 64 * e];
+        for (int s = 0; s < 4; ++s)
+#pragma unroll
+            for (int e = 0; e < kE; ++e) x[s][e] = o[(int64_t)min(s0 + s, ns - 1) * dims.rows_per_group * D + e];
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            const float ws = __shfl(w, s0 + s, kWave);              // (0 behind the last)
+            if (s0 + s < ns) {
+#pragma unroll
+                for (int e = 0; e < kE; ++e) acc[e] += ws * x[s][e];
+            }
         }
-        const int64_t obase = ((u.qrow0 + row / G) * dims.Hq + u.gkv * G + row % G) * (int64_t)D;
-#pragma unroll
-        for (int e = 0; e < D / 64; ++e) store_out(out, obase + lane + 64 * e, acc[e] * (1.0f / den), out_dtype);
     }
+    const int G = dims.Hq / dims.Hkv;
+    const int64_t obase = ((u.qrow0 + row / G) * dims.Hq + u.gkv * G + row % G) * (int64_t)D + kE * lane;
+#pragma unroll
+    for (int e = 0; e < kE; ++e) store_out(out, obase + e, acc[e] * (1.0f / den), out_dtype);
 }
 
 hipError_t launch_attn_window_mfma(const WindowArgs &a, const WindowDims &w)
@@ -470,7 +482,7 @@ hipError_t launch_attn_window_mfma(const WindowArgs &a, const WindowDims &w)
     else with_dim(BF16{});
     if (p.splits > 1) {
         auto combine = [&](auto dim) {
-            hipLaunchKernelGGL((attn_window_combine_kernel<decltype(dim)::value>), dim3((unsigned)p.units), dim3(256), 0, a.stream, w, ml, o,
+            hipLaunchKernelGGL((attn_window_combine_kernel<decltype(dim)::value>), dim3((unsigned)(p.units * p.rows_per_group / 4)), dim3(256), 0, a.stream, w, ml, o,
                                a.out, p.splits, p.block_pages, d.out_dtype);
         };
         if (d.head_dim == 128) combine(std::integral_constant<int, 128>{});

@@ -30,7 +30,7 @@ SHARED = [(dict(old_batch=-1), -2), (dict(max_pages_per_req=0), -2), (dict(num_p
 
 
 @pytest.mark.parametrize("kw,code", SHARED + [(dict(batch=-1), -2), (dict(window=-1), -2), (dict(sinks=-1), -2),
-                                              (dict(batch=65000, old_batch=600), -6)])
+                                              (dict(batch=65000, old_batch=600), -6), (dict(batch=60000, max_pages_per_req=1 << 15), -6)])
 def test_remap_rejects_bad_dims(kw, code):
     d = _pages(**kw)
     assert _remap(d) == code and pkg.lib().adaspec_kv_remap_workspace_bytes(C.byref(d)) == 0
