@@ -54,6 +54,7 @@ __device__ __forceinline__ bool window_sees(const WindowUnit &u, int pos, int t)
     return t <= pos && (pos - t < u.window || t < u.sinks);
 }
 
-hipError_t launch_attn_window_mfma(const WindowArgs &a, const WindowDims &w);
+hipError_t launch_attn_window_mfma(const WindowArgs &a, const WindowDims &w);      // 16 bits
+hipError_t launch_attn_window_f32(const WindowArgs &a, const WindowDims &w);
 
 }  // namespace adaspec

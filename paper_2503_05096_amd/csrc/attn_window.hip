@@ -1,9 +1,11 @@
-// Windowed verification attention, portable form: any of the three storage types, any head_dim that is a multiple of 8 up
+// Windowed verification attention: the plan of a call, the merge of a unit's parts, and the portable form: any of the three storage types, any head_dim that is a multiple of 8 up
 // to 256.  One wavefront per (request, kv head, chunk of 8 query rows).
 //
 // Per 64 tokens: lane <-> token for the scores (each lane walks its key row, the query rows are broadcast from LDS),
 // wavefront reductions for the online softmax, then lane <-> channel for P.V.  A token that a row does not see has a weight
 // below zero in LDS and is left out of that row's sum, not multiplied by zero: whatever it holds cannot reach the row.
+#include <type_traits>
+
 #include "attn_window.h"
 
 namespace adaspec {
@@ -112,9 +114,54 @@ __global__ __launch_bounds__(64) void attn_window_vector_kernel(WindowDims dims,
     }
 }
 
+// Rows of a unit whose pages were cut: out = sum_s 2^(m_s - m*) O_s / sum_s 2^(m_s - m*) l_s.  One wavefront per row, four
+// rows of a unit per workgroup; lane s looks at (m_s, l_s), the O_s are requested four at a time.
+template <int D>
+__global__ __launch_bounds__(256) void attn_window_combine_kernel(WindowDims dims, const float *__restrict__ part_ml,
+                                                                  const float *__restrict__ part_o, void *__restrict__ out, int splits,
+                                                                  int block_pages, int out_dtype)
+{
+    constexpr int kE = D / 64;
+    const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int quads = dims.rows_per_group / 4, unit = blockIdx.x / quads, rl = 4 * (blockIdx.x % quads) + wv;
+    WindowUnit u;
+    if (!window_unit(u, dims, unit / (dims.Hkv * dims.groups), unit / dims.Hkv % dims.groups, unit % dims.Hkv, lane)) return;
+    const int row = u.r0 + rl;
+    const int all_blocks = (u.pages + block_pages - 1) / block_pages, per = (all_blocks + splits - 1) / splits;
+    const int ns = per > 0 ? (all_blocks + per - 1) / per : 1;      // (at most 64)
+    if (ns == 1 || row >= u.rows) return;
+    const int64_t first = (int64_t)unit * splits * dims.rows_per_group + rl;
+    float2 ml = make_float2(-INFINITY, 0.f);
+    if (lane < ns) ml = *reinterpret_cast<const float2 *>(part_ml + (first + (int64_t)lane * dims.rows_per_group) * 2);
+    const float m = wave_max(ml.x);
+    const float w = lane < ns ? (m > -INFINITY ? __builtin_amdgcn_exp2f(ml.x - m) : 1.f) : 0.f;
+    const float den = wave_sum(w * ml.y);
+    float acc[kE] = {};
+    const float *o = part_o + first * D + kE * lane;
+    for (int s0 = 0; s0 < ns; s0 += 4) {
+        float x[4][kE];
+#pragma unroll
+        for (int s = 0; s < 4; ++s)
+#pragma unroll
+            for (int e = 0; e < kE; ++e) x[s][e] = o[(int64_t)min(s0 + s, ns - 1) * dims.rows_per_group * D + e];
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            const float ws = __shfl(w, s0 + s, kWave);              // (0 behind the last)
+            if (s0 + s < ns) {
+#pragma unroll
+                for (int e = 0; e < kE; ++e) acc[e] += ws * x[s][e];
+            }
+        }
+    }
+    const int G = dims.Hq / dims.Hkv;
+    const int64_t obase = ((u.qrow0 + row / G) * dims.Hq + u.gkv * G + row % G) * (int64_t)D + kE * lane;
+#pragma unroll
+    for (int e = 0; e < kE; ++e) store_out(out, obase + e, acc[e] * (1.0f / den), out_dtype);
+}
+
 bool window_fast_supported(const adaspec_attn_dims &d)
 {
-    return d.dtype != ADASPEC_F32 && (d.head_dim == 64 || d.head_dim == 128);
+    return d.head_dim == 64 || d.head_dim == 128;
 }
 
 WindowPlan make_window_plan(const adaspec_attn_dims &d, int window, int sinks)
@@ -127,7 +174,7 @@ WindowPlan make_window_plan(const adaspec_attn_dims &d, int window, int sinks)
     p.groups = (int)((rows + p.rows_per_group - 1) / p.rows_per_group);
     p.units = (int64_t)d.batch * d.n_kv_heads * p.groups;
     p.splits = 1;
-    p.block_pages = d.head_dim == 64 ? 4 : 2;
+    p.block_pages = d.dtype == ADASPEC_F32 ? 1 : d.head_dim == 64 ? 4 : 2;
     if (p.kind == WindowKind::kMfma) {
         // entries of a unit's list of pages at most: a row group spans this many positions
         const int64_t span = (p.rows_per_group - 1) / G + 2 < d.max_spec_len + 1 ? (p.rows_per_group - 1) / G + 2 : d.max_spec_len + 1;
@@ -152,7 +199,19 @@ hipError_t launch_attn_window(const WindowArgs &a)
     const adaspec_attn_dims &d = a.dims;
     const WindowDims w{a.block_table, a.ctx_lens, a.spec_lens, d.total_q, d.max_spec_len, d.max_pages_per_req, d.n_q_heads,
                        d.n_kv_heads, a.window, a.sinks, a.plan.groups, a.plan.rows_per_group};
-    if (a.plan.kind == WindowKind::kMfma) return launch_attn_window_mfma(a, w);
+    const WindowPlan &p = a.plan;
+    if (p.kind == WindowKind::kMfma) {
+        const hipError_t e = d.dtype == ADASPEC_F32 ? launch_attn_window_f32(a, w) : launch_attn_window_mfma(a, w);
+        if (e != hipSuccess || p.splits == 1) return e;
+        auto combine = [&](auto dim) {
+            hipLaunchKernelGGL((attn_window_combine_kernel<decltype(dim)::value>), dim3((unsigned)(p.units * p.rows_per_group / 4)), dim3(256), 0,
+                               a.stream, w, (const float *)(a.ws + p.off_part_ml), (const float *)(a.ws + p.off_part_o), a.out, p.splits,
+                               p.block_pages, d.out_dtype);
+        };
+        if (d.head_dim == 128) combine(std::integral_constant<int, 128>{});
+        else combine(std::integral_constant<int, 64>{});
+        return hipGetLastError();
+    }
     auto launch = [&](auto tag) {
         hipLaunchKernelGGL(attn_window_vector_kernel<decltype(tag)>, dim3((unsigned)a.plan.units), dim3(64), 0, a.stream, w, a.q,
                            a.k_pages, a.v_pages, a.out, d.head_dim, a.scale_log2, d.out_dtype);

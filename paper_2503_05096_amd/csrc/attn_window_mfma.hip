@@ -15,8 +15,7 @@
 // Softmax weights reach the matrix core as two 16-bit pieces, which hold 16 (bf16) or 22 (f16) bits of the fp32 weight; the
 // sum of weights is taken before that.  One bf16 piece would be off by 2^-9 of the weight, the size of the output's own
 // rounding; the second product costs nothing that the memory does not hide.
-#include "attn_mfma_common.h"
-#include "attn_window.h"
+#include "attn_window_merge.h"
 
 namespace adaspec {
 
@@ -53,49 +52,6 @@ __device__ __forceinline__ void load_lds_2(const v4i32 &rsrc, uint32_t off0, uin
                  :: "s"(lds), "v"(off0), "v"(off1), "s"(rsrc) : "memory", "m0");
 }
 
-// State of one row over the entries [v0, v1) of its unit's list, by one wavefront: lane <-> token for the scores, lane <-> two
-// channels side by side for the values.  A token that the row does not see is left out, whatever it holds.
-template <class T, int D>
-__device__ __forceinline__ void row_by_selection(const WindowUnit &u, const WindowDims &dims, const int32_t *block_table, const char *q, const char *k_pages, const char *v_pages,
-                                                 int row, int v0, int v1, float scale_log2, float &m, float &l, float2 &acc)
-{
-    const int lane = threadIdx.x & 63, G = dims.Hq / dims.Hkv, pos = u.first_pos + row / G;
-    const int64_t qbase = ((u.qrow0 + row / G) * dims.Hq + u.gkv * G + row % G) * (int64_t)D;
-    m = -INFINITY; l = 0.f;
-    acc = make_float2(0.f, 0.f);
-    for (int vb = v0; vb < v1; vb += 4) {
-        const int v = vb + (lane >> 4), pg = u.page_of(min(v, v1 - 1)), t = pg * 16 + (lane & 15);
-        const bool vis = v < v1 && window_sees(u, pos, t);
-        float s = -INFINITY;
-        if (vis) {
-            const int64_t at = (((int64_t)block_table[u.bt_off + pg] * dims.Hkv + u.gkv) * 16 + (lane & 15)) * D;
-            s = 0.f;
-            for (int c = 0; c < D; ++c) s = fmaf(load_as_float<T>(q, qbase + c), load_as_float<T>(k_pages, at + c), s);
-            s *= scale_log2;
-        }
-        const float mn = fmaxf(m, wave_max(s));
-        float p = 0.f, alpha = 1.f;
-        if (mn > -INFINITY) {
-            alpha = __builtin_amdgcn_exp2f(m - mn);
-            p = vis ? __builtin_amdgcn_exp2f(s - mn) : 0.f;
-        } else if (vis) {
-            p = s == s ? 0.f : s;
-        }
-        l = l * alpha + wave_sum(p);
-        m = mn;
-        acc.x *= alpha; acc.y *= alpha;
-        const unsigned long long seen = __ballot(vis);
-        for (int tt = 0; tt < 64; ++tt) {
-            if (!((seen >> tt) & 1)) continue;
-            const float w = __shfl(p, tt, kWave);
-            const int64_t at = (((int64_t)block_table[u.bt_off + u.page_of(vb + (tt >> 4))] * dims.Hkv + u.gkv) * 16 + (tt & 15)) * D;
-            const int c = 2 * (lane & (D / 2 - 1));
-            acc.x = fmaf(w, load_as_float<T>(v_pages, at + c), acc.x);
-            acc.y = fmaf(w, load_as_float<T>(v_pages, at + c + 1), acc.y);
-        }
-    }
-}
-
 template <class T, int D, int RT>
 __global__ __launch_bounds__(256, 2) void attn_window_kernel(WindowDims dims, const int32_t *__restrict__ block_table,
                                                              const char *__restrict__ q, const char *__restrict__ k_pages, const char *__restrict__ v_pages,
@@ -105,7 +61,6 @@ __global__ __launch_bounds__(256, 2) void attn_window_kernel(WindowDims dims, co
     using Lds = WindowLds<D, RT>;
     using Weights = WindowWeights<T>;
     constexpr int kRows = 16 * RT, kS = D / 32, kDt = D / 16, kPages = 256 / D, kPageBytes = 32 * D, kRowBytes = 2 * D;
-    constexpr int kPieces = D / 64;                                 // of four channels, per thread and row tile of the merge
     __shared__ __attribute__((aligned(1024))) char smem[Lds::kBytes];
     const uint32_t lds_base = lds_address(smem);
     float *s_m = reinterpret_cast<float *>(smem + Lds::kMl), *s_l = s_m + kWaves * kRows;    // [wavefront][row]
@@ -330,9 +285,7 @@ __global__ __launch_bounds__(256, 2) void attn_window_kernel(WindowDims dims, co
         }
     }
 
-    // ---- merge the four wavefronts' states through LDS, one row tile at a time, each wavefront's in its V slot:
-    //   O = sum_w 2^(m_w - m*) O_w, m* = max over wavefronts.
-    // The 16-byte pieces of a row are exchanged by the row's number so that neither side meets bank conflicts.
+    // ---- merge the four wavefronts' states through LDS, one row tile at a time, each wavefront's in its V slot
     if constexpr (Lds::kFull) lds_barrier();                        // (m, l) go where Q stands: all are done with it
 #pragma unroll
     for (int nt = 0; nt < RT; ++nt) {
@@ -340,120 +293,17 @@ __global__ __launch_bounds__(256, 2) void attn_window_kernel(WindowDims dims, co
         lsum[nt] += __shfl_xor(lsum[nt], 32, kWave);
         if (g == 0) { s_m[wv * kRows + 16 * nt + n16] = m[nt]; s_l[wv * kRows + 16 * nt + n16] = lsum[nt]; }
     }
-    constexpr int kSwap = kDt * 4 - 1;                              // 16-byte pieces of a row: 32 or 16
 #pragma unroll
     for (int nt = 0; nt < RT; ++nt) {
         if (u.r0 + 16 * nt >= u.rows) break;
 #pragma unroll
         for (int dt = 0; dt < kDt; ++dt)
-            *reinterpret_cast<f32x4 *>(v_slot + n16 * (4 * D) + 16 * ((4 * dt + g) ^ (n16 & kSwap))) = o[nt][dt];
+            *reinterpret_cast<f32x4 *>(v_slot + window_piece<D>(n16, 4 * dt + g)) = o[nt][dt];
         lds_barrier();
-        const int rt = tid >> 4, rl = 16 * nt + rt, row = u.r0 + rl;
-        float ms = s_m[rl], ltot = 0.f;
-#pragma unroll
-        for (int w = 1; w < kWaves; ++w) ms = fmaxf(ms, s_m[w * kRows + rl]);
-        f32x4 acc[kPieces];
-#pragma unroll
-        for (int p = 0; p < kPieces; ++p) acc[p] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
-            const float sc = __builtin_amdgcn_exp2f(s_m[w * kRows + rl] - ms);
-            ltot += sc * s_l[w * kRows + rl];
-#pragma unroll
-            for (int p = 0; p < kPieces; ++p)
-                acc[p] += sc * *reinterpret_cast<const f32x4 *>(smem + (2 * w + 1) * kSlotBytes + rt * (4 * D) + 16 * ((kPieces * (tid & 15) + p) ^ (rt & kSwap)));
-        }
-        // a NaN or an infinity: the row's own, or one that it does not see (see above)
-        float total = ltot;
-#pragma unroll
-        for (int p = 0; p < kPieces; ++p) total += (acc[p][0] + acc[p][1]) + (acc[p][2] + acc[p][3]);
-        unsigned long long odd = __ballot(row < u.rows && !(fabsf(total) < INFINITY));
-        while (__builtin_expect(odd != 0, 0)) {
-            const int of = (int)__builtin_ctzll(odd) >> 4;          // row of this wavefront, 0 .. 3
-            float rm, rl_;
-            float2 ra;
-            row_by_selection<T, D>(u, dims, block_table, q, k_pages, v_pages, u.r0 + 16 * nt + 4 * wv + of, b0 * kPages, min(b1 * kPages, u.pages), scale_log2, rm, rl_, ra);
-#pragma unroll
-            for (int p = 0; p < kPieces; ++p) {
-                const int from = 2 * (kPieces * (lane & 15) + p);
-                const f32x4 val = {__shfl(ra.x, from, kWave), __shfl(ra.y, from, kWave), __shfl(ra.x, from + 1, kWave), __shfl(ra.y, from + 1, kWave)};
-                if (lane >> 4 == of) acc[p] = val;
-            }
-            if (lane >> 4 == of) { ms = rm + Weights::kShiftLog2; ltot = rl_; }    // (the stream's weights are that much larger)
-            odd &= ~(0xffffull << (16 * of));
-        }
-        if (row < u.rows) {
-            if (ns == 1) {
-                const float inv = 1.0f / ltot;
-                const int64_t obase = ((u.qrow0 + row / G) * dims.Hq + u.gkv * G + row % G) * (int64_t)D + 4 * kPieces * (tid & 15);
-                if (out_dtype == ADASPEC_F32) {
-#pragma unroll
-                    for (int p = 0; p < kPieces; ++p) *reinterpret_cast<f32x4 *>(reinterpret_cast<float *>(out) + obase + 4 * p) = acc[p] * inv;
-                } else {
-                    uint32_t w[2 * kPieces];
-#pragma unroll
-                    for (int p = 0; p < kPieces; ++p) {
-                        w[2 * p] = Mma<T>::pack2(acc[p][0] * inv, acc[p][1] * inv);
-                        w[2 * p + 1] = Mma<T>::pack2(acc[p][2] * inv, acc[p][3] * inv);
-                    }
-                    uint16_t *to = reinterpret_cast<uint16_t *>(out) + obase;
-                    if constexpr (kPieces == 2) *reinterpret_cast<uint4 *>(to) = make_uint4(w[0], w[1], w[2], w[3]);
-                    else *reinterpret_cast<uint2 *>(to) = make_uint2(w[0], w[1]);
-                }
-            } else {
-                const int64_t at = ((int64_t)unit * splits + sp) * kRows + rl;
-#pragma unroll
-                for (int p = 0; p < kPieces; ++p) *reinterpret_cast<f32x4 *>(part_o + at * D + 4 * (kPieces * (tid & 15) + p)) = acc[p];
-                if ((tid & 15) == 0) *reinterpret_cast<float2 *>(part_ml + at * 2) = make_float2(ms, ltot);
-            }
-        }
+        finish_window_tile<T, D>(u, dims, block_table, q, k_pages, v_pages, out, part_ml, part_o, smem + kSlotBytes, 2 * kSlotBytes, s_m, s_l, kRows, nt, ns, b0 * kPages,
+                                 min(b1 * kPages, u.pages), scale_log2, Weights::kShiftLog2, out_dtype, ((int64_t)unit * splits + sp) * kRows);
         if (nt + 1 < RT) lds_barrier();                             // the next tile overwrites the slots
     }
-}
-
-// Rows of a unit whose pages were cut: out = sum_s 2^(m_s - m*) O_s / sum_s 2^(m_s - m*) l_s.  One wavefront per row, four
-// rows of a unit per workgroup; lane s looks at (m_s, l_s), the O_s are requested four at a time.
-template <int D>
-__global__ __launch_bounds__(256) void attn_window_combine_kernel(WindowDims dims, const float *__restrict__ part_ml,
-                                                                  const float *__restrict__ part_o, void *__restrict__ out, int splits,
-                                                                  int block_pages, int out_dtype)
-{
-    constexpr int kE = D / 64;
-    const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int quads = dims.rows_per_group / 4, unit = blockIdx.x / quads, rl = 4 * (blockIdx.x % quads) + wv;
-    WindowUnit u;
-    if (!window_unit(u, dims, unit / (dims.Hkv * dims.groups), unit / dims.Hkv % dims.groups, unit % dims.Hkv, lane)) return;
-    const int row = u.r0 + rl;
-    const int all_blocks = (u.pages + block_pages - 1) / block_pages, per = (all_blocks + splits - 1) / splits;
-    const int ns = per > 0 ? (all_blocks + per - 1) / per : 1;      // (at most 64)
-    if (ns == 1 || row >= u.rows) return;
-    const int64_t first = (int64_t)unit * splits * dims.rows_per_group + rl;
-    float2 ml = make_float2(-INFINITY, 0.f);
-    if (lane < ns) ml = *reinterpret_cast<const float2 *>(part_ml + (first + (int64_t)lane * dims.rows_per_group) * 2);
-    const float m = wave_max(ml.x);
-    const float w = lane < ns ? (m > -INFINITY ? __builtin_amdgcn_exp2f(ml.x - m) : 1.f) : 0.f;
-    const float den = wave_sum(w * ml.y);
-    float acc[kE] = {};
-    const float *o = part_o + first * D + kE * lane;
-    for (int s0 = 0; s0 < ns; s0 += 4) {
-        float x[4][kE];
-#pragma unroll
-        for (int s = 0; s < 4; ++s)
-#pragma unroll
-            for (int e = 0; e < kE; ++e) x[s][e] = o[(int64_t)min(s0 + s, ns - 1) * dims.rows_per_group * D + e];
-#pragma unroll
-        for (int s = 0; s < 4; ++s) {
-            const float ws = __shfl(w, s0 + s, kWave);              // (0 behind the last)
-            if (s0 + s < ns) {
-#pragma unroll
-                for (int e = 0; e < kE; ++e) acc[e] += ws * x[s][e];
-            }
-        }
-    }
-    const int G = dims.Hq / dims.Hkv;
-    const int64_t obase = ((u.qrow0 + row / G) * dims.Hq + u.gkv * G + row % G) * (int64_t)D + kE * lane;
-#pragma unroll
-    for (int e = 0; e < kE; ++e) store_out(out, obase + e, acc[e] * (1.0f / den), out_dtype);
 }
 
 hipError_t launch_attn_window_mfma(const WindowArgs &a, const WindowDims &w)
@@ -480,14 +330,6 @@ hipError_t launch_attn_window_mfma(const WindowArgs &a, const WindowDims &w)
     };
     if (d.dtype == ADASPEC_F16) with_dim(F16{});
     else with_dim(BF16{});
-    if (p.splits > 1) {
-        auto combine = [&](auto dim) {
-            hipLaunchKernelGGL((attn_window_combine_kernel<decltype(dim)::value>), dim3((unsigned)(p.units * p.rows_per_group / 4)), dim3(256), 0, a.stream, w, ml, o,
-                               a.out, p.splits, p.block_pages, d.out_dtype);
-        };
-        if (d.head_dim == 128) combine(std::integral_constant<int, 128>{});
-        else combine(std::integral_constant<int, 64>{});
-    }
     return hipGetLastError();
 }
 
