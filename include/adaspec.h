@@ -441,6 +441,7 @@ int adaspec_kv_remap(const int32_t *block_table, const int32_t *page_refs, const
  *                                             for holders outside the table
  *   copy_src, copy_dst [max_moves]            the moves, then -1: for adaspec_kv_copy_pages
  *   status [2]                                N; moves that the pool takes altogether
+ * At most 2^21 pages.
  */
 size_t adaspec_kv_compact_pages_workspace_bytes(const adaspec_pages_dims *dims);
 

@@ -316,7 +316,8 @@ struct CompactArgs {
     int32_t *out_table, *out_refs, *page_map, *copy_src, *copy_dst, *status;
     adaspec_pages_dims dims;
     int chunks, table_groups;                                       // workgroups for the pages, for the table
-    int32_t *chunk_used, *rank;                                     // workspace: [chunks], [num_pages]
+    int32_t *grain_used;                                            // workspace: [4 chunks]
+    int2 *words;                                                    // workspace: [chunks][32]
 };
 // bytes of workspace; fills in its pointers where `a` is given
 size_t remap_workspace(const adaspec_pages_dims &d, RemapArgs *a, char *ws);

@@ -139,7 +139,7 @@ __global__ __launch_bounds__(kPagesThreads) void remap_rows_kernel(RemapArgs a)
 }
 
 // Workgroups 0 .. chunks - 1: free pages of a chunk.  Those behind, for 256 rows each: what a row wants, as a record of
-// (its first want's number among these rows', the entry that it is for, the page to copy into it or -1).
+// (its first want's number among these rows', the entry that it is for, the page to copy into it or -1, how many).
 __global__ __launch_bounds__(kPagesThreads) void remap_count_kernel(RemapArgs a)
 {
     __shared__ int s_sum[kPagesThreads / kWave];
@@ -168,32 +168,152 @@ __global__ __launch_bounds__(kPagesThreads) void remap_count_kernel(RemapArgs a)
     }
     int total;
     const int first = block_scan(want, s_sum, &total);
-    if (i < d.batch) a.want[i] = make_int4(first, start, from, 0);
+    if (i < d.batch) a.want[i] = make_int4(first, start, from, want);
     if (tid == 0) a.tile_wants[tile] = total;
 }
 
-// Free page number f of the pool goes to want number f.
-constexpr int kFirstRows = 2048;            // rows whose first wants are looked up in LDS
+// Everything up to here in one launch, where the old table and both batches are small: a workgroup per 1024 pages goes through
+// the whole old table and keeps the counts of its own pages in LDS, so that nobody has to wait for anybody.  It also decides
+// what those rows want that are about to write into one of its pages (the first workgroup: into none that holds tokens).  The
+// workgroups behind write a new row each.
+constexpr int kSmallRows = 1024;
+constexpr int64_t kSmallEntries = 32768;
+constexpr int kScan = 2;                    // loads of four entries that a thread has under way
+static_assert(kSmallRows == kChunk, "a thread per row");
+__global__ __launch_bounds__(kChunk) void remap_small_kernel(RemapArgs a)
+{
+    __shared__ int s_refs[kChunk], s_writers[kChunk], s_last[kChunk], s_sum[kChunk / kWave];
+    __shared__ int s_children[kSmallRows], s_pages[kSmallRows], s_low[kSmallRows];
+    const adaspec_pages_dims &d = a.dims;
+    const int tid = threadIdx.x, width = d.max_pages_per_req, P = d.page_size;
+    if ((int)blockIdx.x >= a.chunks) {
+        const int i = blockIdx.x - a.chunks, s = source_of(a, i);
+        const Kept kept(len_of(a, s), d);
+        const int32_t *t = a.block_table + (int64_t)max(s, 0) * width;
+        int32_t *o = a.out_table + (int64_t)i * width;
+        for (int j = tid; j < width; j += kChunk) {
+            const int p = s >= 0 && kept.keeps(j) ? t[j] : -1;
+            o[j] = p < d.num_pages ? max(p, -1) : -1;
+        }
+        if (tid == 0) {
+            a.copy_src[i] = -1;
+            a.copy_dst[i] = -1;
+        }
+        return;
+    }
+    const int p0 = blockIdx.x * kChunk, p = p0 + tid;
+    const int old = p < d.num_pages ? a.page_refs[p] : 1;
+    // new row tid: the page that it is about to write into
+    int len = 0, grown = 0, part = -1;
+    const int src = tid < d.batch ? source_of(a, tid) : -1;
+    if (tid < d.batch) grown = a.new_lens[tid];
+    s_refs[tid] = 0; s_writers[tid] = 0; s_last[tid] = -1; s_children[tid] = 0;
+    __syncthreads();
+    if (src >= 0) atomicAdd(&s_children[src], 1);
+    if (tid < d.old_batch) {
+        const Kept kept(len_of(a, tid), d);
+        s_pages[tid] = kept.pages;
+        s_low[tid] = kept.low;
+    }
+    if (src >= 0) {
+        len = len_of(a, src);
+        if (len % P != 0 && grown > len) part = a.block_table[(int64_t)src * width + len / P];
+        if (part >= d.num_pages) part = -1;
+    }
+    __syncthreads();
+    const int first = d.window > 0 ? ceil_div(d.sinks, P) : 0;      // (entries of the sinks; without a window s_low is 0)
+    const int entries = d.old_batch * width;
+    auto count = [&](int e, int q) {                                // entry e of the table, which holds page q of this chunk
+        const int row = e / width, j = e - row * width;
+        const bool keeps = j < s_pages[row] && (j < first || j >= s_low[row]);
+        const int delta = (keeps ? s_children[row] : 0) - 1;
+        if (delta != 0) atomicAdd(&s_refs[q - p0], delta);
+    };
+    // About one entry per thread holds one of the chunk's pages: they are put aside, and looked at by all threads together.
+    const unsigned mine = min(kChunk, d.num_pages - p0);
+    int aside[4] = {-1, -1, -1, -1}, held[4] = {0, 0, 0, 0};
+    for (int e0 = 4 * tid; e0 < entries; e0 += kScan * 4 * kChunk) {
+        int4 q[kScan];
+#pragma unroll
+        for (int k = 0; k < kScan; ++k) q[k] = four(a.block_table, e0 + k * 4 * kChunk, entries, -1);
+#pragma unroll
+        for (int k = 0; k < kScan; ++k) {
+            const int v[4] = {q[k].x, q[k].y, q[k].z, q[k].w};
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                if ((unsigned)(v[c] - p0) >= mine) continue;
+                if (aside[3] >= 0) count(aside[3], held[3]);
+#pragma unroll
+                for (int i = 3; i > 0; --i) { aside[i] = aside[i - 1]; held[i] = held[i - 1]; }
+                aside[0] = e0 + k * 4 * kChunk + c;
+                held[0] = v[c];
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (aside[i] >= 0) count(aside[i], held[i]);
+    const bool here = part >= p0 && part < p0 + kChunk;
+    if (here) {
+        atomicAdd(&s_writers[part - p0], 1);
+        atomicMax(&s_last[part - p0], tid);
+    }
+    __syncthreads();
+    const int now = old + s_refs[tid];
+    if (p < d.num_pages) a.out_refs[p] = now;
+    const unsigned long long free = __ballot(p < d.num_pages && now == 0);
+    if ((tid & 63) == 0) s_sum[tid >> 6] = __popcll(free);
+    s_refs[tid] = now;                                              // (every thread reads its own before)
+    __syncthreads();
+    if (tid == 0) {
+        int n = 0;
+#pragma unroll
+        for (int w = 0; w < kChunk / kWave; ++w) n += s_sum[w];
+        a.chunk_free[blockIdx.x] = n;
+    }
+    if (tid < d.batch && (here || (part < 0 && blockIdx.x == 0))) {
+        int from = -1;
+        if (here) {             // shared, unless this row is the last of those who hold it, all of which are about to write
+            const int q = part - p0, refs = s_refs[q];
+            if (refs > 1 && !(s_writers[q] == refs && s_last[q] == tid)) from = part;
+        }
+        const int start = from >= 0 ? len / P : ceil_div(len, P);
+        a.want[tid] = make_int4(0, start, from, max(ceil_div(min(max(grown, 0), width * P), P) - start, 0));
+    }
+}
+
+// Free page number f of the pool goes to want number f.  kFew: at most kFewRows rows, whose wants every workgroup adds up itself.
+constexpr int kFewRows = 2048;
+template <bool kFew>
 __global__ __launch_bounds__(kPagesThreads) void remap_assign_kernel(RemapArgs a)
 {
+    constexpr int kRows = kFew ? kFewRows / kPagesThreads : 1;
     __shared__ int s_sum[kPagesThreads / kWave];
-    __shared__ int s_tile[kPagesThreads];                   // where the wants of every 256 rows begin
-    __shared__ int s_first[kFirstRows];
+    __shared__ int s_first[kFew ? kFewRows : kPagesThreads];        // where the wants of every row, or of every 256 rows, begin
     const adaspec_pages_dims &d = a.dims;
     const int tid = threadIdx.x, p0 = blockIdx.x * kChunk + kPerThread * tid;
     const int4 r = four(a.out_refs, p0, d.num_pages, 1);
     const bool free[kPerThread] = {r.x == 0, r.y == 0, r.z == 0, r.w == 0};
-    const bool in_lds = d.batch <= kFirstRows;
-    if (in_lds)
-        for (int i = tid; i < d.batch; i += kPagesThreads) s_first[i] = a.want[i].x;
+    int n[kRows], mine = 0;
+#pragma unroll
+    for (int k = 0; k < kRows; ++k) {
+        if constexpr (kFew) n[k] = tid * kRows + k < d.batch ? a.want[tid * kRows + k].w : 0;
+        else n[k] = tid < a.tiles ? a.tile_wants[tid] : 0;          // (at most 256 tiles: 65535 rows)
+        mine += n[k];
+    }
     int before = 0, all = 0;
     for (int c = tid; c < a.chunks; c += kPagesThreads) {
-        const int n = a.chunk_free[c];
-        before += c < (int)blockIdx.x ? n : 0;
-        all += n;
+        const int m = a.chunk_free[c];
+        before += c < (int)blockIdx.x ? m : 0;
+        all += m;
     }
     int wants, here;
-    s_tile[tid] = block_scan(tid < a.tiles ? a.tile_wants[tid] : 0, s_sum, &wants);         // (at most 256 tiles: 65535 rows)
+    int at = block_scan(mine, s_sum, &wants);
+#pragma unroll
+    for (int k = 0; k < kRows; ++k) {
+        s_first[tid * kRows + k] = at;
+        at += n[k];
+    }
     before = block_sum(before, s_sum);
     if (blockIdx.x == 0) {
         all = block_sum(all, s_sum);
@@ -209,23 +329,28 @@ __global__ __launch_bounds__(kPagesThreads) void remap_assign_kernel(RemapArgs a
     for (int e = 0; e < kPerThread; ++e) {
         if (!free[e] || f >= wants) continue;
         const int p = p0 + e;
-        int lo = 0, hi = a.tiles;                           // the rows, then the row, whose wants f is among
+        int lo = 0, hi = kFew ? d.batch : a.tiles;                  // the row, or the rows and then the row, whose wants f is among
         while (hi - lo > 1) {
             const int mid = (lo + hi) >> 1;
-            if (s_tile[mid] <= f) lo = mid;
+            if (s_first[mid] <= f) lo = mid;
             else hi = mid;
         }
-        const int in_tile = f - s_tile[lo];
+        int nth = f - s_first[lo];
         ++f;
-        hi = min((lo + 1) * kPagesThreads, d.batch);
-        lo *= kPagesThreads;
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
-            if ((in_lds ? s_first[mid] : a.want[mid].x) <= in_tile) lo = mid;
-            else hi = mid;
+        int4 w;
+        if constexpr (kFew) {
+            w = a.want[lo];
+        } else {
+            hi = min((lo + 1) * kPagesThreads, d.batch);
+            lo *= kPagesThreads;
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) >> 1;
+                if (a.want[mid].x <= nth) lo = mid;
+                else hi = mid;
+            }
+            w = a.want[lo];
+            nth -= w.x;
         }
-        const int4 w = a.want[lo];
-        const int nth = in_tile - w.x;
         a.out_refs[p] = 1;
         a.out_table[(int64_t)lo * d.max_pages_per_req + w.y + nth] = p;
         if (w.z >= 0 && nth == 0) {
@@ -258,12 +383,17 @@ size_t remap_workspace(const adaspec_pages_dims &d, RemapArgs *a, char *ws)
 hipError_t launch_kv_remap(const RemapArgs &a, hipStream_t stream)
 {
     const adaspec_pages_dims &d = a.dims;
-    hipLaunchKernelGGL(remap_start_kernel, dim3(a.chunks), dim3(kPagesThreads), 0, stream, a);
-    if (d.old_batch + d.batch > 0)
-        hipLaunchKernelGGL(remap_rows_kernel, dim3(ceil_div(d.max_pages_per_req, kRowPart), d.old_batch + d.batch), dim3(kPagesThreads), 0,
-                           stream, a);
-    hipLaunchKernelGGL(remap_count_kernel, dim3(a.chunks + a.tiles), dim3(kPagesThreads), 0, stream, a);
-    hipLaunchKernelGGL(remap_assign_kernel, dim3(a.chunks), dim3(kPagesThreads), 0, stream, a);
+    if (d.old_batch <= kSmallRows && d.batch <= kSmallRows && (int64_t)d.old_batch * d.max_pages_per_req <= kSmallEntries) {
+        hipLaunchKernelGGL(remap_small_kernel, dim3(a.chunks + d.batch), dim3(kChunk), 0, stream, a);
+    } else {
+        hipLaunchKernelGGL(remap_start_kernel, dim3(a.chunks), dim3(kPagesThreads), 0, stream, a);
+        if (d.old_batch + d.batch > 0)
+            hipLaunchKernelGGL(remap_rows_kernel, dim3(ceil_div(d.max_pages_per_req, kRowPart), d.old_batch + d.batch), dim3(kPagesThreads), 0,
+                               stream, a);
+        hipLaunchKernelGGL(remap_count_kernel, dim3(a.chunks + a.tiles), dim3(kPagesThreads), 0, stream, a);
+    }
+    if (d.batch <= kFewRows) hipLaunchKernelGGL(remap_assign_kernel<true>, dim3(a.chunks), dim3(kPagesThreads), 0, stream, a);
+    else hipLaunchKernelGGL(remap_assign_kernel<false>, dim3(a.chunks), dim3(kPagesThreads), 0, stream, a);
     return hipGetLastError();
 }
 
@@ -271,105 +401,213 @@ hipError_t launch_kv_remap(const RemapArgs &a, hipStream_t stream)
 // N pages are used (counts above 0).  The m-th used page at or behind N moves to the m-th free page below N, for the first
 // `max_moves` of them.
 
-__global__ __launch_bounds__(kPagesThreads) void compact_count_kernel(CompactArgs a)
+//
+// Which pages are used is one bit per page, in words of 32 with the number of used pages before them; everything else follows
+// from the number of used pages below a page and from where the m-th free page is, which are two or three look-ups each.
+
+// A thread's four bits and those of its seven neighbours: within four lanes, then the other four by mirroring the eight
+__device__ __forceinline__ uint32_t word_of(const int4 &r)
 {
-    __shared__ int s_sum[kPagesThreads / kWave];
-    const int4 r = four(a.page_refs, blockIdx.x * kChunk + kPerThread * threadIdx.x, a.dims.num_pages, 0);
-    const int n = block_sum((r.x > 0) + (r.y > 0) + (r.z > 0) + (r.w > 0), s_sum);
-    if (threadIdx.x == 0) a.chunk_used[blockIdx.x] = n;
+    uint32_t w = ((r.x > 0) | (r.y > 0) << 1 | (r.z > 0) << 2 | (r.w > 0) << 3) << (4 * (threadIdx.x & 7));
+    w |= dpp_move<0xb1, 0xf>(0, w);
+    w |= dpp_move<0x4e, 0xf>(0, w);
+    w |= dpp_move<0x141, 0xf>(0, w);
+    return w;
 }
 
-// rank[p]: of a page that moves or is moved to, the number of its move; -1 otherwise.  Both lists of moves.
-__global__ __launch_bounds__(kPagesThreads) void compact_rank_kernel(CompactArgs a)
+// Words of a wavefront's 256 pages, counted from their beginning, and how many of these are used.
+constexpr int kGrain = kWave * kPerThread;
+__global__ __launch_bounds__(kPagesThreads) void compact_words_kernel(CompactArgs a)
 {
+    const int tid = threadIdx.x, lane = tid & 63, grain = blockIdx.x * (kChunk / kGrain) + (tid >> 6);
+    const uint32_t w = word_of(four(a.page_refs, blockIdx.x * kChunk + kPerThread * tid, a.dims.num_pages, 0));
+    const int n = (lane & 7) == 0 ? __popc(w) : 0, upto = wave_scan_incl_dpp(n);
+    if ((lane & 7) == 0) a.words[grain * (kGrain / 32) + (lane >> 3)] = make_int2((int)w, upto - n);
+    if (lane == 63) a.grain_used[grain] = upto;
+}
+
+// Workgroups 0 .. chunks - 1: counts, map and moves of a chunk of pages; those behind: the table.  Every count is read and
+// written by one thread each, so that the new counts may lie over the old ones (not with kSelf).
+// kSelf: small pools, whose words every workgroup works out itself.
+constexpr int kSelfPages = 16384;
+template <bool kSelf>
+__global__ __launch_bounds__(kPagesThreads) void compact_write_kernel(CompactArgs a)
+{
+    extern __shared__ int s_base[];                                 // used pages before every 256; behind the last: all
+    __shared__ int2 s_words[kSelf ? kSelfPages / 32 : 1];
     __shared__ int s_sum[kPagesThreads / kWave];
     const adaspec_pages_dims &d = a.dims;
-    const int tid = threadIdx.x, p0 = blockIdx.x * kChunk + kPerThread * tid;
-    const int4 r = four(a.page_refs, p0, d.num_pages, 0);
-    const bool used[kPerThread] = {r.x > 0, r.y > 0, r.z > 0, r.w > 0};
-    int N = 0, before = 0;
-    for (int c = tid; c < a.chunks; c += kPagesThreads) {
-        const int n = a.chunk_used[c];
-        N += n;
-        before += c < (int)blockIdx.x ? n : 0;
+    const int tid = threadIdx.x, grains = a.chunks * (kChunk / kGrain);
+    if constexpr (kSelf) {
+        constexpr int kMost = kSelfPages / kChunk;
+        int4 r[kMost];
+#pragma unroll
+        for (int c = 0; c < kMost; ++c) r[c] = c < a.chunks ? four(a.page_refs, c * kChunk + kPerThread * tid, d.num_pages, 0) : make_int4(0, 0, 0, 0);
+#pragma unroll
+        for (int c = 0; c < kMost; ++c) {
+            const uint32_t w = c < a.chunks ? word_of(r[c]) : 0;
+            if ((tid & 7) == 0) s_words[c * (kChunk / 32) + (tid >> 3)].x = (int)w;
+        }
+        __syncthreads();
+        const int w0 = s_words[2 * tid].x, w1 = s_words[2 * tid + 1].x;
+        int total;
+        const int before = block_scan(__popc(w0) + __popc(w1), s_sum, &total);
+        s_words[2 * tid].y = before;                                // (from the pool's beginning: no bases of chunks)
+        s_words[2 * tid + 1].y = before + __popc(w0);
+        if (tid <= grains) s_base[tid] = tid < grains ? 0 : total;
+        __syncthreads();
+    } else {
+        int base = 0;
+        for (int c0 = 0; c0 < grains; c0 += 4 * kPagesThreads) {
+            const int c = c0 + 4 * tid;
+            const int4 n = four(a.grain_used, c, grains, 0);
+            int total;
+            const int at = base + block_scan((n.x + n.y) + (n.z + n.w), s_sum, &total);
+            if (c < grains) {                                       // (a multiple of four)
+                s_base[c] = at;
+                s_base[c + 1] = at + n.x;
+                s_base[c + 2] = at + n.x + n.y;
+                s_base[c + 3] = at + n.x + n.y + n.z;
+            }
+            base += total;
+        }
+        if (tid == 0) s_base[grains] = base;
+        __syncthreads();
     }
-    N = block_sum(N, s_sum);
-    before = block_sum(before, s_sum);
-    // used pages below N: whole chunks, and the part of the one that N lies in
-    int low = 0;
-    const int last = N / kChunk, q0 = last * kChunk + kPerThread * tid;
-    for (int c = tid; c < last; c += kPagesThreads) low += a.chunk_used[c];
-    const int4 q = four(a.page_refs, q0, N, 0);
-    low = block_sum(low + (q.x > 0) + (q.y > 0) + (q.z > 0) + (q.w > 0), s_sum);
+    const int N = s_base[grains];
+    auto word = [&](int w) -> int2 {
+        if constexpr (kSelf) return s_words[w];
+        else return a.words[w];
+    };
+    auto used_before = [&](int p, int2 w) { return s_base[p / kGrain] + w.y + __popc((uint32_t)w.x & ((1u << (p & 31)) - 1u)); };
+    int low = N;                                                    // used pages below N
+    if (N < a.chunks * kChunk) low = used_before(N, word(N / 32));
     const int moves = N - low;
+    // to[k] = the m[k]-th free page, for m[k] < moves (m[k] < 0: as it is); the four look-ups step by step together
+    auto free_pages = [&](const int (&of)[kPerThread], int (&to)[kPerThread]) {
+        bool any = false;
+#pragma unroll
+        for (int k = 0; k < kPerThread; ++k) any |= of[k] >= 0;
+        if (__ballot(any) == 0) return;
+        int m[kPerThread], lo[kPerThread];
+#pragma unroll
+        for (int k = 0; k < kPerThread; ++k) { m[k] = max(of[k], 0); lo[k] = 0; }
+        const int size = kSelf ? a.chunks * (kChunk / 32) : grains;
+        for (int step = 1 << (31 - __builtin_clz(size)); step > 0; step >>= 1) {
+#pragma unroll
+            for (int k = 0; k < kPerThread; ++k) {
+                const int at = min(lo[k] + step, size - 1);
+                int before;                                         // free pages in front of word, or grain, `at`
+                if constexpr (kSelf) before = 32 * at - s_words[at].y;
+                else before = at * kGrain - s_base[at];
+                lo[k] = before <= m[k] ? at : lo[k];
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < kPerThread; ++k) {
+            if constexpr (kSelf) {
+                m[k] -= 32 * lo[k] - s_words[lo[k]].y;
+            } else {
+                m[k] -= lo[k] * kGrain - s_base[lo[k]];
+                lo[k] *= kGrain / 32;
+            }
+        }
+        uint32_t mask[kPerThread];
+        if constexpr (kSelf) {
+#pragma unroll
+            for (int k = 0; k < kPerThread; ++k) mask[k] = (uint32_t)s_words[lo[k]].x;
+        } else {                                                    // which of the grain's eight words
+            int4 w[kPerThread][4];
+#pragma unroll
+            for (int k = 0; k < kPerThread; ++k)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) w[k][i] = reinterpret_cast<const int4 *>(a.words + lo[k])[i];
+#pragma unroll
+            for (int k = 0; k < kPerThread; ++k) {
+                int at = 0, before = 0;
+                mask[k] = (uint32_t)w[k][0].x;
+#pragma unroll
+                for (int i = 1; i < 8; ++i) {
+                    const int b = 32 * i - (i & 1 ? w[k][i / 2].w : w[k][i / 2].y);
+                    if (b <= m[k]) { at = i; before = b; mask[k] = (uint32_t)(i & 1 ? w[k][i / 2].z : w[k][i / 2].x); }
+                }
+                m[k] -= before;
+                lo[k] += at;
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < kPerThread; ++k) {
+            uint32_t rest = ~mask[k];                               // its m-th set bit
+            int bit = 0;
+#pragma unroll
+            for (int half = 16; half > 0; half >>= 1) {
+                const int below = __popc(rest & ((1u << half) - 1u));
+                const bool up = m[k] >= below;
+                m[k] -= up ? below : 0;
+                bit += up ? half : 0;
+                rest = up ? rest >> half : rest;
+            }
+            if (of[k] >= 0) to[k] = lo[k] * 32 + bit;
+        }
+    };
     if (blockIdx.x == 0 && tid == 0) {
         a.status[0] = N;
         a.status[1] = moves;
     }
-    int total;
-    int u = before + block_scan(used[0] + used[1] + used[2] + used[3], s_sum, &total);      // used pages below p
-#pragma unroll
-    for (int e = 0; e < kPerThread; ++e) {
-        const int p = p0 + e;
-        if (p >= d.num_pages) break;
-        int rank = -1;
-        if (used[e] && p >= N) rank = u - low;
-        else if (!used[e] && p < N) rank = p - u;
-        u += used[e];
-        if (rank >= d.max_moves) rank = -1;
-        if (rank >= 0) (used[e] ? a.copy_src : a.copy_dst)[rank] = p;
-        a.rank[p] = rank;
-        if (p >= moves && p < d.max_moves) {                        // (max_moves <= num_pages: every unused place is met)
-            a.copy_src[p] = -1;
-            a.copy_dst[p] = -1;
-        }
-    }
-}
-
-// Workgroups 0 .. chunks - 1: counts and map of a chunk of pages; those behind: the table.  Every count is read and written by
-// one thread each, so that the new counts may lie over the old ones.
-__global__ __launch_bounds__(kPagesThreads) void compact_write_kernel(CompactArgs a)
-{
-    const adaspec_pages_dims &d = a.dims;
-    const int N = a.status[0];
-    const int tid = threadIdx.x;
+    // of a page, or of what an entry names: the number of its move, or -1
+    auto move_of = [&](int p) {
+        if (p < N || p >= d.num_pages) return -1;
+        const int2 w = word(p / 32);
+        const int m = used_before(p, w) - low;
+        return (((uint32_t)w.x >> (p & 31)) & 1u) && m < d.max_moves ? m : -1;
+    };
+    // (what has to be looked up is, for all four, before anything is written: the loads are under way together)
     if ((int)blockIdx.x < a.chunks) {
-        int r[kPerThread], to[kPerThread];
-#pragma unroll
-        for (int k = 0; k < kPerThread; ++k) {                      // (all of them under way together)
-            const int p = blockIdx.x * kChunk + k * kPagesThreads + tid;
-            r[k] = p < d.num_pages ? a.rank[p] : -1;
-        }
+        int move[kPerThread], to[kPerThread] = {}, refs[kPerThread];
+        bool hole[kPerThread];
 #pragma unroll
         for (int k = 0; k < kPerThread; ++k) {
             const int p = blockIdx.x * kChunk + k * kPagesThreads + tid;
-            to[k] = r[k] >= 0 && p >= N ? a.copy_dst[r[k]] : p;
+            refs[k] = p < d.num_pages ? a.page_refs[p] : 0;
+            move[k] = move_of(p);
+            hole[k] = false;
+            if (p < N) {
+                const int2 w = word(p / 32);
+                hole[k] = !(((uint32_t)w.x >> (p & 31)) & 1u) && p - used_before(p, w) < d.max_moves;
+            }
         }
+        free_pages(move, to);
 #pragma unroll
         for (int k = 0; k < kPerThread; ++k) {
             const int p = blockIdx.x * kChunk + k * kPagesThreads + tid;
             if (p >= d.num_pages) break;
-            if (r[k] >= 0 && p < N) {
-                a.page_map[p] = -1;             // was free; its count comes from the page that moves here
+            if (p >= moves && p < d.max_moves) {                    // (max_moves <= num_pages: every unused place is met)
+                a.copy_src[p] = -1;
+                a.copy_dst[p] = -1;
+            }
+            if (move[k] >= 0) {                                     // its new place takes over its holders
+                a.out_refs[to[k]] = refs[k];
+                a.out_refs[p] = 0;
+                a.page_map[p] = to[k];
+                a.copy_src[move[k]] = p;
+                a.copy_dst[move[k]] = to[k];
+            } else if (hole[k]) {
+                a.page_map[p] = -1;                                 // was free; its count comes from the page that moves here
             } else {
-                const int refs = a.page_refs[p];
-                a.out_refs[to[k]] = refs;
-                if (to[k] != p) a.out_refs[p] = 0;
-                a.page_map[p] = refs > 0 ? to[k] : -1;
+                a.out_refs[p] = refs[k];
+                a.page_map[p] = refs[k] > 0 ? p : -1;
             }
         }
         return;
     }
     const int64_t n = (int64_t)d.old_batch * d.max_pages_per_req;
     for (int64_t e0 = (int64_t)(blockIdx.x - a.chunks) * kChunk; e0 < n; e0 += (int64_t)a.table_groups * kChunk) {
-        int p[kPerThread], r[kPerThread];
+        int p[kPerThread], move[kPerThread];
 #pragma unroll
         for (int k = 0; k < kPerThread; ++k) p[k] = e0 + k * kPagesThreads + tid < n ? a.block_table[e0 + k * kPagesThreads + tid] : -1;
 #pragma unroll
-        for (int k = 0; k < kPerThread; ++k) r[k] = p[k] >= N && p[k] < d.num_pages ? a.rank[p[k]] : -1;
-#pragma unroll
-        for (int k = 0; k < kPerThread; ++k)
-            if (r[k] >= 0) p[k] = a.copy_dst[r[k]];
+        for (int k = 0; k < kPerThread; ++k) move[k] = move_of(p[k]);
+        free_pages(move, p);
 #pragma unroll
         for (int k = 0; k < kPerThread; ++k)
             if (e0 + k * kPagesThreads + tid < n) a.out_table[e0 + k * kPagesThreads + tid] = p[k];
@@ -379,22 +617,27 @@ __global__ __launch_bounds__(kPagesThreads) void compact_write_kernel(CompactArg
 size_t compact_workspace(const adaspec_pages_dims &d, CompactArgs *a, char *ws)
 {
     const int chunks = ceil_div(d.num_pages, kChunk);
-    const size_t used = align_up((size_t)chunks * 4, 256), rank = align_up((size_t)d.num_pages * 4, 256);
+    const size_t used = align_up((size_t)chunks * (kChunk / kGrain) * 4, 256), words = align_up((size_t)chunks * (kChunk / 32) * 8, 256);
     if (a) {
         a->chunks = chunks;
-        a->chunk_used = reinterpret_cast<int32_t *>(ws);
-        a->rank = reinterpret_cast<int32_t *>(ws + used);
+        a->grain_used = reinterpret_cast<int32_t *>(ws);
+        a->words = reinterpret_cast<int2 *>(ws + used);
         const int64_t n = ((int64_t)d.old_batch * d.max_pages_per_req + kChunk - 1) / kChunk;
         a->table_groups = (int)(n < 2048 ? n : 2048);
     }
-    return used + rank;
+    return used + words;
 }
 
 hipError_t launch_kv_compact_pages(const CompactArgs &a, hipStream_t stream)
 {
-    hipLaunchKernelGGL(compact_count_kernel, dim3(a.chunks), dim3(kPagesThreads), 0, stream, a);
-    hipLaunchKernelGGL(compact_rank_kernel, dim3(a.chunks), dim3(kPagesThreads), 0, stream, a);
-    hipLaunchKernelGGL(compact_write_kernel, dim3(a.chunks + a.table_groups), dim3(kPagesThreads), 0, stream, a);
+    const dim3 grid(a.chunks + a.table_groups);
+    const size_t lds = ((size_t)a.chunks * (kChunk / kGrain) + 1) * 4;
+    if (a.dims.num_pages <= kSelfPages && a.out_refs != a.page_refs) {
+        hipLaunchKernelGGL(compact_write_kernel<true>, grid, dim3(kPagesThreads), lds, stream, a);
+    } else {
+        hipLaunchKernelGGL(compact_words_kernel, dim3(a.chunks), dim3(kPagesThreads), 0, stream, a);
+        hipLaunchKernelGGL(compact_write_kernel<false>, grid, dim3(kPagesThreads), lds, stream, a);
+    }
     return hipGetLastError();
 }
 

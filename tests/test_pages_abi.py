@@ -36,7 +36,7 @@ def test_remap_rejects_bad_dims(kw, code):
     assert _remap(d) == code and pkg.lib().adaspec_kv_remap_workspace_bytes(C.byref(d)) == 0
 
 
-@pytest.mark.parametrize("kw,code", SHARED + [(dict(max_moves=0), -2), (dict(max_moves=65), -2)])
+@pytest.mark.parametrize("kw,code", SHARED + [(dict(max_moves=0), -2), (dict(max_moves=65), -2), (dict(num_pages=(1 << 21) + 1), -6)])
 def test_compact_rejects_bad_dims(kw, code):
     d = _pages(**kw)
     assert _compact(d) == code and pkg.lib().adaspec_kv_compact_pages_workspace_bytes(C.byref(d)) == 0
