@@ -199,6 +199,7 @@ struct WindowPlan {
     WindowKind kind;
     int groups, rows_per_group;     // row groups of a request with max_spec_len + 1 rows, query rows (times G) in one
     int64_t units;                  // batch * n_kv_heads * groups
+    bool alone;                     // one wavefront per unit (attn_window_mfma.hip)
     int splits, block_pages;        // parts that the blocks of a unit's pages are cut into at most; pages per block
     size_t off_part_ml, off_part_o; // float[units][splits][rows_per_group][2], [d]: states of the parts
     size_t total_bytes;

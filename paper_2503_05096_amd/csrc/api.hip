@@ -428,7 +428,9 @@ static int validate_window(const adaspec_attn_dims *d, int32_t &window, int32_t 
     if (window > tokens) window = (int32_t)tokens;
     if (sinks > tokens) sinks = (int32_t)tokens;
     const WindowPlan p = make_window_plan(*d, window, sinks);
-    if (p.units * p.splits > INT32_MAX) return ADASPEC_ERR_UNSUPPORTED;
+    // grids (their threads are counted in 32 bits), and byte offsets inside a row group's Q rows
+    if ((int64_t)d->batch * p.groups >= 1 << 24 || p.units > INT32_MAX || d->n_kv_heads > 65535 || (int64_t)d->n_q_heads * d->head_dim > 1 << 23)
+        return ADASPEC_ERR_UNSUPPORTED;
     return ADASPEC_OK;
 }
 

@@ -12,7 +12,7 @@ namespace adaspec {
 
 struct WindowDims {                 // what every kernel needs to find its unit
     const int32_t *block_table, *ctx_lens, *spec_lens;
-    int total_q, max_spec_len, max_pages, Hq, Hkv, window, sinks, groups, rows_per_group;      // (16 max_pages is at most 2^30)
+    int batch, total_q, max_spec_len, max_pages, Hq, Hkv, window, sinks, groups, rows_per_group;      // (16 max_pages is at most 2^30)
 };
 
 struct WindowUnit {                 // wave-uniform
@@ -23,18 +23,34 @@ struct WindowUnit {                 // wave-uniform
     __device__ __forceinline__ int page_of(int v) const { return v < first ? v : v + skip; }
 };
 
-// Unit (i, rg, gkv); false: the request has fewer rows, or the lengths contradict the host's bounds.  Called by whole
-// wavefronts: the rows before the request are added up by the lanes.
-__device__ __forceinline__ bool window_unit(WindowUnit &u, const WindowDims &d, int i, int rg, int gkv, int lane)
+// Rows of the requests before request i, added up by the lanes of a whole wavefront.  Two steps, so that the loads are under way
+// while the unit's first pages are looked up: nothing but Q and the results needs the sum.
+struct RowsBefore {
+    static constexpr int kAhead = 4;
+    int k[kAhead];
+    __device__ __forceinline__ RowsBefore(const WindowDims &d, int i, int lane)
+    {
+#pragma unroll
+        for (int c = 0; c < kAhead; ++c) k[c] = c * kWave + lane < i ? d.spec_lens[c * kWave + lane] : -1;
+    }
+    __device__ __forceinline__ int sum(const WindowDims &d, int i, int lane) const
+    {
+        int part = 0;
+#pragma unroll
+        for (int c = 0; c < kAhead; ++c) part += c * kWave + lane < i ? min(max(k[c], 0), d.max_spec_len) + 1 : 0;
+        for (int j = kAhead * kWave + lane; j < i; j += kWave) part += min(max(d.spec_lens[j], 0), d.max_spec_len) + 1;
+        return wave_sum(part);
+    }
+};
+
+// Unit (i, rg, gkv) but for its first row; false: the request has fewer rows.
+__device__ __forceinline__ bool window_unit(WindowUnit &u, const WindowDims &d, int i, int rg, int gkv)
 {
     u.i = i; u.rg = rg; u.gkv = gkv;
     u.bt_off = (int64_t)i * d.max_pages;
     const int G = d.Hq / d.Hkv;
-    int part = 0;
-    for (int j = lane; j < i; j += kWave) part += min(max(d.spec_lens[j], 0), d.max_spec_len) + 1;
     u.L = min(max(d.ctx_lens[i], 1), d.max_pages * 16);
     u.n = min(max(d.spec_lens[i], 0), d.max_spec_len) + 1;
-    u.qrow0 = wave_sum(part);
     u.rows = u.n * G;
     u.r0 = rg * d.rows_per_group;
     u.window = d.window; u.sinks = d.sinks;
@@ -45,7 +61,7 @@ __device__ __forceinline__ bool window_unit(WindowUnit &u, const WindowDims &d, 
     u.first = min((u.sinks + 15) >> 4, low);
     u.skip = low - u.first;
     u.pages = max(end - u.skip, 0);
-    return u.r0 < u.rows && u.qrow0 + u.n <= d.total_q;
+    return u.r0 < u.rows;
 }
 
 // whether the row at position `pos` sees token t

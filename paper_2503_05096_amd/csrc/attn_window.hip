@@ -12,6 +12,7 @@ namespace adaspec {
 
 constexpr int kWinRows = 8;
 constexpr int kWinMaxD = 256;
+constexpr int kWindowMaxSplits = 64;        // a lane of the combine kernel each
 
 template <class T>
 __global__ __launch_bounds__(64) void attn_window_vector_kernel(WindowDims dims, const void *__restrict__ q,
@@ -22,9 +23,12 @@ __global__ __launch_bounds__(64) void attn_window_vector_kernel(WindowDims dims,
     __shared__ float ps[kWinRows][64];
     const int lane = threadIdx.x;
     const int G = dims.Hq / dims.Hkv;
-    const int gkv = blockIdx.x % dims.Hkv, rest = blockIdx.x / dims.Hkv;
+    const int gkv = blockIdx.y, i = blockIdx.x / dims.groups;
+    const RowsBefore before(dims, i, lane);
     WindowUnit u;
-    if (!window_unit(u, dims, rest / dims.groups, rest % dims.groups, gkv, lane)) return;
+    if (!window_unit(u, dims, i, blockIdx.x % dims.groups, gkv)) return;
+    u.qrow0 = before.sum(dims, i, lane);
+    if (u.qrow0 + u.n > dims.total_q) return;                       // inconsistent lengths
 
     for (int idx = lane; idx < kWinRows * d; idx += 64) {
         const int r = u.r0 + idx / d, c = idx % d;
@@ -115,48 +119,55 @@ __global__ __launch_bounds__(64) void attn_window_vector_kernel(WindowDims dims,
 }
 
 // Rows of a unit whose pages were cut: out = sum_s 2^(m_s - m*) O_s / sum_s 2^(m_s - m*) l_s.  One wavefront per row, four
-// rows of a unit per workgroup; lane s looks at (m_s, l_s), the O_s are requested four at a time.
+// rows of a unit per workgroup; lane s looks at (m_s, l_s).  Latency is all there is to it: the states of the first parts are
+// requested before it is known how many parts there are (the places are there in any case).
 template <int D>
 __global__ __launch_bounds__(256) void attn_window_combine_kernel(WindowDims dims, const float *__restrict__ part_ml,
                                                                   const float *__restrict__ part_o, void *__restrict__ out, int splits,
                                                                   int block_pages, int out_dtype)
 {
-    constexpr int kE = D / 64;
+    constexpr int kE = D / 64, kAhead = 16;
     const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int quads = dims.rows_per_group / 4, unit = blockIdx.x / quads, rl = 4 * (blockIdx.x % quads) + wv;
+    const int i = blockIdx.x / dims.groups, rl = 4 * blockIdx.z + wv;
+    const RowsBefore before(dims, i, lane);
+    const int64_t first = ((int64_t)blockIdx.x * dims.Hkv + blockIdx.y) * splits * dims.rows_per_group + rl;
+    float2 ml = make_float2(-INFINITY, 0.f);
+    if (lane < splits) ml = *reinterpret_cast<const float2 *>(part_ml + (first + (int64_t)lane * dims.rows_per_group) * 2);
+    const float *o = part_o + first * D + kE * lane;
+    float x[kAhead][kE];
+#pragma unroll
+    for (int s = 0; s < kAhead; ++s)
+#pragma unroll
+        for (int e = 0; e < kE; ++e) x[s][e] = s < splits ? o[(int64_t)s * dims.rows_per_group * D + e] : 0.f;
     WindowUnit u;
-    if (!window_unit(u, dims, unit / (dims.Hkv * dims.groups), unit / dims.Hkv % dims.groups, unit % dims.Hkv, lane)) return;
+    if (!window_unit(u, dims, i, blockIdx.x % dims.groups, blockIdx.y)) return;
     const int row = u.r0 + rl;
     const int all_blocks = (u.pages + block_pages - 1) / block_pages, per = (all_blocks + splits - 1) / splits;
-    const int ns = per > 0 ? (all_blocks + per - 1) / per : 1;      // (at most 64)
-    if (ns == 1 || row >= u.rows) return;
-    const int64_t first = (int64_t)unit * splits * dims.rows_per_group + rl;
-    float2 ml = make_float2(-INFINITY, 0.f);
-    if (lane < ns) ml = *reinterpret_cast<const float2 *>(part_ml + (first + (int64_t)lane * dims.rows_per_group) * 2);
+    const int ns = per > 0 ? (all_blocks + per - 1) / per : 1;      // (at most kWindowMaxSplits)
+    u.qrow0 = before.sum(dims, i, lane);
+    if (ns == 1 || row >= u.rows || u.qrow0 + u.n > dims.total_q) return;
+    if (lane >= ns) ml = make_float2(-INFINITY, 0.f);
     const float m = wave_max(ml.x);
     const float w = lane < ns ? (m > -INFINITY ? __builtin_amdgcn_exp2f(ml.x - m) : 1.f) : 0.f;
-    const float den = wave_sum(w * ml.y);
+    const float inv = 1.0f / wave_sum(w * ml.y);
     float acc[kE] = {};
-    const float *o = part_o + first * D + kE * lane;
-    for (int s0 = 0; s0 < ns; s0 += 4) {
-        float x[4][kE];
 #pragma unroll
-        for (int s = 0; s < 4; ++s)
+    for (int s = 0; s < kAhead; ++s) {
+        const float ws = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w), s));
+        if (s < ns) {
 #pragma unroll
-            for (int e = 0; e < kE; ++e) x[s][e] = o[(int64_t)min(s0 + s, ns - 1) * dims.rows_per_group * D + e];
-#pragma unroll
-        for (int s = 0; s < 4; ++s) {
-            const float ws = __shfl(w, s0 + s, kWave);              // (0 behind the last)
-            if (s0 + s < ns) {
-#pragma unroll
-                for (int e = 0; e < kE; ++e) acc[e] += ws * x[s][e];
-            }
+            for (int e = 0; e < kE; ++e) acc[e] += ws * x[s][e];
         }
+    }
+    for (int s = kAhead; s < ns; ++s) {
+        const float ws = __shfl(w, s, kWave);
+#pragma unroll
+        for (int e = 0; e < kE; ++e) acc[e] += ws * o[(int64_t)s * dims.rows_per_group * D + e];
     }
     const int G = dims.Hq / dims.Hkv;
     const int64_t obase = ((u.qrow0 + row / G) * dims.Hq + u.gkv * G + row % G) * (int64_t)D + kE * lane;
 #pragma unroll
-    for (int e = 0; e < kE; ++e) store_out(out, obase + e, acc[e] * (1.0f / den), out_dtype);
+    for (int e = 0; e < kE; ++e) store_out(out, obase + e, acc[e] * inv, out_dtype);
 }
 
 bool window_fast_supported(const adaspec_attn_dims &d)
@@ -174,16 +185,33 @@ WindowPlan make_window_plan(const adaspec_attn_dims &d, int window, int sinks)
     p.groups = (int)((rows + p.rows_per_group - 1) / p.rows_per_group);
     p.units = (int64_t)d.batch * d.n_kv_heads * p.groups;
     p.splits = 1;
+    p.alone = false;
     p.block_pages = d.dtype == ADASPEC_F32 ? 1 : d.head_dim == 64 ? 4 : 2;
     if (p.kind == WindowKind::kMfma) {
         // entries of a unit's list of pages at most: a row group spans this many positions
         const int64_t span = (p.rows_per_group - 1) / G + 2 < d.max_spec_len + 1 ? (p.rows_per_group - 1) / G + 2 : d.max_spec_len + 1;
         int64_t pages = ((int64_t)sinks + 15) / 16 + ((int64_t)window + span + 14) / 16 + 1;
         if (pages > d.max_pages_per_req) pages = d.max_pages_per_req;
-        const int64_t turns = (pages + 4 * p.block_pages - 1) / (4 * p.block_pages);       // of the four wavefronts
-        int64_t want = p.units > 0 ? 512 / p.units : 1;
-        if (want > turns / 2) want = turns / 2;
-        p.splits = (int)(want > 1 ? want : 1);
+        const int64_t blocks = (pages + p.block_pages - 1) / p.block_pages, turns = (blocks + 3) / 4;   // turns of four wavefronts
+        // One wavefront per unit where units are many and short.  A workgroup of four costs its look-ups, its merging and its
+        // quarter-filled last turn whatever the length: 512 of them fill the chip, a thousand lone wavefronts take their place.
+        // Measured, alone / four (us, 16 bits, 8 kv heads, 1-3 drafts; window 16, 128, 256, 512, 1024):
+        //   head_dim 128, 320 units   7.5/7.3   11.6/9.9    17.0/12.7  27.8/19.7   48.8/33.9
+        //   head_dim 128, 528 units   8.0/10.3  13.2/15.4   20.0/20.4  33.1/31.3   59.6/53.5
+        //   head_dim 128, 1152 units  10.4/15.6 19.8/25.1   32.0/33.6  56.7/55.2  105.7/101.7
+        //   head_dim 64, 1152 units   7.7/14.6  13.4/16.9   19.6/25.2  31.9/32.7   56.3/53.8
+        p.alone = d.dtype != ADASPEC_F32 && p.rows_per_group <= 48 && p.units > 512 && blocks <= 10;
+        // Parts of a unit where units are few: one workgroup per compute unit in all, at least two blocks in a part, and only
+        // where that saves the joining launch's 3-4 us: four turns, or eight with less than four parts, whose workgroups
+        // still wait for each other's memory.  Measured, parts / whole (us, head_dim 128, 16 bits):
+        //   window 1024: 8 units, 16 parts 10.7/17.6; 64 units, 4 parts 15.7/18.6; 128 units, 2 parts 21.0/19.5; 256 units, 2 parts 33/26.5
+        //   window 4096: 8 units, 16 parts 13.5/47.7; 64 units, 4 parts 29.9/49.0; 128 units, 2 parts 50.0/53.5
+        if (!p.alone && p.units > 0) {
+            int64_t want = 256 / p.units;
+            if (want > blocks / 2) want = blocks / 2;
+            if (want > kWindowMaxSplits) want = kWindowMaxSplits;
+            if (want > 1 && turns - (blocks + 4 * want - 1) / (4 * want) >= (want >= 4 ? 4 : 8)) p.splits = (int)want;
+        }
     }
     size_t off = 0;
     p.off_part_ml = off;
@@ -197,14 +225,14 @@ WindowPlan make_window_plan(const adaspec_attn_dims &d, int window, int sinks)
 hipError_t launch_attn_window(const WindowArgs &a)
 {
     const adaspec_attn_dims &d = a.dims;
-    const WindowDims w{a.block_table, a.ctx_lens, a.spec_lens, d.total_q, d.max_spec_len, d.max_pages_per_req, d.n_q_heads,
+    const WindowDims w{a.block_table, a.ctx_lens, a.spec_lens, d.batch, d.total_q, d.max_spec_len, d.max_pages_per_req, d.n_q_heads,
                        d.n_kv_heads, a.window, a.sinks, a.plan.groups, a.plan.rows_per_group};
     const WindowPlan &p = a.plan;
     if (p.kind == WindowKind::kMfma) {
         const hipError_t e = d.dtype == ADASPEC_F32 ? launch_attn_window_f32(a, w) : launch_attn_window_mfma(a, w);
         if (e != hipSuccess || p.splits == 1) return e;
         auto combine = [&](auto dim) {
-            hipLaunchKernelGGL((attn_window_combine_kernel<decltype(dim)::value>), dim3((unsigned)(p.units * p.rows_per_group / 4)), dim3(256), 0,
+            hipLaunchKernelGGL((attn_window_combine_kernel<decltype(dim)::value>), dim3((unsigned)(d.batch * p.groups), d.n_kv_heads, p.rows_per_group / 4), dim3(256), 0,
                                a.stream, w, (const float *)(a.ws + p.off_part_ml), (const float *)(a.ws + p.off_part_o), a.out, p.splits,
                                p.block_pages, d.out_dtype);
         };
@@ -213,7 +241,7 @@ hipError_t launch_attn_window(const WindowArgs &a)
         return hipGetLastError();
     }
     auto launch = [&](auto tag) {
-        hipLaunchKernelGGL(attn_window_vector_kernel<decltype(tag)>, dim3((unsigned)a.plan.units), dim3(64), 0, a.stream, w, a.q,
+        hipLaunchKernelGGL(attn_window_vector_kernel<decltype(tag)>, dim3((unsigned)(d.batch * a.plan.groups), d.n_kv_heads), dim3(64), 0, a.stream, w, a.q,
                            a.k_pages, a.v_pages, a.out, d.head_dim, a.scale_log2, d.out_dtype);
     };
     if (d.dtype == ADASPEC_F32) launch(F32{});

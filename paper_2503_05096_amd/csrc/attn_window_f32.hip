@@ -28,9 +28,10 @@ __global__ __launch_bounds__(256, (RT <= 2 ? 2 : 1)) void attn_window_f32_kernel
     const int g = lane >> 4, n16 = lane & 15;
     const int G = dims.Hq / dims.Hkv;
 
-    const int sp = blockIdx.x % splits, unit = blockIdx.x / splits;
+    const int sp = blockIdx.z, i = blockIdx.x / dims.groups;
+    const RowsBefore before(dims, i, lane);
     WindowUnit u;
-    if (!window_unit(u, dims, unit / (dims.Hkv * dims.groups), unit / dims.Hkv % dims.groups, unit % dims.Hkv, lane)) return;
+    if (!window_unit(u, dims, i, blockIdx.x % dims.groups, blockIdx.y)) return;
     const int per = (u.pages + splits - 1) / splits, ns = per > 0 ? (u.pages + per - 1) / per : 1;
     const int b0 = sp * per, b1 = min(u.pages, b0 + per);
     if (sp >= ns) return;
@@ -49,16 +50,18 @@ __global__ __launch_bounds__(256, (RT <= 2 ? 2 : 1)) void attn_window_f32_kernel
 #pragma unroll
             for (int h = 0; h < kH; ++h) vreg[r][h] = __builtin_nontemporal_load(reinterpret_cast<const f32x4 *>(v_pages + at + v_lane_off + r * (D * 4) + 256 * h));
     };
+    if (b0 + wv < b1) {
+        const int64_t at = page_base(b0 + wv);
+        load_k(at);
+        load_v(at);
+    }
+    u.qrow0 = before.sum(dims, i, lane);
+    if (u.qrow0 + u.n > dims.total_q) return;                       // inconsistent lengths
     f32x4 qv[kQLoads];
 #pragma unroll
     for (int k = 0; k < kQLoads; ++k) {                             // entry (row tile, j, lane)
         const int e = (tid >> 6) + 4 * k, row = min(u.r0 + 16 * (e / kJ) + n16, u.rows - 1);
         qv[k] = *reinterpret_cast<const f32x4 *>(q + (((u.qrow0 + row / G) * dims.Hq + u.gkv * G + row % G) * (int64_t)D + 16 * (e % kJ) + 4 * g) * 4);
-    }
-    if (b0 + wv < b1) {
-        const int64_t at = page_base(b0 + wv);
-        load_k(at);
-        load_v(at);
     }
 #pragma unroll
     for (int k = 0; k < kQLoads; ++k) q_lds[tid + 256 * k] = qv[k];
@@ -177,7 +180,7 @@ __global__ __launch_bounds__(256, (RT <= 2 ? 2 : 1)) void attn_window_f32_kernel
                     f32x4{o[nt][h][0][r], o[nt][h][1][r], o[nt][h][2][r], o[nt][h][3][r]};
         lds_barrier();
         finish_window_tile<F32, D>(u, dims, block_table, q, k_pages, v_pages, out, part_ml, part_o, slabs, kSlab, s_m, s_l, kRows, nt, ns, b0, b1, scale_log2,
-                                   0.f, ADASPEC_F32, ((int64_t)unit * splits + sp) * kRows);
+                                   0.f, ADASPEC_F32, (((int64_t)blockIdx.x * dims.Hkv + blockIdx.y) * splits + sp) * kRows);
         if (nt + 1 < RT) lds_barrier();                             // the next tile overwrites the slabs
     }
 }
@@ -186,7 +189,7 @@ hipError_t launch_attn_window_f32(const WindowArgs &a, const WindowDims &w)
 {
     const WindowPlan &p = a.plan;
     auto launch = [&](auto dim, auto rt) {
-        hipLaunchKernelGGL((attn_window_f32_kernel<decltype(dim)::value, decltype(rt)::value>), dim3((unsigned)(p.units * p.splits)), dim3(256), 0,
+        hipLaunchKernelGGL((attn_window_f32_kernel<decltype(dim)::value, decltype(rt)::value>), dim3((unsigned)(a.dims.batch * p.groups), a.dims.n_kv_heads, p.splits), dim3(256), 0,
                            a.stream, w, a.block_table, (const char *)a.q, (const char *)a.k_pages, (const char *)a.v_pages, a.out,
                            (float *)(a.ws + p.off_part_ml), (float *)(a.ws + p.off_part_o), p.splits, a.scale_log2);
     };

@@ -20,7 +20,6 @@
 namespace adaspec {
 
 constexpr int kSlotBytes = 8192;                // K, or V, of a block
-constexpr int kWinRing = kWaves * 2 * kSlotBytes;
 
 template <class T> struct WindowWeights;
 template <> struct WindowWeights<BF16> {
@@ -34,13 +33,18 @@ template <> struct WindowWeights<F16> {         // kept 2^7 larger: at most 2^15
     static __device__ __forceinline__ float hi(uint32_t w) { return f16_bits_to_float((uint16_t)(w >> 16)); }
 };
 
-// LDS of a workgroup: the slots; Q^T operands in MFMA lane order; (m, l) of every wavefront's rows, which take the place of
-// Q where two workgroups would not fit a compute unit otherwise.
-template <int D, int RT> struct WindowLds {
-    static constexpr int kRows = 16 * RT;
+// Two forms (make_window_plan chooses):
+//   four wavefronts per unit: K and V through slots of the wavefronts, two workgroups per compute unit;
+//   kAlone, one: nothing to merge, for many short units.  K goes to the registers that its operands are read into anyway, only V
+//   has a slot, so that twelve to sixteen (of one row tile; eight of three) of these workgroups fit a compute unit.
+// LDS: the slots; Q^T operands in MFMA lane order; (m, l) of every wavefront's rows, which take the place of Q where two
+// workgroups would not fit otherwise.
+template <int D, int RT, bool kAlone> struct WindowLds {
+    static constexpr int kWavesHere = kAlone ? 1 : kWaves, kRows = 16 * RT;
+    static constexpr int kV = kAlone ? 0 : kSlotBytes, kWaveBytes = kV + kSlotBytes;
     static constexpr bool kFull = RT == 4 && D == 128;
-    static constexpr int kQ = kWinRing, kQBytes = RT * (D / 32) * 1024;
-    static constexpr int kMl = kFull ? kQ : kQ + kQBytes, kMlBytes = kWaves * kRows * 2 * 4;
+    static constexpr int kQ = kWavesHere * kWaveBytes, kQBytes = RT * (D / 32) * 1024;
+    static constexpr int kMl = kFull ? kQ : kQ + kQBytes, kMlBytes = kAlone ? 0 : kWaves * kRows * 2 * 4;
     static constexpr int kBytes = kFull ? kQ + kQBytes : kMl + kMlBytes;
     static_assert(kBytes <= 81920, "two workgroups per compute unit");
 };
@@ -52,27 +56,28 @@ __device__ __forceinline__ void load_lds_2(const v4i32 &rsrc, uint32_t off0, uin
                  :: "s"(lds), "v"(off0), "v"(off1), "s"(rsrc) : "memory", "m0");
 }
 
-template <class T, int D, int RT>
-__global__ __launch_bounds__(256, 2) void attn_window_kernel(WindowDims dims, const int32_t *__restrict__ block_table,
+template <class T, int D, int RT, bool kAlone>
+__global__ __launch_bounds__(kAlone ? 64 : 256, kAlone ? (RT == 1 ? 4 : RT == 2 && D == 64 ? 3 : 2) : 2) void attn_window_kernel(WindowDims dims, const int32_t *__restrict__ block_table,
                                                              const char *__restrict__ q, const char *__restrict__ k_pages, const char *__restrict__ v_pages,
                                                              void *__restrict__ out, float *__restrict__ part_ml,
                                                              float *__restrict__ part_o, int splits, float scale_log2, int out_dtype)
 {
-    using Lds = WindowLds<D, RT>;
+    using Lds = WindowLds<D, RT, kAlone>;
+    constexpr int kStep = Lds::kWavesHere;                          // wavefronts that share a unit's blocks
     using Weights = WindowWeights<T>;
     constexpr int kRows = 16 * RT, kS = D / 32, kDt = D / 16, kPages = 256 / D, kPageBytes = 32 * D, kRowBytes = 2 * D;
     __shared__ __attribute__((aligned(1024))) char smem[Lds::kBytes];
     const uint32_t lds_base = lds_address(smem);
     float *s_m = reinterpret_cast<float *>(smem + Lds::kMl), *s_l = s_m + kWaves * kRows;    // [wavefront][row]
     const int tid = threadIdx.x, lane = tid & 63;
-    const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wv = kAlone ? 0 : __builtin_amdgcn_readfirstlane(tid >> 6);
     const int g = lane >> 4, n16 = lane & 15;
     const int G = dims.Hq / dims.Hkv;
 
-    const int sp = blockIdx.x % splits, unit = blockIdx.x / splits;
+    const int sp = blockIdx.z, i = blockIdx.x / dims.groups;
+    const RowsBefore before(dims, i, lane);
     WindowUnit u;
-    if (!window_unit(u, dims, unit / (dims.Hkv * dims.groups), unit / dims.Hkv % dims.groups, unit % dims.Hkv, lane)) return;
-    u.qrow0 = __builtin_amdgcn_readfirstlane((int)u.qrow0);
+    if (!window_unit(u, dims, i, blockIdx.x % dims.groups, blockIdx.y)) return;
     const int all_blocks = (u.pages + kPages - 1) / kPages, per = (all_blocks + splits - 1) / splits;
     const int ns = per > 0 ? (all_blocks + per - 1) / per : 1;
     const int b0 = sp * per, b1 = min(all_blocks, b0 + per);
@@ -82,8 +87,8 @@ __global__ __launch_bounds__(256, 2) void attn_window_kernel(WindowDims dims, co
     // Token rows of 256 (128) bytes.  In K's the 16-byte chunk c of token t stands at place c ^ key of its row (key: t % 16 at
     // head_dim 128, t / 2 % 8 at 64), in V's the 32-byte chunk cc at place cc ^ key (t % 8, t / 2 % 4): operand reads, of one chunk
     // of 16 tokens in a row, meet no bank twice, while the loader fetches whole rows.
-    char *k_slot = smem + wv * 2 * kSlotBytes, *v_slot = k_slot + kSlotBytes;
-    const uint32_t k_lds = lds_base + wv * 2 * kSlotBytes, v_lds = k_lds + kSlotBytes;
+    char *k_slot = smem + wv * Lds::kWaveBytes, *v_slot = k_slot + Lds::kV;
+    const uint32_t k_lds = lds_base + wv * Lds::kWaveBytes, v_lds = k_lds + Lds::kV;
     constexpr int kLoads = kPageBytes / 1024;                       // load instructions per page
     uint32_t k_voff[kLoads], v_voff[kLoads], k_rd[kS], v_rd;
 #pragma unroll
@@ -129,29 +134,46 @@ __global__ __launch_bounds__(256, 2) void attn_window_kernel(WindowDims dims, co
         }
     };
 
+    // K as A operand of (mt, s): lane (g, m) <- token m of page mt, channels 32 s + 8 g .. + 7
+    uint4 ka[kPages][kS];
+    auto request_k = [&]() {
+        if constexpr (kAlone) {
+#pragma unroll
+            for (int mt = 0; mt < kPages; ++mt)
+#pragma unroll
+                for (int s = 0; s < kS; ++s) ka[mt][s] = ld16_stream(k_pages + base[mt] + n16 * kRowBytes + 64 * s + 16 * g);
+        } else {
+            issue(k_pages, k_voff, k_lds);
+        }
+    };
+
     const bool works = b0 + wv < b1;
     if (works) {
         look_up(b0 + wv);
-        issue(k_pages, k_voff, k_lds);
+        request_k();
+    }
+    u.qrow0 = __builtin_amdgcn_readfirstlane(before.sum(dims, i, lane));
+    if (u.qrow0 + u.n > dims.total_q) {                             // inconsistent lengths
+        wait_loads<0>();
+        return;
     }
     // Q^T operands: entry (row tile, s) of 1 KB, shared out to the wavefronts.  Rows past the last one repeat it (their results
     // are never stored).
 #pragma unroll
-    for (int e0 = 0; e0 < RT * kS; e0 += kWaves) {
+    for (int e0 = 0; e0 < RT * kS; e0 += kStep) {
         const int e = e0 + wv;
-        if (RT * kS % kWaves == 0 || e < RT * kS) {
+        if (RT * kS % kStep == 0 || e < RT * kS) {
             const int row = min(u.r0 + 16 * (e / kS) + n16, u.rows - 1), n0 = u.r0 / G;
             const v4i32 rs = buffer_rsrc(q + (u.qrow0 + n0) * dims.Hq * (int64_t)kRowBytes, (uint32_t)(min(u.n - n0, kRows + 1) * dims.Hq) * kRowBytes);
             load16_to_lds(rs, (uint32_t)(((row / G - n0) * dims.Hq + u.gkv * G + row % G) * kRowBytes + 64 * (e % kS) + 16 * g), lds_base + Lds::kQ + e * 1024);
         }
     }
-    if (works) {
-        issue(v_pages, v_voff, v_lds);
-        wait_loads<8>();                                            // all but the first block's V
-    } else {
-        wait_loads<0>();
+    if (works) issue(v_pages, v_voff, v_lds);
+    if (!works) wait_loads<0>();
+    if constexpr (!kAlone) {
+        if (works) wait_loads<8>();                                 // all but the first block's V
+        lds_barrier();
     }
-    lds_barrier();
 
     int pos[RT];
 #pragma unroll
@@ -170,7 +192,7 @@ __global__ __launch_bounds__(256, 2) void attn_window_kernel(WindowDims dims, co
     }
 
 #pragma unroll 1
-    for (int bi = b0 + wv; bi < b1; bi += kWaves) {
+    for (int bi = b0 + wv; bi < b1; bi += kStep) {
         // first token of every page of the block; a place past the list's end is behind every row
         int tb[kPages];
         bool need_mask = false;
@@ -180,19 +202,21 @@ __global__ __launch_bounds__(256, 2) void attn_window_kernel(WindowDims dims, co
             tb[j] = v < u.pages ? u.page_of(v) * 16 : 1 << 30;
             need_mask |= tb[j] + 15 > oldest || !(newest - tb[j] < u.window || tb[j] + 15 < u.sinks);
         }
-        const bool more = bi + kWaves < b1;
-        if (more) look_up(bi + kWaves);
-        if (bi != b0 + wv) wait_loads<8>();                         // K of this block (its V is 8 loads younger)
-
-        // ---- K operands out of the slot, the next block's K into it ----------------------------------------
-        uint4 ka[kPages][kS];
+        const bool more = bi + kStep < b1;
+        if (more) look_up(bi + kStep);
+        if constexpr (kAlone) {
+            wait_loads<0>();                                        // K and V of this block (and Q)
+        } else {
+            if (bi != b0 + wv) wait_loads<8>();                     // K of this block (its V is 8 loads younger)
+            // ---- K operands out of the slot, the next block's K into it ----------------------------------------
 #pragma unroll
-        for (int mt = 0; mt < kPages; ++mt)
+            for (int mt = 0; mt < kPages; ++mt)
 #pragma unroll
-            for (int s = 0; s < kS; ++s) ka[mt][s] = *reinterpret_cast<const uint4 *>(k_slot + mt * kPageBytes + k_rd[s]);
-        if (more) {
-            wait_lds();
-            issue(k_pages, k_voff, k_lds);
+                for (int s = 0; s < kS; ++s) ka[mt][s] = *reinterpret_cast<const uint4 *>(k_slot + mt * kPageBytes + k_rd[s]);
+            if (more) {
+                wait_lds();
+                request_k();
+            }
         }
 
         // ---- S^T = K Q^T, online softmax (per lane: row n16 of each row tile, 4 tokens of every page) -----------
@@ -210,6 +234,9 @@ __global__ __launch_bounds__(256, 2) void attn_window_kernel(WindowDims dims, co
                 for (int s = 0; s < kS; ++s) acc = Mma<T>::run(ka[mt][s], qop[s], acc);
 #pragma unroll
                 for (int r = 0; r < 4; ++r) p[4 * mt + r] = acc[r];
+            }
+            if constexpr (kAlone) {
+                if (nt == RT - 1 && more) request_k();              // (all row tiles have had their products)
             }
             if (need_mask) {
 #pragma unroll
@@ -250,8 +277,10 @@ __global__ __launch_bounds__(256, 2) void attn_window_kernel(WindowDims dims, co
         }
 
         // ---- V of this block: zero for tokens that no row sees -----------------------------------------
-        if (more) wait_loads<8>();
-        else wait_loads<0>();
+        if constexpr (!kAlone) {
+            if (more) wait_loads<8>();
+            else wait_loads<0>();
+        }
         if (need_mask) {
             constexpr int kLanesPerRow = kRowBytes / 16, kRowsPerStep = 64 / kLanesPerRow;
 #pragma unroll
@@ -285,6 +314,43 @@ __global__ __launch_bounds__(256, 2) void attn_window_kernel(WindowDims dims, co
         }
     }
 
+    if constexpr (kAlone) {
+        // the state is the result: lane (g, n16) holds the channels 16 dt + 4 g .. + 3 of row n16
+#pragma unroll
+        for (int nt = 0; nt < RT; ++nt) {
+            lsum[nt] += __shfl_xor(lsum[nt], 16, kWave);
+            lsum[nt] += __shfl_xor(lsum[nt], 32, kWave);
+            const int row = u.r0 + 16 * nt + n16;
+            float total = lsum[nt];
+#pragma unroll
+            for (int dt = 0; dt < kDt; ++dt) total += (o[nt][dt][0] + o[nt][dt][1]) + (o[nt][dt][2] + o[nt][dt][3]);
+            unsigned long long odd = __ballot(row < u.rows && !(fabsf(total) < INFINITY));
+            while (__builtin_expect(odd != 0, 0)) {
+                const int of = (int)__builtin_ctzll(odd) & 15;
+                float rm, rsum;
+                float2 ra;
+                row_by_selection<T, D>(u, dims, block_table, q, k_pages, v_pages, u.r0 + 16 * nt + of, 0, u.pages, scale_log2, rm, rsum, ra);
+#pragma unroll
+                for (int dt = 0; dt < kDt; ++dt) {
+                    const int from = 8 * dt + 2 * g;
+                    const f32x4 val = {__shfl(ra.x, from, kWave), __shfl(ra.y, from, kWave), __shfl(ra.x, from + 1, kWave), __shfl(ra.y, from + 1, kWave)};
+                    if (n16 == of) o[nt][dt] = val;
+                }
+                if (n16 == of) lsum[nt] = rsum;
+                odd &= ~(0x0001000100010001ull << of);
+            }
+            if (row >= u.rows) continue;
+            const float inv = 1.0f / lsum[nt];
+            const int64_t obase = ((u.qrow0 + row / G) * dims.Hq + u.gkv * G + row % G) * (int64_t)D + 4 * g;
+#pragma unroll
+            for (int dt = 0; dt < kDt; ++dt) {
+                const f32x4 val = o[nt][dt] * inv;
+                if (out_dtype == ADASPEC_F32) *reinterpret_cast<f32x4 *>(reinterpret_cast<float *>(out) + obase + 16 * dt) = val;
+                else *reinterpret_cast<uint2 *>(reinterpret_cast<uint16_t *>(out) + obase + 16 * dt) = make_uint2(Mma<T>::pack2(val[0], val[1]), Mma<T>::pack2(val[2], val[3]));
+            }
+        }
+        return;
+    }
     // ---- merge the four wavefronts' states through LDS, one row tile at a time, each wavefront's in its V slot
     if constexpr (Lds::kFull) lds_barrier();                        // (m, l) go where Q stands: all are done with it
 #pragma unroll
@@ -300,8 +366,8 @@ __global__ __launch_bounds__(256, 2) void attn_window_kernel(WindowDims dims, co
         for (int dt = 0; dt < kDt; ++dt)
             *reinterpret_cast<f32x4 *>(v_slot + window_piece<D>(n16, 4 * dt + g)) = o[nt][dt];
         lds_barrier();
-        finish_window_tile<T, D>(u, dims, block_table, q, k_pages, v_pages, out, part_ml, part_o, smem + kSlotBytes, 2 * kSlotBytes, s_m, s_l, kRows, nt, ns, b0 * kPages,
-                                 min(b1 * kPages, u.pages), scale_log2, Weights::kShiftLog2, out_dtype, ((int64_t)unit * splits + sp) * kRows);
+        finish_window_tile<T, D>(u, dims, block_table, q, k_pages, v_pages, out, part_ml, part_o, smem + Lds::kV, Lds::kWaveBytes, s_m, s_l, kRows, nt, ns, b0 * kPages,
+                                 min(b1 * kPages, u.pages), scale_log2, Weights::kShiftLog2, out_dtype, (((int64_t)blockIdx.x * dims.Hkv + blockIdx.y) * splits + sp) * kRows);
         if (nt + 1 < RT) lds_barrier();                             // the next tile overwrites the slots
     }
 }
@@ -311,17 +377,22 @@ hipError_t launch_attn_window_mfma(const WindowArgs &a, const WindowDims &w)
     const adaspec_attn_dims &d = a.dims;
     const WindowPlan &p = a.plan;
     float *ml = reinterpret_cast<float *>(a.ws + p.off_part_ml), *o = reinterpret_cast<float *>(a.ws + p.off_part_o);
-    auto launch = [&](auto tag, auto dim, auto rt) {
-        hipLaunchKernelGGL((attn_window_kernel<decltype(tag), decltype(dim)::value, decltype(rt)::value>), dim3((unsigned)(p.units * p.splits)),
-                           dim3(256), 0, a.stream, w, a.block_table, (const char *)a.q, (const char *)a.k_pages, (const char *)a.v_pages, a.out, ml, o,
-                           p.splits, a.scale_log2, d.out_dtype);
+    auto launch = [&](auto tag, auto dim, auto rt, auto alone) {
+        hipLaunchKernelGGL((attn_window_kernel<decltype(tag), decltype(dim)::value, decltype(rt)::value, decltype(alone)::value>),
+                           dim3((unsigned)(d.batch * p.groups), d.n_kv_heads, p.splits), dim3(decltype(alone)::value ? 64 : 256), 0, a.stream, w,
+                           a.block_table, (const char *)a.q, (const char *)a.k_pages, (const char *)a.v_pages, a.out, ml, o, p.splits,
+                           a.scale_log2, d.out_dtype);
     };
     auto with_rt = [&](auto tag, auto dim) {
+        auto with_form = [&](auto rt) {
+            if (p.alone) launch(tag, dim, rt, std::true_type{});
+            else launch(tag, dim, rt, std::false_type{});
+        };
         switch (p.rows_per_group / 16) {
-        case 1: launch(tag, dim, std::integral_constant<int, 1>{}); break;
-        case 2: launch(tag, dim, std::integral_constant<int, 2>{}); break;
-        case 3: launch(tag, dim, std::integral_constant<int, 3>{}); break;
-        default: launch(tag, dim, std::integral_constant<int, 4>{}); break;
+        case 1: with_form(std::integral_constant<int, 1>{}); break;
+        case 2: with_form(std::integral_constant<int, 2>{}); break;
+        case 3: with_form(std::integral_constant<int, 3>{}); break;
+        default: launch(tag, dim, std::integral_constant<int, 4>{}, std::false_type{}); break;
         }
     };
     auto with_dim = [&](auto tag) {

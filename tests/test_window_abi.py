@@ -24,6 +24,8 @@ def _bytes(dims, window=100, sinks=4):
     (dict(max_pages_per_req=(1 << 26) + 1, batch=1, total_q=1, max_spec_len=0), -6),            # more than 2^30 tokens in a row
     # units that do not fit the grid: 16384 requests of 8192 rows with 1024 kv heads
     (dict(batch=1 << 14, total_q=1 << 14, max_spec_len=8191, n_q_heads=1024, n_kv_heads=1024, max_pages_per_req=1), -6),
+    (dict(batch=1 << 20, total_q=1 << 20, max_spec_len=1023, n_q_heads=1, n_kv_heads=1, max_pages_per_req=1), -6),
+    (dict(n_q_heads=65536, n_kv_heads=65536), -6), (dict(n_q_heads=(1 << 16) + 2, n_kv_heads=2), -6),
 ])
 def test_bad_dims(kw, code):
     d = _attn_dims(**kw)
