@@ -664,7 +664,7 @@ def kv_remap(block_table, page_refs, sources, lens, new_lens, *, window: Optiona
 
     block_table [old_batch][max_pages], page_refs [num_pages], sources [batch], lens [old_batch], new_lens [batch], all int32.
     window, sinks: pages that no later row of verify_attn(window=, sinks=) sees are given back as well.  out_refs may be
-    page_refs; out_table must not overlap block_table."""
+    page_refs; out_table must not overlap block_table.  Results that are not given are new tensors, of one allocation."""
     if window is None and sinks != 0:
         raise ValueError("kv_remap(sinks=...) needs a window: without one every token is visible")
     if window is not None and window < 1:
@@ -699,7 +699,8 @@ def kv_compact_pages(block_table, page_refs, *, max_moves: Optional[int] = None,
                      copy_src=None, copy_dst=None, status=None, page_size: int = 16, workspace=None, stream=None):
     """adaspec_kv_compact_pages: used pages to the front of the pool; returns (out_table, out_refs, page_map [num_pages],
     copy_src [max_moves], copy_dst [max_moves], status [2]).  max_moves: half of the pool's pages unless given, which is always
-    enough.  out_table may be block_table, out_refs may be page_refs."""
+    enough.  out_table may be block_table, out_refs may be page_refs.  Results that are not given are new tensors, of one
+    allocation."""
     batch, max_pages = block_table.shape
     num_pages = page_refs.shape[0]
     max_moves = max(1, num_pages // 2) if max_moves is None else int(max_moves)

@@ -343,11 +343,53 @@ PyObject *verify_attn_window(PyObject *, PyObject *const *a, Py_ssize_t nargs)
     });
 }
 
-// an integer output: the caller's tensor of exactly this shape, or a new one
-struct Ints : Output {
-    Ints(PyObject *given, at::IntArrayRef shape, const at::Tensor &like) : Output(given, shape, at::kInt, like)
+// Integer outputs: the caller's tensors of exactly these shapes; the new ones share one allocation, from which each begins at
+// 256 bytes (an allocation of its own costs each of them 0.7 us, and these calls have five or six).
+template <int N> struct Ints {
+    struct Spec { PyObject *given; c10::SmallVector<int64_t, 2> shape; };
+    at::Tensor t[N];
+    PyObject *object[N] = {};
+    Ints(const at::Tensor &like, std::initializer_list<Spec> all)
     {
-        need(t.scalar_type() == at::kInt && t.is_contiguous() && t.sizes() == shape && device_index(t) == device_index(like));
+        int64_t total = 0, at_[N];
+        int i = 0;
+        for (const Spec &w : all) {
+            at_[i++] = total;
+            if (w.given == Py_None) total += (c10::multiply_integers(w.shape) + 63) / 64 * 64;
+        }
+        at::Tensor whole;
+        if (total > 0) whole = empty({total}, at::kInt, like);
+        i = 0;
+        for (const Spec &w : all) {
+            if (w.given != Py_None) {
+                t[i] = tensor(w.given);
+                need(t[i].scalar_type() == at::kInt && t[i].is_contiguous() && t[i].sizes() == at::IntArrayRef(w.shape) && device_index(t[i]) == device_index(like));
+            } else if (c10::multiply_integers(w.shape) == 0) {
+                t[i] = empty(w.shape, at::kInt, like);
+            } else {
+                t[i] = at::detail::make_tensor<at::TensorImpl>(c10::Storage(whole.storage()), whole.key_set(), whole.dtype());
+                t[i].unsafeGetTensorImpl()->set_storage_offset(at_[i]);
+                t[i].unsafeGetTensorImpl()->set_sizes_contiguous(w.shape);
+            }
+            ++i;
+        }
+        // their Python objects, before the call is made (see Output)
+        i = 0;
+        for (const Spec &w : all) {
+            object[i] = w.given != Py_None ? Py_NewRef(w.given) : THPVariable_Wrap(t[i]);
+            if (!object[i]) { drop(); failed_in_python(); }
+            ++i;
+        }
+    }
+    void drop() { for (PyObject *o : object) Py_XDECREF(o); }
+    ~Ints() { drop(); }
+    Ints(const Ints &) = delete;
+    int32_t *operator[](int i) const { return ptr<int32_t>(t[i]); }
+    PyObject *result() const
+    {
+        PyObject *r = PyTuple_New(N);
+        for (int i = 0; r && i < N; ++i) PyTuple_SET_ITEM(r, i, Py_NewRef(object[i]));
+        return r;
     }
 };
 
@@ -372,13 +414,12 @@ PyObject *kv_remap(PyObject *, PyObject *const *a, Py_ssize_t nargs)
         const size_t nbytes = api.remap_ws(&d);
         need(nbytes > 0);
         on_current_device({&bt, &refs, &src, &lens, &more});
-        const Ints table(a[8], {d.batch, d.max_pages_per_req}, bt), counts(a[9], {d.num_pages}, bt), cs(a[10], {d.batch}, bt), cd(a[11], {d.batch}, bt);
-        const Ints status(a[12], {2}, bt);
+        const Ints<5> out(bt, {{a[8], {d.batch, d.max_pages_per_req}}, {a[9], {d.num_pages}}, {a[10], {d.batch}}, {a[11], {d.batch}}, {a[12], {2}}});
         const at::Tensor ws = workspace(a[13], nbytes, kPages, bt);
         void *s = stream_of(a[14]);
         call("adaspec_kv_remap", api.remap, ptr<int32_t>(bt), ptr<int32_t>(refs), ptr<int32_t>(src), ptr<int32_t>(lens), ptr<int32_t>(more),
-             ptr<int32_t>(table.t), ptr<int32_t>(counts.t), ptr<int32_t>(cs.t), ptr<int32_t>(cd.t), ptr<int32_t>(status.t), &d, ptr(ws), (size_t)ws.numel(), s);
-        return Py_BuildValue("(NNNNN)", table.result(), counts.result(), cs.result(), cd.result(), status.result());
+             out[0], out[1], out[2], out[3], out[4], &d, ptr(ws), (size_t)ws.numel(), s);
+        return out.result();
     });
 }
 
@@ -398,13 +439,13 @@ PyObject *kv_compact_pages(PyObject *, PyObject *const *a, Py_ssize_t nargs)
         const size_t nbytes = api.compact_ws(&d);
         need(nbytes > 0);
         on_current_device({&bt, &refs});
-        const Ints table(a[4], bt.sizes(), bt), counts(a[5], {d.num_pages}, bt), map(a[6], {d.num_pages}, bt);
-        const Ints cs(a[7], {d.max_moves}, bt), cd(a[8], {d.max_moves}, bt), status(a[9], {2}, bt);
+        need(d.max_moves >= 0);
+        const Ints<6> out(bt, {{a[4], {d.old_batch, d.max_pages_per_req}}, {a[5], {d.num_pages}}, {a[6], {d.num_pages}},
+                               {a[7], {d.max_moves}}, {a[8], {d.max_moves}}, {a[9], {2}}});
         const at::Tensor ws = workspace(a[10], nbytes, kPages, bt);
         void *s = stream_of(a[11]);
-        call("adaspec_kv_compact_pages", api.compact, ptr<int32_t>(bt), ptr<int32_t>(refs), ptr<int32_t>(table.t), ptr<int32_t>(counts.t), ptr<int32_t>(map.t),
-             ptr<int32_t>(cs.t), ptr<int32_t>(cd.t), ptr<int32_t>(status.t), &d, ptr(ws), (size_t)ws.numel(), s);
-        return Py_BuildValue("(NNNNNN)", table.result(), counts.result(), map.result(), cs.result(), cd.result(), status.result());
+        call("adaspec_kv_compact_pages", api.compact, ptr<int32_t>(bt), ptr<int32_t>(refs), out[0], out[1], out[2], out[3], out[4], out[5], &d, ptr(ws), (size_t)ws.numel(), s);
+        return out.result();
     });
 }
 

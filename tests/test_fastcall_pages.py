@@ -75,6 +75,23 @@ def test_what_is_not_plain_is_left_to_python(module):  # noqa: F811
     assert stubs.calls == []
 
 
+def test_new_outputs_share_an_allocation_and_nothing_else(module):  # noqa: F811
+    Stubs(module, ENTRIES + MORE)
+    given = ints(9)
+    for shape in ((1, 2), (0, 2), (1, 0), (70, 3)):
+        table, lens = ints(*shape), ints(shape[0])
+        remap = module.kv_remap(table, ints(9), ints(3), lens, ints(3), 0, 0, 16, None, given, *[None] * 5)
+        compact = module.kv_compact_pages(table, given, 65, 16, None, None, None, None, None, None, None, None)
+        assert remap[1] is given
+        assert [tuple(t.shape) for t in remap] == [(3, shape[1]), (9,), (3,), (3,), (2,)]
+        assert [tuple(t.shape) for t in compact] == [shape, (9,), (9,), (65,), (65,), (2,)]
+        for out in (remap[:1] + remap[2:], compact):
+            spans = sorted((t.storage_offset(), t.storage_offset() + t.numel()) for t in out if t.numel())
+            assert all(a % 64 == 0 and t.is_contiguous() and t.dtype == torch.int32 for t in out for a in (t.storage_offset(),))
+            assert all(a[1] <= b[0] for a, b in zip(spans, spans[1:]))
+            assert spans[-1][1] * 4 <= out[-1].untyped_storage().nbytes()
+
+
 def test_entry_points_that_are_not_there(module):  # noqa: F811
     """A library without them: the older calls work, these are left to Python."""
     stubs = Stubs(module, ENTRIES)
