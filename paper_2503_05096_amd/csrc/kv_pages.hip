@@ -324,39 +324,51 @@ __global__ __launch_bounds__(kPagesThreads) void remap_assign_kernel(RemapArgs a
     }
     // (wants that no page is left for: their entries are -1 already, a shared page stays shared)
     if (before >= wants) return;
-    int f = before + block_scan(free[0] + free[1] + free[2] + free[3], s_sum, &here);
+    int f[kPerThread];
+    f[0] = before + block_scan(free[0] + free[1] + free[2] + free[3], s_sum, &here);
+#pragma unroll
+    for (int e = 1; e < kPerThread; ++e) f[e] = f[e - 1] + free[e - 1];
+    // The row, or the rows and then the row, whose wants f is among: the last one whose wants begin at or before it.  All four
+    // pages' look-ups step by step together.
+    bool takes[kPerThread], any = false;
+    int lo[kPerThread] = {}, nth[kPerThread];
+#pragma unroll
+    for (int e = 0; e < kPerThread; ++e) any |= takes[e] = free[e] && f[e] < wants;
+    if (!any) return;
+    const int size = kFew ? d.batch : a.tiles;
+    for (int step = 1 << (31 - __builtin_clz(size)); step > 0; step >>= 1) {
+#pragma unroll
+        for (int e = 0; e < kPerThread; ++e) {
+            const int at = min(lo[e] + step, size - 1);
+            lo[e] = s_first[at] <= f[e] ? at : lo[e];
+        }
+    }
+    int4 w[kPerThread];
 #pragma unroll
     for (int e = 0; e < kPerThread; ++e) {
-        if (!free[e] || f >= wants) continue;
-        const int p = p0 + e;
-        int lo = 0, hi = kFew ? d.batch : a.tiles;                  // the row, or the rows and then the row, whose wants f is among
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
-            if (s_first[mid] <= f) lo = mid;
-            else hi = mid;
-        }
-        int nth = f - s_first[lo];
-        ++f;
-        int4 w;
-        if constexpr (kFew) {
-            w = a.want[lo];
-        } else {
-            hi = min((lo + 1) * kPagesThreads, d.batch);
-            lo *= kPagesThreads;
-            while (hi - lo > 1) {
-                const int mid = (lo + hi) >> 1;
-                if (a.want[mid].x <= nth) lo = mid;
+        nth[e] = f[e] - s_first[lo[e]];
+        if constexpr (!kFew) {
+            int hi = min((lo[e] + 1) * kPagesThreads, d.batch);
+            lo[e] *= kPagesThreads;
+            while (takes[e] && hi - lo[e] > 1) {
+                const int mid = (lo[e] + hi) >> 1;
+                if (a.want[mid].x <= nth[e]) lo[e] = mid;
                 else hi = mid;
             }
-            w = a.want[lo];
-            nth -= w.x;
         }
+        w[e] = a.want[lo[e]];
+        if constexpr (!kFew) nth[e] -= w[e].x;
+    }
+#pragma unroll
+    for (int e = 0; e < kPerThread; ++e) {
+        if (!takes[e]) continue;
+        const int p = p0 + e;
         a.out_refs[p] = 1;
-        a.out_table[(int64_t)lo * d.max_pages_per_req + w.y + nth] = p;
-        if (w.z >= 0 && nth == 0) {
-            atomicAdd(a.out_refs + w.z, -1);
-            a.copy_src[lo] = w.z;
-            a.copy_dst[lo] = p;
+        a.out_table[(int64_t)lo[e] * d.max_pages_per_req + w[e].y + nth[e]] = p;
+        if (w[e].z >= 0 && nth[e] == 0) {
+            atomicAdd(a.out_refs + w[e].z, -1);
+            a.copy_src[lo[e]] = w[e].z;
+            a.copy_dst[lo[e]] = p;
         }
     }
 }
@@ -438,6 +450,23 @@ __global__ __launch_bounds__(kPagesThreads) void compact_write_kernel(CompactArg
     __shared__ int s_sum[kPagesThreads / kWave];
     const adaspec_pages_dims &d = a.dims;
     const int tid = threadIdx.x, grains = a.chunks * (kChunk / kGrain);
+    // the workgroup's counts, or its first entries of the table: under way while the bases are worked out
+    const bool on_counts = (int)blockIdx.x < a.chunks;
+    const int64_t entries = (int64_t)d.old_batch * d.max_pages_per_req;
+    int got[kPerThread];
+    auto table_entries = [&](int64_t e0) {
+#pragma unroll
+        for (int k = 0; k < kPerThread; ++k) got[k] = e0 + k * kPagesThreads + tid < entries ? a.block_table[e0 + k * kPagesThreads + tid] : -1;
+    };
+    if (on_counts) {
+#pragma unroll
+        for (int k = 0; k < kPerThread; ++k) {
+            const int p = blockIdx.x * kChunk + k * kPagesThreads + tid;
+            got[k] = p < d.num_pages ? a.page_refs[p] : 0;
+        }
+    } else {
+        table_entries((int64_t)(blockIdx.x - a.chunks) * kChunk);
+    }
     if constexpr (kSelf) {
         constexpr int kMost = kSelfPages / kChunk;
         int4 r[kMost];
@@ -562,13 +591,13 @@ __global__ __launch_bounds__(kPagesThreads) void compact_write_kernel(CompactArg
         return (((uint32_t)w.x >> (p & 31)) & 1u) && m < d.max_moves ? m : -1;
     };
     // (what has to be looked up is, for all four, before anything is written: the loads are under way together)
-    if ((int)blockIdx.x < a.chunks) {
-        int move[kPerThread], to[kPerThread] = {}, refs[kPerThread];
+    if (on_counts) {
+        int move[kPerThread], to[kPerThread] = {};
+        const int (&refs)[kPerThread] = got;
         bool hole[kPerThread];
 #pragma unroll
         for (int k = 0; k < kPerThread; ++k) {
             const int p = blockIdx.x * kChunk + k * kPagesThreads + tid;
-            refs[k] = p < d.num_pages ? a.page_refs[p] : 0;
             move[k] = move_of(p);
             hole[k] = false;
             if (p < N) {
@@ -600,17 +629,19 @@ __global__ __launch_bounds__(kPagesThreads) void compact_write_kernel(CompactArg
         }
         return;
     }
-    const int64_t n = (int64_t)d.old_batch * d.max_pages_per_req;
-    for (int64_t e0 = (int64_t)(blockIdx.x - a.chunks) * kChunk; e0 < n; e0 += (int64_t)a.table_groups * kChunk) {
+    const int64_t step = (int64_t)a.table_groups * kChunk;
+    for (int64_t e0 = (int64_t)(blockIdx.x - a.chunks) * kChunk; e0 < entries; e0 += step) {
         int p[kPerThread], move[kPerThread];
 #pragma unroll
-        for (int k = 0; k < kPerThread; ++k) p[k] = e0 + k * kPagesThreads + tid < n ? a.block_table[e0 + k * kPagesThreads + tid] : -1;
-#pragma unroll
-        for (int k = 0; k < kPerThread; ++k) move[k] = move_of(p[k]);
+        for (int k = 0; k < kPerThread; ++k) {
+            p[k] = got[k];
+            move[k] = move_of(p[k]);
+        }
+        table_entries(e0 + step);
         free_pages(move, p);
 #pragma unroll
         for (int k = 0; k < kPerThread; ++k)
-            if (e0 + k * kPagesThreads + tid < n) a.out_table[e0 + k * kPagesThreads + tid] = p[k];
+            if (e0 + k * kPagesThreads + tid < entries) a.out_table[e0 + k * kPagesThreads + tid] = p[k];
     }
 }
 
