@@ -1,27 +1,64 @@
-// Windowed verification attention: the plan of a call, the merge of a unit's parts, and the portable form: any of the three storage types, any head_dim that is a multiple of 8 up
-// to 256.  One wavefront per (request, kv head, chunk of 8 query rows).
+// Windowed verification attention: the plan of a call, the merge of a unit's parts, and the portable form: any of the three
+// storage types, any head_dim that is a multiple of 8 up to 256.  A workgroup of four wavefronts per (request, kv head, chunk of
+// 8 query rows); wavefront w takes the 64 tokens w, w + 4, ... of the unit's list of pages.
 //
-// Per 64 tokens: lane <-> token for the scores (each lane walks its key row, the query rows are broadcast from LDS),
-// wavefront reductions for the online softmax, then lane <-> channel for P.V.  A token that a row does not see has a weight
-// below zero in LDS and is left out of that row's sum, not multiplied by zero: whatever it holds cannot reach the row.
+// Per 64 tokens: lane <-> token for the scores (each lane walks its key row in pieces of 8 channels, the query rows are broadcast
+// from LDS), wavefront reductions for the online softmax, then lane <-> two channels side by side for P.V, 16 value rows (8 above 128
+// channels) under way at a time.  In pages that some row does not see whole, a token that a row does not see has a weight below zero in LDS
+// and is left out of that row's sum, not multiplied by zero: whatever it holds cannot reach the row.
+//
+// Its vector units bound it: 16 multiply-adds per value of K and of V that arrives, twice as many instructions with unpacking
+// and LDS.  Window 1024, 32 requests of 16 rows at 8 kv heads: 72 us for 102 MB (bf16, head_dim 96; one wavefront per unit, a
+// value row at a time: 1125), 150 us for 273 MB (head_dim 256; 2236), 83 us for 204 MB (fp32, 96; 855).
 #include <type_traits>
 
 #include "attn_window.h"
 
 namespace adaspec {
 
-constexpr int kWinRows = 8;
-constexpr int kWinMaxD = 256;
+constexpr int kWinRows = 8, kWinWaves = 4;
 constexpr int kWindowMaxSplits = 64;        // a lane of the combine kernel each
 
-template <class T>
-__global__ __launch_bounds__(64) void attn_window_vector_kernel(WindowDims dims, const void *__restrict__ q,
-                                                                const void *__restrict__ k_pages, const void *__restrict__ v_pages,
-                                                                void *__restrict__ out, int d, float scale_log2, int out_dtype)
+// 8 values side by side, from a multiple of 8 on
+template <class T> __device__ __forceinline__ void load8(const void *base, int64_t at, float (&v)[8])
 {
-    __shared__ float qs[kWinRows][kWinMaxD];
-    __shared__ float ps[kWinRows][64];
-    const int lane = threadIdx.x;
+    if constexpr (sizeof(typename T::storage) == 4) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const float4 x = reinterpret_cast<const float4 *>(base)[at / 4 + h];
+            v[4 * h] = x.x; v[4 * h + 1] = x.y; v[4 * h + 2] = x.z; v[4 * h + 3] = x.w;
+        }
+    } else {
+        const uint4 x = reinterpret_cast<const uint4 *>(base)[at / 8];
+        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            v[2 * e] = load_as_float<T>(&w[e], 0);
+            v[2 * e + 1] = load_as_float<T>(&w[e], 1);
+        }
+    }
+}
+template <class T> struct Pair { typedef uint32_t type; };
+template <> struct Pair<F32> { typedef float2 type; };
+template <class T> __device__ __forceinline__ float2 pair_values(typename Pair<T>::type x)
+{
+    return make_float2(load_as_float<T>(&x, 0), load_as_float<T>(&x, 1));
+}
+
+template <class T, int kP>                  // kP: pairs of channels that a lane has, head_dim at most 128 kP
+__global__ __launch_bounds__(64 * kWinWaves, kP == 1 ? 4 : 3) void attn_window_vector_kernel(WindowDims dims, const void *__restrict__ q,
+                                                                            const void *__restrict__ k_pages,
+                                                                            const void *__restrict__ v_pages, void *__restrict__ out, int d,
+                                                                            float scale_log2, int out_dtype)
+{
+    constexpr int kD = 128 * kP, kAhead = 16 / kP;                  // value rows under way
+    typedef typename Pair<T>::type pair;
+    // Q rows and weights of every wavefront; then its state.  (12 or 16 KB; 16 or 32)
+    __shared__ __attribute__((aligned(16))) float smem[kWinWaves * kWinRows * kD];
+    static_assert(kWinRows * kD + kWinWaves * 64 * kWinRows <= kWinWaves * kWinRows * kD, "Q and weights fit where the states go");
+    __shared__ float s_m[kWinWaves][kWinRows], s_l[kWinWaves][kWinRows];
+    const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+    float *qs = smem, *ps = smem + kWinRows * kD + wv * 64 * kWinRows;      // [row][channel]; [token][row]
     const int G = dims.Hq / dims.Hkv;
     const int gkv = blockIdx.y, i = blockIdx.x / dims.groups;
     const RowsBefore before(dims, i, lane);
@@ -30,91 +67,140 @@ __global__ __launch_bounds__(64) void attn_window_vector_kernel(WindowDims dims,
     u.qrow0 = before.sum(dims, i, lane);
     if (u.qrow0 + u.n > dims.total_q) return;                       // inconsistent lengths
 
-    for (int idx = lane; idx < kWinRows * d; idx += 64) {
-        const int r = u.r0 + idx / d, c = idx % d;
-        qs[idx / d][c] = r < u.rows ? load_as_float<T>(q, ((u.qrow0 + r / G) * dims.Hq + gkv * G + r % G) * d + c) : 0.f;
+    for (int idx = tid; idx < kWinRows * (d / 8); idx += 64 * kWinWaves) {
+        const int r = idx / (d / 8), row = min(u.r0 + r, u.rows - 1), c = 8 * (idx % (d / 8));
+        float v[8];
+        load8<T>(q, ((u.qrow0 + row / G) * dims.Hq + gkv * G + row % G) * d + c, v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) qs[r * kD + c + e] = v[e];
     }
     __syncthreads();
 
-    float m[kWinRows], l[kWinRows], acc[kWinRows][4];
+    int pos[kWinRows];
+#pragma unroll
+    for (int r = 0; r < kWinRows; ++r) pos[r] = u.r0 + r < u.rows ? u.first_pos + (u.r0 + r) / G : -1;
+    const int oldest = u.first_pos + u.r0 / G, newest = u.first_pos + (min(u.r0 + kWinRows, u.rows) - 1) / G;
+    float m[kWinRows], l[kWinRows], acc[kWinRows][2 * kP];          // l: this lane's tokens only
 #pragma unroll
     for (int r = 0; r < kWinRows; ++r) {
         m[r] = -INFINITY; l[r] = 0.f;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) acc[r][e] = 0.f;
+        for (int e = 0; e < 2 * kP; ++e) acc[r][e] = 0.f;
     }
-    for (int v0 = 0; v0 < u.pages; v0 += 4) {
-        const int v = v0 + (lane >> 4);
-        const int pg = u.page_of(min(v, u.pages - 1)), t = pg * 16 + (lane & 15);
-        const bool valid = v < u.pages && t < u.L;
+    for (int v0 = 4 * wv; v0 < u.pages; v0 += 4 * kWinWaves) {
+        const int v = v0 + (lane >> 4), pg = u.page_of(min(v, u.pages - 1)), t = pg * 16 + (lane & 15);
+        const bool there = v < u.pages;
+        const int page = dims.block_table[u.bt_off + pg];
+        const int64_t koff = (((int64_t)page * dims.Hkv + gkv) * 16 + (lane & 15)) * d;
         float sc[kWinRows];
 #pragma unroll
         for (int r = 0; r < kWinRows; ++r) sc[r] = 0.f;
-        if (valid) {
-            const int64_t page = dims.block_table[u.bt_off + pg];
-            const int64_t koff = ((page * dims.Hkv + gkv) * 16 + (lane & 15)) * (int64_t)d;
-            for (int c = 0; c < d; c += 8) {
-                float kv[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) kv[e] = load_as_float<T>(k_pages, koff + c + e);
-#pragma unroll
-                for (int r = 0; r < kWinRows; ++r)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) sc[r] = fmaf(qs[r][c + e], kv[e], sc[r]);
-            }
-        }
-        __syncthreads();                                            // the last 64 tokens' weights have been read
-#pragma unroll
-        for (int r = 0; r < kWinRows; ++r) {
-            const int row = u.r0 + r;
-            const bool vis = valid && row < u.rows && window_sees(u, u.first_pos + row / G, t);
-            const float sv = vis ? sc[r] * scale_log2 : -INFINITY;
-            const float mn = fmaxf(m[r], wave_max(sv));
-            float p = 0.f, alpha = 1.f;
-            if (mn > -INFINITY) {
-                alpha = __builtin_amdgcn_exp2f(m[r] - mn);
-                p = vis ? __builtin_amdgcn_exp2f(sv - mn) : 0.f;
-            } else if (vis) {
-                p = sv == sv ? 0.f : sv;                            // (every score so far is -inf or NaN)
-            }
-            l[r] = l[r] * alpha + wave_sum(p);
-            m[r] = mn;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) acc[r][e] *= alpha;
-            ps[r][lane] = vis ? p : -1.f;
-        }
-        __syncthreads();
-        const int most = min(4, u.pages - v0) * 16;
-        for (int tt = 0; tt < most; ++tt) {
-            const int pv = u.page_of(v0 + (tt >> 4));
-            if (pv * 16 + (tt & 15) >= u.L) break;                  // (the last page of the list is the newest)
-            const int64_t page = dims.block_table[u.bt_off + pv];
-            const int64_t voff = ((page * dims.Hkv + gkv) * 16 + (tt & 15)) * (int64_t)d;
-            float vv[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int c = lane + 64 * e;
-                vv[e] = c < d ? load_as_float<T>(v_pages, voff + c) : 0.f;
-            }
+#pragma unroll 4
+        for (int c = 0; c < d; c += 8) {
+            float kv[8];
+            load8<T>(k_pages, koff + c, kv);
 #pragma unroll
             for (int r = 0; r < kWinRows; ++r) {
-                const float p = ps[r][tt];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) acc[r][e] = p < 0.f ? acc[r][e] : fmaf(p, vv[e], acc[r][e]);
+                const float4 a = *reinterpret_cast<const float4 *>(qs + r * kD + c), b = *reinterpret_cast<const float4 *>(qs + r * kD + c + 4);
+                sc[r] = fmaf(a.x, kv[0], sc[r]); sc[r] = fmaf(a.y, kv[1], sc[r]); sc[r] = fmaf(a.z, kv[2], sc[r]); sc[r] = fmaf(a.w, kv[3], sc[r]);
+                sc[r] = fmaf(b.x, kv[4], sc[r]); sc[r] = fmaf(b.y, kv[5], sc[r]); sc[r] = fmaf(b.z, kv[6], sc[r]); sc[r] = fmaf(b.w, kv[7], sc[r]);
             }
         }
+        float p[kWinRows];
+#pragma unroll
+        for (int r = 0; r < kWinRows; ++r) {
+            const bool vis = there && window_sees(u, pos[r], t);
+            const float sv = vis ? sc[r] * scale_log2 : -INFINITY;
+            const float mn = fmaxf(m[r], wave_max(sv));
+            float alpha = 1.f;
+            p[r] = 0.f;
+            if (mn > -INFINITY) {
+                alpha = __builtin_amdgcn_exp2f(m[r] - mn);
+                p[r] = vis ? __builtin_amdgcn_exp2f(sv - mn) : 0.f;
+            } else if (vis) {
+                p[r] = sv == sv ? 0.f : sv;                         // (every score so far is -inf or NaN)
+            }
+            l[r] = l[r] * alpha + p[r];
+            m[r] = mn;
+#pragma unroll
+            for (int e = 0; e < 2 * kP; ++e) acc[r][e] *= alpha;
+            if (!vis) p[r] = -1.f;
+        }
+        // (the wavefront's own part of LDS, whose accesses keep their order)
+        *reinterpret_cast<float4 *>(ps + lane * kWinRows) = make_float4(p[0], p[1], p[2], p[3]);
+        *reinterpret_cast<float4 *>(ps + lane * kWinRows + 4) = make_float4(p[4], p[5], p[6], p[7]);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        for (int j = 0; j < 4 && v0 + j < u.pages; ++j) {
+            const int tb = u.page_of(v0 + j) * 16;
+            const int64_t voff = ((int64_t)__builtin_amdgcn_readlane(page, 16 * j) * dims.Hkv + gkv) * 16 * d;
+            const bool whole = tb + 15 <= oldest && (newest - tb < u.window || tb + 15 < u.sinks);
+            pair x[kAhead][kP];
+            auto request = [&](int t0) {
+#pragma unroll
+                for (int tt = 0; tt < kAhead; ++tt)
+#pragma unroll
+                    for (int k = 0; k < kP; ++k) {
+                        const int c = min(2 * lane + 128 * k, d - 2);       // (lanes behind the last channel repeat it)
+                        x[tt][k] = *reinterpret_cast<const pair *>(reinterpret_cast<const typename T::storage *>(v_pages) + voff + (t0 + tt) * d + c);
+                    }
+            };
+            auto add = [&](int t0, auto all) {                      // all: every row sees every token of the page
+#pragma unroll
+                for (int tt = 0; tt < kAhead; ++tt) {
+                    const float *at = ps + (16 * j + t0 + tt) * kWinRows;
+                    const float4 a = *reinterpret_cast<const float4 *>(at), b = *reinterpret_cast<const float4 *>(at + 4);
+                    const float w[kWinRows] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+                    for (int k = 0; k < kP; ++k) {
+                        const float2 val = pair_values<T>(x[tt][k]);
+#pragma unroll
+                        for (int r = 0; r < kWinRows; ++r) {
+                            const float y0 = fmaf(w[r], val.x, acc[r][2 * k]), y1 = fmaf(w[r], val.y, acc[r][2 * k + 1]);
+                            const bool in = decltype(all)::value || !(w[r] < 0.f);
+                            acc[r][2 * k] = in ? y0 : acc[r][2 * k];
+                            acc[r][2 * k + 1] = in ? y1 : acc[r][2 * k + 1];
+                        }
+                    }
+                }
+            };
+            for (int t0 = 0; t0 < 16; t0 += kAhead) {
+                request(t0);
+                if (whole) add(t0, std::true_type{});
+                else add(t0, std::false_type{});
+            }
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
     }
+    // O = sum_w 2^(m_w - m*) O_w, m* = max over wavefronts
+    __syncthreads();
 #pragma unroll
     for (int r = 0; r < kWinRows; ++r) {
-        const int row = u.r0 + r;
-        if (row >= u.rows) continue;
-        const float inv = 1.0f / l[r];
-        const int64_t obase = ((u.qrow0 + row / G) * dims.Hq + gkv * G + row % G) * (int64_t)d;
+        const float all = wave_sum(l[r]);
+        if (lane == 0) { s_m[wv][r] = m[r]; s_l[wv][r] = all; }
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int c = lane + 64 * e;
-            if (c < d) store_out(out, obase + c, acc[r][e] * inv, out_dtype);
-        }
+        for (int k = 0; k < kP; ++k)
+            *reinterpret_cast<float2 *>(smem + (wv * kWinRows + r) * kD + 2 * lane + 128 * k) = make_float2(acc[r][2 * k], acc[r][2 * k + 1]);
+    }
+    __syncthreads();
+    const int r = tid / 32, row = u.r0 + r;
+    if (row >= u.rows) return;
+    float ms = s_m[0][r], ltot = 0.f, sc[kWinWaves];
+#pragma unroll
+    for (int w = 1; w < kWinWaves; ++w) ms = fmaxf(ms, s_m[w][r]);
+#pragma unroll
+    for (int w = 0; w < kWinWaves; ++w) {
+        sc[w] = ms > -INFINITY ? __builtin_amdgcn_exp2f(s_m[w][r] - ms) : 1.f;
+        ltot += sc[w] * s_l[w][r];
+    }
+    const float inv = 1.0f / ltot;
+    const int64_t obase = ((u.qrow0 + row / G) * dims.Hq + gkv * G + row % G) * (int64_t)d;
+    for (int c = tid & 31; c < d; c += 32) {
+        float o = 0.f;
+#pragma unroll
+        for (int w = 0; w < kWinWaves; ++w) o += sc[w] * smem[(w * kWinRows + r) * kD + c];
+        store_out(out, obase + c, o * inv, out_dtype);
     }
 }
 
@@ -240,13 +326,17 @@ hipError_t launch_attn_window(const WindowArgs &a)
         else combine(std::integral_constant<int, 64>{});
         return hipGetLastError();
     }
-    auto launch = [&](auto tag) {
-        hipLaunchKernelGGL(attn_window_vector_kernel<decltype(tag)>, dim3((unsigned)(d.batch * a.plan.groups), d.n_kv_heads), dim3(64), 0, a.stream, w, a.q,
-                           a.k_pages, a.v_pages, a.out, d.head_dim, a.scale_log2, d.out_dtype);
+    auto launch = [&](auto tag, auto pairs) {
+        hipLaunchKernelGGL((attn_window_vector_kernel<decltype(tag), decltype(pairs)::value>), dim3((unsigned)(d.batch * a.plan.groups), d.n_kv_heads),
+                           dim3(64 * kWinWaves), 0, a.stream, w, a.q, a.k_pages, a.v_pages, a.out, d.head_dim, a.scale_log2, d.out_dtype);
     };
-    if (d.dtype == ADASPEC_F32) launch(F32{});
-    else if (d.dtype == ADASPEC_F16) launch(F16{});
-    else launch(BF16{});
+    auto with_pairs = [&](auto tag) {
+        if (d.head_dim <= 128) launch(tag, std::integral_constant<int, 1>{});
+        else launch(tag, std::integral_constant<int, 2>{});
+    };
+    if (d.dtype == ADASPEC_F32) with_pairs(F32{});
+    else if (d.dtype == ADASPEC_F16) with_pairs(F16{});
+    else with_pairs(BF16{});
     return hipGetLastError();
 }
 

@@ -63,6 +63,15 @@ see; rows that see neither are off by the rounding that test_gpu_attn_window.py 
     assert np.abs(out[~sees] - clean[~sees]).max() <= tol
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("d", [24, 128, 136, 248])
+def test_portable_form_over_several_turns(d, dtype, pkg):  # noqa: F811
+    """Lists of pages that end anywhere in a wavefront's turns, of up to three of them; one row in a unit, and eight."""
+    for window, sinks in ((700, 40), (1000, 0), (3, 17)):
+        st = step(1500 + d, [1, 63, 64, 65, 257, 900, 700, 513], [0, 1, 0, 2, 3, 6, 0, 5], 6, 2, d, dtype)
+        check(pkg, poisoned(st, window, sinks), window, sinks, paths=("vector",))
+
+
 def test_two_calls_at_once_and_rows_behind_the_last_request(pkg):  # noqa: F811
     """Two streams, a workspace each; outputs with rows behind the last request's, which stay as they were."""
     import torch
