@@ -64,6 +64,16 @@ __device__ __forceinline__ bool window_unit(WindowUnit &u, const WindowDims &d, 
     return u.r0 < u.rows;
 }
 
+// Request and row group of workgroup x of batch * groups.  Workgroups go round the eight XCDs in turn: the groups of a request,
+// which read the same K and V, are eight apart, so that they run on one XCD at about the same time and share its L2.
+__device__ __forceinline__ void window_place(const WindowDims &d, int x, int &i, int &rg)
+{
+    if (d.groups == 1) { i = x; rg = 0; return; }
+    const int first = x / (8 * d.groups) * 8, rest = x - first * d.groups, n = min(8, d.batch - first);
+    rg = rest / n;
+    i = first + rest - rg * n;
+}
+
 // whether the row at position `pos` sees token t
 __device__ __forceinline__ bool window_sees(const WindowUnit &u, int pos, int t)
 {

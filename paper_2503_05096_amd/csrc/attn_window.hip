@@ -60,10 +60,12 @@ __global__ __launch_bounds__(64 * kWinWaves, kP == 1 ? 4 : 3) void attn_window_v
     const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
     float *qs = smem, *ps = smem + kWinRows * kD + wv * 64 * kWinRows;      // [row][channel]; [token][row]
     const int G = dims.Hq / dims.Hkv;
-    const int gkv = blockIdx.y, i = blockIdx.x / dims.groups;
+    const int gkv = blockIdx.y;
+    int i, rg;
+    window_place(dims, blockIdx.x, i, rg);
     const RowsBefore before(dims, i, lane);
     WindowUnit u;
-    if (!window_unit(u, dims, i, blockIdx.x % dims.groups, gkv)) return;
+    if (!window_unit(u, dims, i, rg, gkv)) return;
     u.qrow0 = before.sum(dims, i, lane);
     if (u.qrow0 + u.n > dims.total_q) return;                       // inconsistent lengths
 
@@ -214,7 +216,9 @@ __global__ __launch_bounds__(256) void attn_window_combine_kernel(WindowDims dim
 {
     constexpr int kE = D / 64, kAhead = 16;
     const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int i = blockIdx.x / dims.groups, rl = 4 * blockIdx.z + wv;
+    const int rl = 4 * blockIdx.z + wv;
+    int i, rg;
+    window_place(dims, blockIdx.x, i, rg);
     const RowsBefore before(dims, i, lane);
     const int64_t first = ((int64_t)blockIdx.x * dims.Hkv + blockIdx.y) * splits * dims.rows_per_group + rl;
     float2 ml = make_float2(-INFINITY, 0.f);
@@ -226,7 +230,7 @@ __global__ __launch_bounds__(256) void attn_window_combine_kernel(WindowDims dim
 #pragma unroll
         for (int e = 0; e < kE; ++e) x[s][e] = s < splits ? o[(int64_t)s * dims.rows_per_group * D + e] : 0.f;
     WindowUnit u;
-    if (!window_unit(u, dims, i, blockIdx.x % dims.groups, blockIdx.y)) return;
+    if (!window_unit(u, dims, i, rg, blockIdx.y)) return;
     const int row = u.r0 + rl;
     const int all_blocks = (u.pages + block_pages - 1) / block_pages, per = (all_blocks + splits - 1) / splits;
     const int ns = per > 0 ? (all_blocks + per - 1) / per : 1;      // (at most kWindowMaxSplits)
@@ -267,7 +271,9 @@ WindowPlan make_window_plan(const adaspec_attn_dims &d, int window, int sinks)
     const int G = d.n_q_heads / d.n_kv_heads;
     const int64_t rows = (int64_t)(d.max_spec_len + 1) * G;
     p.kind = d.path != ADASPEC_PATH_VECTOR && window_fast_supported(d) ? WindowKind::kMfma : WindowKind::kVector;
-    p.rows_per_group = p.kind == WindowKind::kVector ? kWinRows : 16 * (int)(rows < 64 ? (rows + 15) / 16 : 4);
+    // as few groups of up to 64 rows as there can be, of equal numbers of 16-row tiles
+    const int64_t tiles = (rows + 15) / 16, least = (tiles + 3) / 4;
+    p.rows_per_group = p.kind == WindowKind::kVector ? kWinRows : 16 * (int)((tiles + least - 1) / least);
     p.groups = (int)((rows + p.rows_per_group - 1) / p.rows_per_group);
     p.units = (int64_t)d.batch * d.n_kv_heads * p.groups;
     p.splits = 1;

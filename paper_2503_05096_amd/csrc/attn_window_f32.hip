@@ -28,10 +28,12 @@ __global__ __launch_bounds__(256, (RT <= 2 ? 2 : 1)) void attn_window_f32_kernel
     const int g = lane >> 4, n16 = lane & 15;
     const int G = dims.Hq / dims.Hkv;
 
-    const int sp = blockIdx.z, i = blockIdx.x / dims.groups;
+    const int sp = blockIdx.z;
+    int i, rg;
+    window_place(dims, blockIdx.x, i, rg);
     const RowsBefore before(dims, i, lane);
     WindowUnit u;
-    if (!window_unit(u, dims, i, blockIdx.x % dims.groups, blockIdx.y)) return;
+    if (!window_unit(u, dims, i, rg, blockIdx.y)) return;
     const int per = (u.pages + splits - 1) / splits, ns = per > 0 ? (u.pages + per - 1) / per : 1;
     const int b0 = sp * per, b1 = min(u.pages, b0 + per);
     if (sp >= ns) return;

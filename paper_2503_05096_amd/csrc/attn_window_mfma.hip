@@ -74,10 +74,12 @@ __global__ __launch_bounds__(kAlone ? 64 : 256, kAlone ? (RT == 1 ? 4 : RT == 2 
     const int g = lane >> 4, n16 = lane & 15;
     const int G = dims.Hq / dims.Hkv;
 
-    const int sp = blockIdx.z, i = blockIdx.x / dims.groups;
+    const int sp = blockIdx.z;
+    int i, rg;
+    window_place(dims, blockIdx.x, i, rg);
     const RowsBefore before(dims, i, lane);
     WindowUnit u;
-    if (!window_unit(u, dims, i, blockIdx.x % dims.groups, blockIdx.y)) return;
+    if (!window_unit(u, dims, i, rg, blockIdx.y)) return;
     const int all_blocks = (u.pages + kPages - 1) / kPages, per = (all_blocks + splits - 1) / splits;
     const int ns = per > 0 ? (all_blocks + per - 1) / per : 1;
     const int b0 = sp * per, b1 = min(all_blocks, b0 + per);
