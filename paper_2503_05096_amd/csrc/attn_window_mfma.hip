@@ -56,7 +56,17 @@ __device__ __forceinline__ void load_lds_2(const v4i32 &rsrc, uint32_t off0, uin
                  :: "s"(lds), "v"(off0), "v"(off1), "s"(rsrc) : "memory", "m0");
 }
 
-template <class T, int D, int RT, bool kAlone>
+// a page of 4 KB that another row group reads at about the same time: it may stay in the L2
+__device__ __forceinline__ void load_shared_page(const v4i32 &rsrc, uint32_t off0, uint32_t off1, uint32_t off2, uint32_t off3, uint32_t lds)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %5, 0 offen lds\n\t"
+                 "buffer_load_dwordx4 %2, %5, 0 offen offset:1024 lds\n\t"
+                 "buffer_load_dwordx4 %3, %5, 0 offen offset:2048 lds\n\t"
+                 "buffer_load_dwordx4 %4, %5, 0 offen offset:3072 lds"
+                 :: "s"(lds), "v"(off0), "v"(off1), "v"(off2), "v"(off3), "s"(rsrc) : "memory", "m0");
+}
+
+template <class T, int D, int RT, bool kAlone, bool kShared>
 __global__ __launch_bounds__(kAlone ? 64 : 256, kAlone ? (RT == 1 ? 4 : RT == 2 && D == 64 ? 3 : 2) : 2) void attn_window_kernel(WindowDims dims, const int32_t *__restrict__ block_table,
                                                              const char *__restrict__ q, const char *__restrict__ k_pages, const char *__restrict__ v_pages,
                                                              void *__restrict__ out, float *__restrict__ part_ml,
@@ -131,7 +141,8 @@ __global__ __launch_bounds__(kAlone ? 64 : 256, kAlone ? (RT == 1 ? 4 : RT == 2 
 #pragma unroll
         for (int j = 0; j < kPages; ++j) {
             const v4i32 rs = buffer_rsrc(pages + base[j], kPageBytes);
-            if constexpr (D == 128) load_page_to_lds(rs, voff[0], voff[1], voff[2], voff[3], lds + j * kPageBytes);
+            if constexpr (kShared) load_shared_page(rs, voff[0], voff[1], voff[2], voff[3], lds + j * kPageBytes);
+            else if constexpr (D == 128) load_page_to_lds(rs, voff[0], voff[1], voff[2], voff[3], lds + j * kPageBytes);
             else load_lds_2(rs, voff[0], voff[1], lds + j * kPageBytes);
         }
     };
@@ -379,22 +390,31 @@ hipError_t launch_attn_window_mfma(const WindowArgs &a, const WindowDims &w)
     const adaspec_attn_dims &d = a.dims;
     const WindowPlan &p = a.plan;
     float *ml = reinterpret_cast<float *>(a.ws + p.off_part_ml), *o = reinterpret_cast<float *>(a.ws + p.off_part_o);
-    auto launch = [&](auto tag, auto dim, auto rt, auto alone) {
-        hipLaunchKernelGGL((attn_window_kernel<decltype(tag), decltype(dim)::value, decltype(rt)::value, decltype(alone)::value>),
+    auto launch = [&](auto tag, auto dim, auto rt, auto alone, auto shared) {
+        hipLaunchKernelGGL((attn_window_kernel<decltype(tag), decltype(dim)::value, decltype(rt)::value, decltype(alone)::value, decltype(shared)::value>),
                            dim3((unsigned)(d.batch * p.groups), d.n_kv_heads, p.splits), dim3(decltype(alone)::value ? 64 : 256), 0, a.stream, w,
                            a.block_table, (const char *)a.q, (const char *)a.k_pages, (const char *)a.v_pages, a.out, ml, o, p.splits,
                            a.scale_log2, d.out_dtype);
     };
+    // Two row groups read the same pages: loads that leave them in the L2 (128 requests of 72 rows at 8 kv heads, head_dim 128,
+    // window 1024: 138 us, streaming loads 160; window 4096, 64 requests: 223 and 282).  Head_dim 64 gains nothing (93 us either
+    // way), and one group alone loses by them (32 rows, window 1024: 102 us instead of 91).
     auto with_rt = [&](auto tag, auto dim) {
+        constexpr bool kMay = decltype(dim)::value == 128;
         auto with_form = [&](auto rt) {
-            if (p.alone) launch(tag, dim, rt, std::true_type{});
-            else launch(tag, dim, rt, std::false_type{});
+            if constexpr (decltype(rt)::value < 4) {
+                if (p.alone) { launch(tag, dim, rt, std::true_type{}, std::false_type{}); return; }
+            }
+            if constexpr (kMay && decltype(rt)::value > 2) {        // (more than one group: of three or four tiles)
+                if (p.groups > 1) { launch(tag, dim, rt, std::false_type{}, std::true_type{}); return; }
+            }
+            launch(tag, dim, rt, std::false_type{}, std::false_type{});
         };
         switch (p.rows_per_group / 16) {
         case 1: with_form(std::integral_constant<int, 1>{}); break;
         case 2: with_form(std::integral_constant<int, 2>{}); break;
         case 3: with_form(std::integral_constant<int, 3>{}); break;
-        default: launch(tag, dim, std::integral_constant<int, 4>{}, std::false_type{}); break;
+        default: with_form(std::integral_constant<int, 4>{}); break;
         }
     };
     auto with_dim = [&](auto tag) {
