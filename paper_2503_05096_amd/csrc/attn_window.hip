@@ -269,22 +269,27 @@ WindowPlan make_window_plan(const adaspec_attn_dims &d, int window, int sinks)
 {
     WindowPlan p;
     const int G = d.n_q_heads / d.n_kv_heads;
-    const int64_t rows = (int64_t)(d.max_spec_len + 1) * G;
+    const int64_t rows = (int64_t)(d.max_spec_len + 1) * G, tiles = (rows + 15) / 16;
     p.kind = d.path != ADASPEC_PATH_VECTOR && window_fast_supported(d) ? WindowKind::kMfma : WindowKind::kVector;
-    // as few groups of up to 64 rows as there can be, of equal numbers of 16-row tiles
-    const int64_t tiles = (rows + 15) / 16, least = (tiles + 3) / 4;
-    p.rows_per_group = p.kind == WindowKind::kVector ? kWinRows : 16 * (int)((tiles + least - 1) / least);
-    p.groups = (int)((rows + p.rows_per_group - 1) / p.rows_per_group);
-    p.units = (int64_t)d.batch * d.n_kv_heads * p.groups;
+    p.block_pages = d.dtype == ADASPEC_F32 ? 1 : d.head_dim == 64 ? 4 : 2;
+    // as few groups of up to `most` 16-row tiles as there can be, of equal numbers of tiles
+    auto group = [&](int most) {
+        const int64_t least = (tiles + most - 1) / most;
+        p.rows_per_group = p.kind == WindowKind::kVector ? kWinRows : 16 * (int)((tiles + least - 1) / least);
+        p.groups = (int)((rows + p.rows_per_group - 1) / p.rows_per_group);
+        p.units = (int64_t)d.batch * d.n_kv_heads * p.groups;
+    };
+    // blocks of a unit's list of pages at most: a row group spans this many positions
+    auto most_blocks = [&]() {
+        const int64_t across = (p.rows_per_group - 1) / G + 2, span = across < d.max_spec_len + 1 ? across : d.max_spec_len + 1;
+        const int64_t pages = ((int64_t)sinks + 15) / 16 + ((int64_t)window + span + 14) / 16 + 1;
+        return ((pages < d.max_pages_per_req ? pages : d.max_pages_per_req) + p.block_pages - 1) / p.block_pages;
+    };
     p.splits = 1;
     p.alone = false;
-    p.block_pages = d.dtype == ADASPEC_F32 ? 1 : d.head_dim == 64 ? 4 : 2;
+    group(4);
     if (p.kind == WindowKind::kMfma) {
-        // entries of a unit's list of pages at most: a row group spans this many positions
-        const int64_t span = (p.rows_per_group - 1) / G + 2 < d.max_spec_len + 1 ? (p.rows_per_group - 1) / G + 2 : d.max_spec_len + 1;
-        int64_t pages = ((int64_t)sinks + 15) / 16 + ((int64_t)window + span + 14) / 16 + 1;
-        if (pages > d.max_pages_per_req) pages = d.max_pages_per_req;
-        const int64_t blocks = (pages + p.block_pages - 1) / p.block_pages, turns = (blocks + 3) / 4;   // turns of four wavefronts
+        int64_t blocks = most_blocks();
         // One wavefront per unit where units are many and short.  A workgroup of four costs its look-ups, its merging and its
         // quarter-filled last turn whatever the length: 512 of them fill the chip, a thousand lone wavefronts take their place.
         // Measured, alone / four (us, 16 bits, 8 kv heads, 1-3 drafts; window 16, 128, 256, 512, 1024):
@@ -292,12 +297,20 @@ WindowPlan make_window_plan(const adaspec_attn_dims &d, int window, int sinks)
         //   head_dim 128, 528 units   8.0/10.3  13.2/15.4   20.0/20.4  33.1/31.3   59.6/53.5
         //   head_dim 128, 1152 units  10.4/15.6 19.8/25.1   32.0/33.6  56.7/55.2  105.7/101.7
         //   head_dim 64, 1152 units   7.7/14.6  13.4/16.9   19.6/25.2  31.9/32.7   56.3/53.8
-        p.alone = d.dtype != ADASPEC_F32 && p.rows_per_group <= 48 && p.units > 512 && blocks <= 10;
+        // A lone wavefront has registers for 48 rows; larger groups are cut into more, which read the window again.  8 kv heads, 64
+        // rows, window 16, 128, 256:  head_dim 128, 128 requests 20/27, 33/39, 51/48; 200 requests 31/43, 55/61, 89/74;
+        //                             head_dim 64, 200 requests 18/39, 34/43, 51/62.
+        p.alone = d.dtype != ADASPEC_F32 && p.units > 512 && blocks <= (p.rows_per_group > 48 ? 7 : 10);
+        if (p.alone && p.rows_per_group > 48) {
+            group(3);
+            blocks = most_blocks();
+        }
         // Parts of a unit where units are few: one workgroup per compute unit in all, at least two blocks in a part, and only
         // where that saves the joining launch's 3-4 us: four turns, or eight with less than four parts, whose workgroups
         // still wait for each other's memory.  Measured, parts / whole (us, head_dim 128, 16 bits):
         //   window 1024: 8 units, 16 parts 10.7/17.6; 64 units, 4 parts 15.7/18.6; 128 units, 2 parts 21.0/19.5; 256 units, 2 parts 33/26.5
         //   window 4096: 8 units, 16 parts 13.5/47.7; 64 units, 4 parts 29.9/49.0; 128 units, 2 parts 50.0/53.5
+        const int64_t turns = (blocks + 3) / 4;                     // of four wavefronts
         if (!p.alone && p.units > 0) {
             int64_t want = 256 / p.units;
             if (want > blocks / 2) want = blocks / 2;

@@ -8,8 +8,8 @@ from tests.test_gpu_parity import pkg  # noqa: F401  (fixture)
 
 pytestmark = pytest.mark.gpu
 
-# Hq, Hkv, longest draft: one, two, three row tiles of 16 rows; row groups of 64 (and their rests); one row in a unit
-HEADS = [(2, 2, 5), (8, 2, 7), (10, 2, 8), (16, 2, 10), (3, 3, 0)]
+# Hq, Hkv, longest draft: one, two, three row tiles of 16 rows; two row groups, of 64 rows where windows are longer; one row in a unit
+HEADS = [(2, 2, 5), (8, 2, 7), (10, 2, 8), (16, 2, 10), (16, 2, 7), (3, 3, 0)]
 
 
 def many(seed, batch, hq, hkv, most, d, dtype, longest=420):
