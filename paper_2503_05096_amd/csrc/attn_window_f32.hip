@@ -6,6 +6,12 @@
 //                                (j, e), whose four k-slots are the channels 16 j + 4 g + e;
 //   O^T[d][row]    += V^T P^T    the accumulator lane (g, n) holds S^T[4 g + r][n]: step r takes it as B operand; lane (g, m) loads
 //                                channels 64 h + 4 m .. + 3 of token 4 g + r, element e is the A operand of output tile (h, e).
+//
+// Up to 32 rows the reads bound it: 128 requests, 32 query on 8 kv heads, 3 drafts, window 1024: 182 us for 1095 MB at head_dim
+// 128, 89 us for 547 MB at 64 (6.0-6.2 TB/s).  Beyond that the fp32 matrix products do (138 TFLOP/s in a large product): 64
+// requests, 64 query heads, 48 rows 139 us, 93 of them products at that rate; 64 rows 178 and 124.  Two workgroups per compute
+// unit wherever the registers last: at head_dim 64 always (64 rows: 88 us, one workgroup 105), at 128 up to 32 rows (48 rows:
+// 139 us with one; two spill, 190; groups of 32 rows, which read the window twice, 196).
 #include "attn_window_merge.h"
 
 namespace adaspec {
@@ -13,7 +19,7 @@ namespace adaspec {
 __device__ __forceinline__ f32x4 window_mfma_f32(float a, float b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
 
 template <int D, int RT>
-__global__ __launch_bounds__(256, (RT <= 2 ? 2 : 1)) void attn_window_f32_kernel(WindowDims dims, const int32_t *__restrict__ block_table,
+__global__ __launch_bounds__(256, (D == 64 || RT <= 2 ? 2 : 1)) void attn_window_f32_kernel(WindowDims dims, const int32_t *__restrict__ block_table,
                                                                                  const char *__restrict__ q, const char *__restrict__ k_pages,
                                                                                  const char *__restrict__ v_pages, void *__restrict__ out,
                                                                                  float *__restrict__ part_ml, float *__restrict__ part_o, int splits,
