@@ -174,7 +174,9 @@ int adaspec_verify_attn(const void *q, const void *k_pages, const void *v_pages,
  *     matrix-core form (head_dim 64 or 128), VECTOR the portable one, AUTO the
  *     former where it fits.
  *   - There is no metadata: a PLAN_BUILD_ONLY call checks its arguments and
- *     enqueues nothing, a PLAN_REUSE call is a PLAN_BUILD_AND_RUN call.
+ *     enqueues nothing, a PLAN_REUSE call is a PLAN_BUILD_AND_RUN call.  Every
+ *     call overwrites its workspace: where layers with and without a window
+ *     alternate, a plan that adaspec_verify_attn is to reuse needs one of its own.
  * ---------------------------------------------------------------------- */
 size_t adaspec_verify_attn_window_workspace_bytes(const adaspec_attn_dims *dims, int32_t window, int32_t sinks);
 

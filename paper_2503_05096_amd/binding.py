@@ -297,7 +297,8 @@ def verify_attn(q, k_pages, v_pages, block_table, ctx_lens, spec_lens, out=None,
     and that no other call touches between the build and the last reuse.
     parents [TQ] int32 (a draft tree): adaspec_verify_attn_tree instead.
     window, sinks: adaspec_verify_attn_window instead: a row sees the last `window` tokens up to its own and the request's
-    first `sinks`; block_table entries of pages that no row sees are never read.  Not with parents."""
+    first `sinks`; block_table entries of pages that no row sees are never read.  Not with parents.  Such a call has no plan of
+    its own and overwrites its workspace: not the one that holds a plan for calls without a window."""
     if window is not None or sinks != 0:
         if window is None:
             raise ValueError("verify_attn(sinks=...) needs a window: without one every token is visible")
@@ -560,6 +561,8 @@ def check_ragged_inputs(block_table, ctx_lens, spec_lens, dims: AttnDims, stream
     """Runs the device-side metadata check and returns the flag word (synchronises).  window, sinks: the check of a windowed
     call, which leaves out the entries that such a call never reads."""
     import torch
+    if window is None and sinks != 0:
+        raise ValueError("check_ragged_inputs(sinks=...) needs a window: without one every token is visible")
     flags = torch.zeros(1, dtype=torch.int32, device=block_table.device)
     if window is not None:
         rc = lib().adaspec_check_window_inputs(block_table.data_ptr(), ctx_lens.data_ptr(), spec_lens.data_ptr(), C.byref(dims),

@@ -208,7 +208,8 @@ __global__ __launch_bounds__(64 * kWinWaves, kP == 1 ? 4 : 3) void attn_window_v
 
 // Rows of a unit whose pages were cut: out = sum_s 2^(m_s - m*) O_s / sum_s 2^(m_s - m*) l_s.  One wavefront per row, four
 // rows of a unit per workgroup; lane s looks at (m_s, l_s).  Latency is all there is to it: the states of the first parts are
-// requested before it is known how many parts there are (the places are there in any case).
+// requested before it is known how many parts there are (the places are there in any case).  4.9 us for 8 units of 24 rows in 16
+// parts, of which a call sees 3.7 behind the main kernel.
 template <int D>
 __global__ __launch_bounds__(256) void attn_window_combine_kernel(WindowDims dims, const float *__restrict__ part_ml,
                                                                   const float *__restrict__ part_o, void *__restrict__ out, int splits,

@@ -3,6 +3,11 @@
 //
 // Every result is independent of the order in which workgroups run: counts change by integer atomics, free pages are handed
 // out by their rank in ascending order, requests by theirs.
+//
+// The id calls move little (remap of 128 requests 0.8 MB, compaction of 262144 pages 5.2 MB): launches and chains of dependent
+// accesses bound them, so they are few launches with everything in flight that can be.  Whole calls from Python: remap of
+// 128 requests of up to 8192 tokens 13-16 us (four kernels of 2.6, 3.6, 2.4 and 4.2), of 16 into 256 forks 10.8 (5.4 and 5.5),
+// compaction of 2048 pages 6 us (one of 5.3), of 262144 pages 10.5 us (2.3 and 9.3).
 #include "adaspec_internal.h"
 #include "device_utils.h"
 
@@ -172,12 +177,14 @@ __global__ __launch_bounds__(kPagesThreads) void remap_count_kernel(RemapArgs a)
     if (tid == 0) a.tile_wants[tile] = total;
 }
 
-// Everything up to here in one launch, where the old table and both batches are small: a workgroup per 1024 pages goes through
+// Everything up to here in one launch, where the old table and both batches are small (every workgroup reads the whole old
+// table; whole calls of 64 requests, this way / in three launches: 8.8/13.5 us with 2112 entries, 11.6/13.5 with 32832, 14.0/13.6 with
+// 65664, 18.1/13.6 with 131200; of 256 requests 12.5/13.7 with 32768, 14.5/13.6 with 65536): a workgroup per 1024 pages goes through
 // the whole old table and keeps the counts of its own pages in LDS, so that nobody has to wait for anybody.  It also decides
 // what those rows want that are about to write into one of its pages (the first workgroup: into none that holds tokens).  The
 // workgroups behind write a new row each.
 constexpr int kSmallRows = 1024;
-constexpr int64_t kSmallEntries = 32768;
+constexpr int64_t kSmallEntries = 49152;
 constexpr int kScan = 2;                    // loads of four entries that a thread has under way
 static_assert(kSmallRows == kChunk, "a thread per row");
 __global__ __launch_bounds__(kChunk) void remap_small_kernel(RemapArgs a)
@@ -440,7 +447,8 @@ __global__ __launch_bounds__(kPagesThreads) void compact_words_kernel(CompactArg
 
 // Workgroups 0 .. chunks - 1: counts, map and moves of a chunk of pages; those behind: the table.  Every count is read and
 // written by one thread each, so that the new counts may lie over the old ones (not with kSelf).
-// kSelf: small pools, whose words every workgroup works out itself.
+// kSelf: small pools, whose words every workgroup works out itself, from 16 loads of a thread: one launch (whole calls 5.2 us for
+// 2048 pages, 6.8 for 16384) instead of two (8.0, 9.2).  The new counts must not lie over the old ones then.
 constexpr int kSelfPages = 16384;
 template <bool kSelf>
 __global__ __launch_bounds__(kPagesThreads) void compact_write_kernel(CompactArgs a)
@@ -673,7 +681,8 @@ hipError_t launch_kv_compact_pages(const CompactArgs &a, hipStream_t stream)
 }
 
 // ---- copy ----------------------------------------------------------------------------------------------------------
-// One workgroup per (pair, layer, tensor) at a time: 16 bytes per thread and access.
+// One workgroup per (pair, layer) at a time, K and V side by side: 16 bytes per thread and access.  Memory bounds it: 4096 pages of
+// 64 KB of K and V in 111 us, 4.84 TB/s read and written, the rate of a large copy (4.93).
 __global__ __launch_bounds__(kPagesThreads) void copy_pages_kernel(uint4 *__restrict__ k_pages, uint4 *__restrict__ v_pages,
                                                                    const int32_t *__restrict__ copy_src,
                                                                    const int32_t *__restrict__ copy_dst, int n_copies, int layers,

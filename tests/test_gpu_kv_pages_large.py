@@ -10,7 +10,7 @@ from tests.test_gpu_parity import pkg  # noqa: F401  (fixture)
 pytestmark = pytest.mark.gpu
 
 
-@pytest.mark.parametrize("old,B,width,slack", [(1024, 1024, 32, 900), (1025, 5, 8, 9000), (5, 1025, 8, 300), (1024, 2048, 33, 2500), (700, 2049, 6, 0),
+@pytest.mark.parametrize("old,B,width,slack", [(1024, 1024, 32, 900), (1024, 900, 48, 900), (1024, 30, 49, 100), (1025, 5, 8, 9000), (5, 1025, 8, 300), (1024, 2048, 33, 2500), (700, 2049, 6, 0),
                                                (2049, 2049, 4, 100), (30000, 35535, 2, 70000), (65534, 1, 1, 3), (1, 65534, 3, 150000)])
 @pytest.mark.parametrize("window", [0, 30])
 def test_remap_of_large_batches(old, B, width, slack, window, pkg):  # noqa: F811

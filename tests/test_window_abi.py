@@ -81,6 +81,8 @@ def test_python_refusals():
     kv, bt, one = torch.zeros(1, 2, 16, 64), torch.zeros(1, 1, dtype=torch.int32), torch.ones(1, dtype=torch.int32)
     with pytest.raises(ValueError, match="sinks"):
         pkg.verify_attn(q, kv, kv, bt, one, one, max_spec_len=1, sinks=4)
+    with pytest.raises(ValueError, match="sinks"):
+        pkg.check_ragged_inputs(bt, one, one, _attn_dims(), sinks=4)
     with pytest.raises(ValueError, match="trees"):
         pkg.verify_attn(q, kv, kv, bt, one, one, max_spec_len=1, window=8, parents=one)
     with pytest.raises(AssertionError):                             # tensors that are not on a GPU
