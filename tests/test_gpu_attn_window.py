@@ -3,8 +3,9 @@
 Everything that a row must not see is poisoned: tokens that no row of a request sees hold NaN, pages made of such tokens
 have no entry in the block table (-1), unused slots hold NaN (the workload's own).
 
-Tolerance on the fp32 accumulator: that of the other attention tests, 2e-5, for the same reasons (scores, weights and sums in
-fp32, weights of at least 22 bits, values of N(0, 1)).  16-bit outputs: half a step of the type on top, 2^-9 (bf16) or 2^-12
+Tolerance on the fp32 accumulator: that of the other attention tests, 2e-5.  Scores, weights and sums are fp32; the matrix cores
+take 16-bit weights in two pieces, which leave 2^-24 (f16) or 2^-18 (bf16) of a weight out: of a mean of values below 5, 1.9e-5 if
+every weight were off by that much to the same side.  16-bit outputs: half a step of the type on top, 2^-9 (bf16) or 2^-12
 (fp16) of the next power of two above the value, which is at most 2^-8 or 2^-11 of the value."""
 import numpy as np
 import pytest
