@@ -65,10 +65,10 @@ __device__ __forceinline__ void load_lds_2(const v4i32 &rsrc, uint32_t off0, uin
 __device__ __forceinline__ void load_shared_page(const v4i32 &rsrc, uint32_t off0, uint32_t off1, uint32_t off2, uint32_t off3, uint32_t lds)
 {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %5, 0 offen lds\n\t"
-                 "buffer_load_dwordx4 %2, %5, 0 offen offset:1024 lds\n\t"
-                 "buffer_load_dwordx4 %3, %5, 0 offen offset:2048 lds\n\t"
-                 "buffer_load_dwordx4 %4, %5, 0 offen offset:3072 lds"
-                 :: "s"(lds), "v"(off0), "v"(off1), "v"(off2), "v"(off3), "s"(rsrc) : "memory", "m0");
+                 "buffer_load_dwordx4 %2, %5, 0 offen offset:%6 lds\n\t"
+                 "buffer_load_dwordx4 %3, %5, 0 offen offset:%7 lds\n\t"
+                 "buffer_load_dwordx4 %4, %5, 0 offen offset:%8 lds"
+                 :: "s"(lds), "v"(off0), "v"(off1), "v"(off2), "v"(off3), "s"(rsrc), "n"(1 << 10), "n"(2 << 10), "n"(3 << 10) : "memory", "m0");
 }
 
 template <class T, int D, int RT, bool kAlone, bool kShared>
