@@ -169,7 +169,7 @@ int adaspec_verify_attn(const void *q, const void *k_pages, const void *v_pages,
  *     infinities too).
  *   - Same dims as adaspec_verify_attn, but at most 2^30 tokens per block table
  *     row, 65535 kv heads, n_q_heads * head_dim at most 2^23, and batch * row
- *     groups (of 8 to 64 query rows times group size) below 2^24, below 2^31 with
+ *     groups (of 4 to 64 query rows times group size) below 2^24, below 2^31 with
  *     the kv heads.  path: FAST is the
  *     matrix-core form (head_dim 64 or 128), VECTOR the portable one, AUTO the
  *     former where it fits.

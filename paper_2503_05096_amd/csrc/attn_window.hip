@@ -1,6 +1,6 @@
 // Windowed verification attention: the plan of a call, the merge of a unit's parts, and the portable form: any of the three
 // storage types, any head_dim that is a multiple of 8 up to 256.  A workgroup of four wavefronts per (request, kv head, chunk of
-// 8 query rows); wavefront w takes the 64 tokens w, w + 4, ... of the unit's list of pages.
+// 8 or 4 query rows); wavefront w takes the 64 tokens w, w + 4, ... of the unit's list of pages.
 //
 // Per 64 tokens: lane <-> token for the scores (each lane walks its key row in pieces of 8 channels, the query rows are broadcast
 // from LDS), wavefront reductions for the online softmax, then lane <-> two channels side by side for P.V, 16 value rows (8 above 128
@@ -8,7 +8,7 @@
 // and is left out of that row's sum, not multiplied by zero: whatever it holds cannot reach the row.
 //
 // Its vector units bound it: 16 multiply-adds per value of K and of V that arrives, twice as many instructions with unpacking
-// and LDS.  Window 1024, 32 requests of 16 rows at 8 kv heads: 72 us for 102 MB (bf16, head_dim 96; one wavefront per unit, a
+// and LDS; with few units the latency of a wavefront's turns does.  Window 1024, 32 requests of 16 rows at 8 kv heads: 72 us for 102 MB (bf16, head_dim 96; one wavefront per unit, a
 // value row at a time: 1125), 150 us for 273 MB (head_dim 256; 2236), 83 us for 204 MB (fp32, 96; 855).
 #include <type_traits>
 
@@ -16,7 +16,7 @@
 
 namespace adaspec {
 
-constexpr int kWinRows = 8, kWinWaves = 4;
+constexpr int kWinWaves = 4;
 constexpr int kWindowMaxSplits = 64;        // a lane of the combine kernel each
 
 // 8 values side by side, from a multiple of 8 on
@@ -45,7 +45,8 @@ template <class T> __device__ __forceinline__ float2 pair_values(typename Pair<T
     return make_float2(load_as_float<T>(&x, 0), load_as_float<T>(&x, 1));
 }
 
-template <class T, int kP>                  // kP: pairs of channels that a lane has, head_dim at most 128 kP
+// kP: pairs of channels that a lane has, head_dim at most 128 kP; kWinRows: 8, or 4 where no request has more
+template <class T, int kP, int kWinRows>
 __global__ __launch_bounds__(64 * kWinWaves, kP == 1 ? 4 : 3) void attn_window_vector_kernel(WindowDims dims, const void *__restrict__ q,
                                                                             const void *__restrict__ k_pages,
                                                                             const void *__restrict__ v_pages, void *__restrict__ out, int d,
@@ -55,7 +56,7 @@ __global__ __launch_bounds__(64 * kWinWaves, kP == 1 ? 4 : 3) void attn_window_v
     typedef typename Pair<T>::type pair;
     // Q rows and weights of every wavefront; then its state.  (12 or 16 KB; 16 or 32)
     __shared__ __attribute__((aligned(16))) float smem[kWinWaves * kWinRows * kD];
-    static_assert(kWinRows * kD + kWinWaves * 64 * kWinRows <= kWinWaves * kWinRows * kD, "Q and weights fit where the states go");
+    static_assert(kD + kWinWaves * 64 <= kWinWaves * kD, "Q and weights fit where the states go");
     __shared__ float s_m[kWinWaves][kWinRows], s_l[kWinWaves][kWinRows];
     const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
     float *qs = smem, *ps = smem + kWinRows * kD + wv * 64 * kWinRows;      // [row][channel]; [token][row]
@@ -129,8 +130,9 @@ __global__ __launch_bounds__(64 * kWinWaves, kP == 1 ? 4 : 3) void attn_window_v
             if (!vis) p[r] = -1.f;
         }
         // (the wavefront's own part of LDS, whose accesses keep their order)
-        *reinterpret_cast<float4 *>(ps + lane * kWinRows) = make_float4(p[0], p[1], p[2], p[3]);
-        *reinterpret_cast<float4 *>(ps + lane * kWinRows + 4) = make_float4(p[4], p[5], p[6], p[7]);
+#pragma unroll
+        for (int r = 0; r < kWinRows; r += 4)
+            *reinterpret_cast<float4 *>(ps + lane * kWinRows + r) = make_float4(p[r], p[r + 1], p[r + 2], p[r + 3]);
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
         for (int j = 0; j < 4 && v0 + j < u.pages; ++j) {
@@ -151,8 +153,12 @@ __global__ __launch_bounds__(64 * kWinWaves, kP == 1 ? 4 : 3) void attn_window_v
 #pragma unroll
                 for (int tt = 0; tt < kAhead; ++tt) {
                     const float *at = ps + (16 * j + t0 + tt) * kWinRows;
-                    const float4 a = *reinterpret_cast<const float4 *>(at), b = *reinterpret_cast<const float4 *>(at + 4);
-                    const float w[kWinRows] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+                    float w[kWinRows];
+#pragma unroll
+                    for (int r = 0; r < kWinRows; r += 4) {
+                        const float4 a = *reinterpret_cast<const float4 *>(at + r);
+                        w[r] = a.x; w[r + 1] = a.y; w[r + 2] = a.z; w[r + 3] = a.w;
+                    }
 #pragma unroll
                     for (int k = 0; k < kP; ++k) {
                         const float2 val = pair_values<T>(x[tt][k]);
@@ -186,7 +192,8 @@ __global__ __launch_bounds__(64 * kWinWaves, kP == 1 ? 4 : 3) void attn_window_v
             *reinterpret_cast<float2 *>(smem + (wv * kWinRows + r) * kD + 2 * lane + 128 * k) = make_float2(acc[r][2 * k], acc[r][2 * k + 1]);
     }
     __syncthreads();
-    const int r = tid / 32, row = u.r0 + r;
+    constexpr int kAcross = 64 * kWinWaves / kWinRows;              // threads of a row
+    const int r = tid / kAcross, row = u.r0 + r;
     if (row >= u.rows) return;
     float ms = s_m[0][r], ltot = 0.f, sc[kWinWaves];
 #pragma unroll
@@ -198,7 +205,7 @@ __global__ __launch_bounds__(64 * kWinWaves, kP == 1 ? 4 : 3) void attn_window_v
     }
     const float inv = 1.0f / ltot;
     const int64_t obase = ((u.qrow0 + row / G) * dims.Hq + gkv * G + row % G) * (int64_t)d;
-    for (int c = tid & 31; c < d; c += 32) {
+    for (int c = tid % kAcross; c < d; c += kAcross) {
         float o = 0.f;
 #pragma unroll
         for (int w = 0; w < kWinWaves; ++w) o += sc[w] * smem[(w * kWinRows + r) * kD + c];
@@ -273,10 +280,10 @@ WindowPlan make_window_plan(const adaspec_attn_dims &d, int window, int sinks)
     const int64_t rows = (int64_t)(d.max_spec_len + 1) * G, tiles = (rows + 15) / 16;
     p.kind = d.path != ADASPEC_PATH_VECTOR && window_fast_supported(d) ? WindowKind::kMfma : WindowKind::kVector;
     p.block_pages = d.dtype == ADASPEC_F32 ? 1 : d.head_dim == 64 ? 4 : 2;
-    // as few groups of up to `most` 16-row tiles as there can be, of equal numbers of tiles
+    // as few groups of up to `most` 16-row tiles as there can be, of equal numbers of tiles (portable form: of 4 `most` rows)
     auto group = [&](int most) {
         const int64_t least = (tiles + most - 1) / most;
-        p.rows_per_group = p.kind == WindowKind::kVector ? kWinRows : 16 * (int)((tiles + least - 1) / least);
+        p.rows_per_group = p.kind == WindowKind::kVector ? 4 * most : 16 * (int)((tiles + least - 1) / least);
         p.groups = (int)((rows + p.rows_per_group - 1) / p.rows_per_group);
         p.units = (int64_t)d.batch * d.n_kv_heads * p.groups;
     };
@@ -288,7 +295,16 @@ WindowPlan make_window_plan(const adaspec_attn_dims &d, int window, int sinks)
     };
     p.splits = 1;
     p.alone = false;
-    group(4);
+    if (p.kind == WindowKind::kVector) {
+        // Units of four rows where there are no more, and where they leave room: a unit of eight takes up to twice as long, two of
+        // four read K and V twice.  Four / eight (us; window 512, head_dim 96 bf16, 256 fp32):
+        //   32 units of four rows 20/38, 55/80;  512 units 26/43, 99/100;  2048 units 85/95, 400/338;  4096 units 132/129, 610/424
+        // and one row per kv head, 2048 units of which there are as many either way: 64/104, 300/299 (window 256).
+        group(1);
+        if (rows > 4 && p.units > 512) group(2);
+    } else {
+        group(4);
+    }
     if (p.kind == WindowKind::kMfma) {
         int64_t blocks = most_blocks();
         // One wavefront per unit where units are many and short.  A workgroup of four costs its look-ups, its merging and its
@@ -346,13 +362,18 @@ hipError_t launch_attn_window(const WindowArgs &a)
         else combine(std::integral_constant<int, 64>{});
         return hipGetLastError();
     }
-    auto launch = [&](auto tag, auto pairs) {
-        hipLaunchKernelGGL((attn_window_vector_kernel<decltype(tag), decltype(pairs)::value>), dim3((unsigned)(d.batch * a.plan.groups), d.n_kv_heads),
-                           dim3(64 * kWinWaves), 0, a.stream, w, a.q, a.k_pages, a.v_pages, a.out, d.head_dim, a.scale_log2, d.out_dtype);
+    auto launch = [&](auto tag, auto pairs, auto rows) {
+        hipLaunchKernelGGL((attn_window_vector_kernel<decltype(tag), decltype(pairs)::value, decltype(rows)::value>),
+                           dim3((unsigned)(d.batch * a.plan.groups), d.n_kv_heads), dim3(64 * kWinWaves), 0, a.stream, w, a.q, a.k_pages, a.v_pages, a.out,
+                           d.head_dim, a.scale_log2, d.out_dtype);
     };
     auto with_pairs = [&](auto tag) {
-        if (d.head_dim <= 128) launch(tag, std::integral_constant<int, 1>{});
-        else launch(tag, std::integral_constant<int, 2>{});
+        auto with_rows = [&](auto pairs) {
+            if (p.rows_per_group == 4) launch(tag, pairs, std::integral_constant<int, 4>{});
+            else launch(tag, pairs, std::integral_constant<int, 8>{});
+        };
+        if (d.head_dim <= 128) with_rows(std::integral_constant<int, 1>{});
+        else with_rows(std::integral_constant<int, 2>{});
     };
     if (d.dtype == ADASPEC_F32) with_pairs(F32{});
     else if (d.dtype == ADASPEC_F16) with_pairs(F16{});

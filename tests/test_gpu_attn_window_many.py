@@ -70,6 +70,8 @@ def test_portable_form_over_several_turns(d, dtype, pkg):  # noqa: F811
     for window, sinks in ((700, 40), (1000, 0), (3, 17)):
         st = step(1500 + d, [1, 63, 64, 65, 257, 900, 700, 513], [0, 1, 0, 2, 3, 6, 0, 5], 6, 2, d, dtype)
         check(pkg, poisoned(st, window, sinks), window, sinks, paths=("vector",))
+    st = many(1550 + d, 180, 6, 2, 3, d, dtype)                     # 12 rows: units of eight
+    check(pkg, poisoned(st, 90, 4), 90, 4, paths=("vector",))
 
 
 def test_two_calls_at_once_and_rows_behind_the_last_request(pkg):  # noqa: F811
