@@ -7,7 +7,7 @@
 // The id calls move little (remap of 128 requests 0.8 MB, compaction of 262144 pages 5.2 MB): launches and chains of dependent
 // accesses bound them, so they are few launches with everything in flight that can be.  Whole calls from Python: remap of
 // 128 requests of up to 8192 tokens 13-16 us (four kernels of 2.6, 3.6, 2.4 and 4.2), of 16 into 256 forks 10.8 (5.4 and 5.5),
-// compaction of 2048 pages 6 us (one of 5.3), of 262144 pages 10.5 us (2.3 and 9.3).
+// compaction of 2048 pages 6 us (one of 5.3), of 262144 pages 9.7 us (2.3 and 8.7).
 #include "adaspec_internal.h"
 #include "device_utils.h"
 
@@ -475,6 +475,18 @@ __global__ __launch_bounds__(kPagesThreads) void compact_write_kernel(CompactArg
     } else {
         table_entries((int64_t)(blockIdx.x - a.chunks) * kChunk);
     }
+    // the words of those pages, which the bases are not needed for either (kSelf: there are none yet)
+    int2 own[kPerThread];
+    auto page_at = [&](int k) { return on_counts ? (int)blockIdx.x * kChunk + k * kPagesThreads + tid : got[k]; };
+    auto own_words = [&]() {
+#pragma unroll
+        for (int k = 0; k < kPerThread; ++k) {
+            const int p = page_at(k), w = p >= 0 && p < d.num_pages ? p / 32 : 0;
+            if constexpr (kSelf) own[k] = s_words[w];
+            else own[k] = a.words[w];
+        }
+    };
+    if constexpr (!kSelf) own_words();
     if constexpr (kSelf) {
         constexpr int kMost = kSelfPages / kChunk;
         int4 r[kMost];
@@ -592,13 +604,13 @@ __global__ __launch_bounds__(kPagesThreads) void compact_write_kernel(CompactArg
         a.status[1] = moves;
     }
     // of a page, or of what an entry names: the number of its move, or -1
-    auto move_of = [&](int p) {
+    auto move_of = [&](int p, int2 w) {
         if (p < N || p >= d.num_pages) return -1;
-        const int2 w = word(p / 32);
         const int m = used_before(p, w) - low;
         return (((uint32_t)w.x >> (p & 31)) & 1u) && m < d.max_moves ? m : -1;
     };
     // (what has to be looked up is, for all four, before anything is written: the loads are under way together)
+    if constexpr (kSelf) own_words();
     if (on_counts) {
         int move[kPerThread], to[kPerThread] = {};
         const int (&refs)[kPerThread] = got;
@@ -606,12 +618,8 @@ __global__ __launch_bounds__(kPagesThreads) void compact_write_kernel(CompactArg
 #pragma unroll
         for (int k = 0; k < kPerThread; ++k) {
             const int p = blockIdx.x * kChunk + k * kPagesThreads + tid;
-            move[k] = move_of(p);
-            hole[k] = false;
-            if (p < N) {
-                const int2 w = word(p / 32);
-                hole[k] = !(((uint32_t)w.x >> (p & 31)) & 1u) && p - used_before(p, w) < d.max_moves;
-            }
+            move[k] = move_of(p, own[k]);
+            hole[k] = p < N && !(((uint32_t)own[k].x >> (p & 31)) & 1u) && p - used_before(p, own[k]) < d.max_moves;
         }
         free_pages(move, to);
 #pragma unroll
@@ -643,13 +651,14 @@ __global__ __launch_bounds__(kPagesThreads) void compact_write_kernel(CompactArg
 #pragma unroll
         for (int k = 0; k < kPerThread; ++k) {
             p[k] = got[k];
-            move[k] = move_of(p[k]);
+            move[k] = move_of(p[k], own[k]);
         }
         table_entries(e0 + step);
         free_pages(move, p);
 #pragma unroll
         for (int k = 0; k < kPerThread; ++k)
             if (e0 + k * kPagesThreads + tid < entries) a.out_table[e0 + k * kPagesThreads + tid] = p[k];
+        if (e0 + step < entries) own_words();
     }
 }
 

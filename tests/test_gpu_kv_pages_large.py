@@ -46,6 +46,19 @@ def test_compact_of_large_pools(NP, alias, pkg):  # noqa: F811
         check_compact(pkg, table, refs, max_moves=77, alias=alias)
 
 
+@pytest.mark.parametrize("NP", [5000, 50000])
+def test_compact_of_a_table_with_millions_of_entries(NP, pkg):  # noqa: F811
+    """More entries than the workgroups of one launch take at a time; every page in many of them, ids outside the pool too."""
+    r = np.random.default_rng(NP)
+    table = r.integers(-3, NP + 3, (601, 8192)).astype(np.int32)
+    refs = np.bincount(table[(table >= 0) & (table < NP)], minlength=NP).astype(np.int32)
+    free = r.permutation(NP)[:NP // 3]
+    table[np.isin(table, free)] = -1
+    refs[free] = 0
+    for alias in (False, True):
+        check_compact(pkg, table, refs, alias=alias)
+
+
 @pytest.mark.parametrize("NP", [3000, 40000])
 def test_compact_replayed(NP, pkg):  # noqa: F811
     """In place, a few pages at a time, replayed between eager calls that use the same workspace."""
