@@ -8,8 +8,9 @@
 // and is left out of that row's sum, not multiplied by zero: whatever it holds cannot reach the row.
 //
 // Its vector units bound it: 16 multiply-adds per value of K and of V that arrives, twice as many instructions with unpacking
-// and LDS; with few units the latency of a wavefront's turns does.  Window 1024, 32 requests of 16 rows at 8 kv heads: 72 us for 102 MB (bf16, head_dim 96; one wavefront per unit, a
-// value row at a time: 1125), 150 us for 273 MB (head_dim 256; 2236), 83 us for 204 MB (fp32, 96; 855).
+// and LDS; with few units the latency of a wavefront's turns does.  Window 1024, 32 requests of 16 rows at 8 kv heads: 72 us for
+// 102 MB (bf16, head_dim 96; one wavefront per unit, a value row at a time: 1125), 150 us for 273 MB (head_dim 256; 2236), 83 us
+// for 204 MB (fp32, 96; 855).
 #include <type_traits>
 
 #include "attn_window.h"
@@ -354,8 +355,8 @@ hipError_t launch_attn_window(const WindowArgs &a)
         const hipError_t e = d.dtype == ADASPEC_F32 ? launch_attn_window_f32(a, w) : launch_attn_window_mfma(a, w);
         if (e != hipSuccess || p.splits == 1) return e;
         auto combine = [&](auto dim) {
-            hipLaunchKernelGGL((attn_window_combine_kernel<decltype(dim)::value>), dim3((unsigned)(d.batch * p.groups), d.n_kv_heads, p.rows_per_group / 4), dim3(256), 0,
-                               a.stream, w, (const float *)(a.ws + p.off_part_ml), (const float *)(a.ws + p.off_part_o), a.out, p.splits,
+            hipLaunchKernelGGL((attn_window_combine_kernel<decltype(dim)::value>),
+                               dim3((unsigned)(d.batch * p.groups), d.n_kv_heads, p.rows_per_group / 4), dim3(256), 0, a.stream, w, (const float *)(a.ws + p.off_part_ml), (const float *)(a.ws + p.off_part_o), a.out, p.splits,
                                p.block_pages, d.out_dtype);
         };
         if (d.head_dim == 128) combine(std::integral_constant<int, 128>{});

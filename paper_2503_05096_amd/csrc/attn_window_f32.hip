@@ -56,7 +56,8 @@ __global__ __launch_bounds__(256, (D == 64 || RT <= 2 ? 2 : 1)) void attn_window
 #pragma unroll
         for (int r = 0; r < 4; ++r)
 #pragma unroll
-            for (int h = 0; h < kH; ++h) vreg[r][h] = __builtin_nontemporal_load(reinterpret_cast<const f32x4 *>(v_pages + at + v_lane_off + r * (D * 4) + 256 * h));
+            for (int h = 0; h < kH; ++h)
+                vreg[r][h] = __builtin_nontemporal_load(reinterpret_cast<const f32x4 *>(v_pages + at + v_lane_off + r * (D * 4) + 256 * h));
     };
     if (b0 + wv < b1) {
         const int64_t at = page_base(b0 + wv);
@@ -197,8 +198,8 @@ hipError_t launch_attn_window_f32(const WindowArgs &a, const WindowDims &w)
 {
     const WindowPlan &p = a.plan;
     auto launch = [&](auto dim, auto rt) {
-        hipLaunchKernelGGL((attn_window_f32_kernel<decltype(dim)::value, decltype(rt)::value>), dim3((unsigned)(a.dims.batch * p.groups), a.dims.n_kv_heads, p.splits), dim3(256), 0,
-                           a.stream, w, a.block_table, (const char *)a.q, (const char *)a.k_pages, (const char *)a.v_pages, a.out,
+        hipLaunchKernelGGL((attn_window_f32_kernel<decltype(dim)::value, decltype(rt)::value>), 
+                           dim3((unsigned)(a.dims.batch * p.groups), a.dims.n_kv_heads, p.splits), dim3(256), 0, a.stream, w, a.block_table, (const char *)a.q, (const char *)a.k_pages, (const char *)a.v_pages, a.out,
                            (float *)(a.ws + p.off_part_ml), (float *)(a.ws + p.off_part_o), p.splits, a.scale_log2);
     };
     auto with_rt = [&](auto dim) {

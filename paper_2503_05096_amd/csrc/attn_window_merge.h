@@ -8,8 +8,8 @@ namespace adaspec {
 // State of one row over the entries [v0, v1) of its unit's list, by one wavefront: lane <-> token for the scores, lane <-> two
 // channels side by side for the values.  A token that the row does not see is left out, whatever it holds.
 template <class T, int D>
-__device__ __forceinline__ void row_by_selection(const WindowUnit &u, const WindowDims &dims, const int32_t *block_table, const char *q, const char *k_pages, const char *v_pages,
-                                                 int row, int v0, int v1, float scale_log2, float &m, float &l, float2 &acc)
+__device__ __forceinline__ void row_by_selection(const WindowUnit &u, const WindowDims &dims, const int32_t *block_table, const char *q,
+                                                 const char *k_pages, const char *v_pages, int row, int v0, int v1, float scale_log2, float &m, float &l, float2 &acc)
 {
     const int lane = threadIdx.x & 63, G = dims.Hq / dims.Hkv, pos = u.first_pos + row / G;
     const int64_t qbase = ((u.qrow0 + row / G) * dims.Hq + u.gkv * G + row % G) * (int64_t)D;

@@ -72,10 +72,10 @@ __device__ __forceinline__ void load_shared_page(const v4i32 &rsrc, uint32_t off
 }
 
 template <class T, int D, int RT, bool kAlone, bool kShared>
-__global__ __launch_bounds__(kAlone ? 64 : 256, kAlone ? (RT == 1 ? 4 : RT == 2 && D == 64 ? 3 : 2) : 2) void attn_window_kernel(WindowDims dims, const int32_t *__restrict__ block_table,
-                                                             const char *__restrict__ q, const char *__restrict__ k_pages, const char *__restrict__ v_pages,
-                                                             void *__restrict__ out, float *__restrict__ part_ml,
-                                                             float *__restrict__ part_o, int splits, float scale_log2, int out_dtype)
+__global__ __launch_bounds__(kAlone ? 64 : 256, kAlone ? (RT == 1 ? 4 : RT == 2 && D == 64 ? 3 : 2) : 2)
+void attn_window_kernel(WindowDims dims, const int32_t *__restrict__ block_table, const char *__restrict__ q,
+                        const char *__restrict__ k_pages, const char *__restrict__ v_pages, void *__restrict__ out,
+                        float *__restrict__ part_ml, float *__restrict__ part_o, int splits, float scale_log2, int out_dtype)
 {
     using Lds = WindowLds<D, RT, kAlone>;
     constexpr int kStep = Lds::kWavesHere;                          // wavefronts that share a unit's blocks
@@ -363,8 +363,11 @@ __global__ __launch_bounds__(kAlone ? 64 : 256, kAlone ? (RT == 1 ? 4 : RT == 2 
 #pragma unroll
             for (int dt = 0; dt < kDt; ++dt) {
                 const f32x4 val = o[nt][dt] * inv;
-                if (out_dtype == ADASPEC_F32) *reinterpret_cast<f32x4 *>(reinterpret_cast<float *>(out) + obase + 16 * dt) = val;
-                else *reinterpret_cast<uint2 *>(reinterpret_cast<uint16_t *>(out) + obase + 16 * dt) = make_uint2(Mma<T>::pack2(val[0], val[1]), Mma<T>::pack2(val[2], val[3]));
+                if (out_dtype == ADASPEC_F32)
+                    *reinterpret_cast<f32x4 *>(reinterpret_cast<float *>(out) + obase + 16 * dt) = val;
+                else
+                    *reinterpret_cast<uint2 *>(reinterpret_cast<uint16_t *>(out) + obase + 16 * dt) =
+                        make_uint2(Mma<T>::pack2(val[0], val[1]), Mma<T>::pack2(val[2], val[3]));
             }
         }
         return;
@@ -384,8 +387,9 @@ __global__ __launch_bounds__(kAlone ? 64 : 256, kAlone ? (RT == 1 ? 4 : RT == 2 
         for (int dt = 0; dt < kDt; ++dt)
             *reinterpret_cast<f32x4 *>(v_slot + window_piece<D>(n16, 4 * dt + g)) = o[nt][dt];
         lds_barrier();
-        finish_window_tile<T, D>(u, dims, block_table, q, k_pages, v_pages, out, part_ml, part_o, smem + Lds::kV, Lds::kWaveBytes, s_m, s_l, kRows, nt, ns, b0 * kPages,
-                                 min(b1 * kPages, u.pages), scale_log2, Weights::kShiftLog2, out_dtype, (((int64_t)blockIdx.x * dims.Hkv + blockIdx.y) * splits + sp) * kRows);
+        finish_window_tile<T, D>(u, dims, block_table, q, k_pages, v_pages, out, part_ml, part_o, smem + Lds::kV, Lds::kWaveBytes, s_m, s_l,
+                                 kRows, nt, ns, b0 * kPages, min(b1 * kPages, u.pages), scale_log2, Weights::kShiftLog2, out_dtype,
+                                 (((int64_t)blockIdx.x * dims.Hkv + blockIdx.y) * splits + sp) * kRows);
         if (nt + 1 < RT) lds_barrier();                             // the next tile overwrites the slots
     }
 }
