@@ -399,8 +399,9 @@ int adaspec_commit(const int32_t *out_tokens, const int32_t *out_accept_len,
  *   4. wants - row by row, in a row the page of step 3 first, then entries
  *      ceil(n / P) .. ceil(new_lens[i] / P) - 1 - are served with the pages that
  *      are free after step 2, lowest id first.
- * Outputs (overwritten; entries that hold nothing are -1):
- *   out_table [batch][max_pages_per_req]   must not overlap block_table
+ * Outputs (overwritten; entries that hold nothing are -1; none may overlap another,
+ * an input or the workspace, except as said: ADASPEC_ERR_DIM):
+ *   out_table [batch][max_pages_per_req]   not block_table
  *   out_refs  [num_pages]                  the counts; may be page_refs itself
  *   copy_src, copy_dst [batch]             the pages of step 3: copy_dst[i] has to
  *                                          become a copy of copy_src[i] before it
@@ -438,8 +439,9 @@ int adaspec_kv_remap(const int32_t *block_table, const int32_t *page_refs, const
  * so that what lies behind can be given away.  With N used pages, the m-th used
  * page at or behind N moves to the m-th free page below N, for the first
  * max_moves of them; later calls go on from there.
+ * Outputs, none of which may overlap another, an input or the workspace except as said:
  *   out_table [old_batch][max_pages_per_req]  block_table with the new ids; may be
- *                                             block_table itself, must not overlap it otherwise
+ *                                             block_table itself
  *   out_refs  [num_pages]                     the counts at the new ids; may be page_refs itself
  *   page_map  [num_pages]                     new id of every used page, -1 for free ones:
  *                                             for holders outside the table

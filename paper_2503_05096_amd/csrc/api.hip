@@ -339,6 +339,32 @@ AcceptPlan make_accept_plan(const adaspec_accept_dims &d)
 
 using namespace adaspec;
 
+// An array of a call.  Of an input, `over`: the number of the output that may be the same array, or -1.
+struct Extent {
+    const void *p;
+    size_t bytes;
+    int over;
+};
+
+static bool overlap(const Extent &a, const Extent &b)
+{
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
+    return a.bytes > 0 && b.bytes > 0 && x < y + b.bytes && y < x + a.bytes;
+}
+
+// whether an output (the workspace is one of them) lies over another one, or over an input that it may not replace
+template <int O, int I>
+static bool outputs_clash(const Extent (&outs)[O], const Extent (&ins)[I])
+{
+    for (int o = 0; o < O; ++o) {
+        for (int k = 0; k < o; ++k)
+            if (overlap(outs[o], outs[k])) return true;
+        for (const Extent &in : ins)
+            if (overlap(outs[o], in) && !(in.over == o && in.p == outs[o].p)) return true;
+    }
+    return false;
+}
+
 extern "C" {
 
 size_t adaspec_verify_attn_workspace_bytes(const adaspec_attn_dims *dims)
@@ -773,12 +799,6 @@ static int validate_pages_dims(const adaspec_pages_dims *d, bool remap)
     return ADASPEC_OK;
 }
 
-static bool overlap(const void *a, size_t na, const void *b, size_t nb)
-{
-    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-    return na > 0 && nb > 0 && x < y + nb && y < x + na;
-}
-
 size_t adaspec_kv_remap_workspace_bytes(const adaspec_pages_dims *dims)
 {
     return validate_pages_dims(dims, true) == ADASPEC_OK ? remap_workspace(*dims, nullptr, nullptr) : 0;
@@ -796,13 +816,18 @@ int adaspec_kv_remap(const int32_t *block_table, const int32_t *page_refs, const
     if (dims->old_batch > 0 && (!block_table || !lens)) return ADASPEC_ERR_NULL;
     if (dims->batch > 0 && (!sources || !new_lens || !out_table || !copy_src || !copy_dst)) return ADASPEC_ERR_NULL;
     if (reinterpret_cast<uintptr_t>(workspace) & 255u) return ADASPEC_ERR_ALIGN;
-    const size_t row = (size_t)dims->max_pages_per_req * 4, pool = (size_t)dims->num_pages * 4;
-    if (overlap(block_table, dims->old_batch * row, out_table, dims->batch * row)) return ADASPEC_ERR_DIM;
-    if (page_refs != out_refs && overlap(page_refs, pool, out_refs, pool)) return ADASPEC_ERR_DIM;
+    const size_t need = remap_workspace(*dims, nullptr, nullptr);
+    if (workspace_bytes < need) return ADASPEC_ERR_WORKSPACE;
+    const size_t row = (size_t)dims->max_pages_per_req * 4, pool = (size_t)dims->num_pages * 4, B = (size_t)dims->batch;
+    const Extent outs[] = {{out_table, B * row, -1}, {out_refs, pool, -1}, {copy_src, 4 * B, -1}, {copy_dst, 4 * B, -1}, {status, 8, -1},
+                           {workspace, need, -1}};
+    const Extent ins[] = {{block_table, dims->old_batch * row, -1}, {page_refs, pool, 1}, {sources, 4 * B, -1},
+                          {lens, 4 * (size_t)dims->old_batch, -1}, {new_lens, 4 * B, -1}};
+    if (outputs_clash(outs, ins)) return ADASPEC_ERR_DIM;
     RemapArgs a{block_table, page_refs, sources, lens, new_lens, out_table, out_refs, copy_src, copy_dst, status, *dims,
                 0, 0, nullptr, nullptr, nullptr, nullptr, nullptr};
     if (a.dims.sinks > (1 << 30)) a.dims.sinks = 1 << 30;
-    if (workspace_bytes < remap_workspace(*dims, &a, static_cast<char *>(workspace))) return ADASPEC_ERR_WORKSPACE;
+    remap_workspace(*dims, &a, static_cast<char *>(workspace));
     return launch_kv_remap(a, static_cast<hipStream_t>(stream)) == hipSuccess ? ADASPEC_OK : ADASPEC_ERR_HIP;
 }
 
@@ -822,11 +847,16 @@ int adaspec_kv_compact_pages(const int32_t *block_table, const int32_t *page_ref
     if (!page_refs || !out_refs || !page_map || !copy_src || !copy_dst || !status || !workspace) return ADASPEC_ERR_NULL;
     if (dims->old_batch > 0 && (!block_table || !out_table)) return ADASPEC_ERR_NULL;
     if (reinterpret_cast<uintptr_t>(workspace) & 255u) return ADASPEC_ERR_ALIGN;
+    const size_t need = compact_workspace(*dims, nullptr, nullptr);
+    if (workspace_bytes < need) return ADASPEC_ERR_WORKSPACE;
     const size_t table = (size_t)dims->old_batch * dims->max_pages_per_req * 4, pool = (size_t)dims->num_pages * 4;
-    if (block_table != out_table && overlap(block_table, table, out_table, table)) return ADASPEC_ERR_DIM;
-    if (page_refs != out_refs && overlap(page_refs, pool, out_refs, pool)) return ADASPEC_ERR_DIM;
+    const size_t moves = (size_t)dims->max_moves * 4;
+    const Extent outs[] = {{out_table, table, -1}, {out_refs, pool, -1}, {page_map, pool, -1}, {copy_src, moves, -1}, {copy_dst, moves, -1},
+                           {status, 8, -1}, {workspace, need, -1}};
+    const Extent ins[] = {{block_table, table, 0}, {page_refs, pool, 1}};
+    if (outputs_clash(outs, ins)) return ADASPEC_ERR_DIM;
     CompactArgs a{block_table, page_refs, out_table, out_refs, page_map, copy_src, copy_dst, status, *dims, 0, 0, nullptr, nullptr};
-    if (workspace_bytes < compact_workspace(*dims, &a, static_cast<char *>(workspace))) return ADASPEC_ERR_WORKSPACE;
+    compact_workspace(*dims, &a, static_cast<char *>(workspace));
     return launch_kv_compact_pages(a, static_cast<hipStream_t>(stream)) == hipSuccess ? ADASPEC_OK : ADASPEC_ERR_HIP;
 }
 

@@ -96,3 +96,26 @@ def test_two_calls_at_once_and_rows_behind_the_last_request(pkg):  # noqa: F811
     torch.cuda.synchronize()
     for _, _, ref, _, _, outs in jobs:
         assert all(torch.equal(o, ref) for o in outs)
+
+
+@pytest.mark.parametrize("dtype,hkv", [("bf16", 8), ("f32", 8)])
+def test_a_pool_beyond_32_bits(dtype, hkv, pkg):  # noqa: F811
+    """Pages whose byte offsets pass 2^32, and whose values' offsets pass 2^31, give what the same pages give at the pool's
+beginning: few units, many (lone wavefronts), and the portable form."""
+    import torch
+    for batch, longest, window in ((3, 1500, 1000), (90, 200, 60)):
+        st = poisoned(many(1600 + batch, max(batch, 5), 2 * hkv, hkv, 2, 128, dtype, longest), window, 4)
+        d = to_device(st, acceptance=False)
+        used = d.k_pages.shape[0]
+        NP = 2 ** 32 // (hkv * 16 * 128 * (2 if dtype == "bf16" else 4)) + 2 * used + 100
+        k, v = (torch.empty((NP,) + tuple(d.k_pages.shape[1:]), dtype=d.q.dtype, device="cuda") for _ in range(2))
+        at = NP - used
+        k[at:], v[at:] = d.k_pages, d.v_pages
+        far = torch.where(d.block_table >= 0, d.block_table + at, d.block_table)
+        for path in ("auto", "vector"):
+            kw = dict(max_spec_len=st.max_spec_len, window=window, sinks=4, path=path)
+            ref = pkg.verify_attn(d.q, d.k_pages, d.v_pages, d.block_table, d.ctx_lens, d.spec_lens, **kw)
+            out = pkg.verify_attn(d.q, k, v, far, d.ctx_lens, d.spec_lens, **kw)
+            assert torch.isfinite(ref).all() and torch.equal(out, ref), (batch, path)
+        del k, v
+        torch.cuda.empty_cache()

@@ -69,6 +69,31 @@ def test_pointers_workspaces_and_overlaps():
         assert _compact(d, p) == -2, (at, by)
 
 
+def test_outputs_over_anything_else():
+    """Every output over every other array, at its beginning and at its last entry; what may be the same array may not be so
+    shifted."""
+    d = _pages()
+    need = [pkg.lib().adaspec_kv_remap_workspace_bytes(C.byref(d)), pkg.lib().adaspec_kv_compact_pages_workspace_bytes(C.byref(d))]
+    # entries of every argument, and which of them are outputs
+    for call, entries, outs, same, ws in ((_remap, [16, 64, 3, 2, 3, 24, 64, 3, 3, 2], range(5, 10), [(6, 1)], need[0]),
+                                          (_compact, [16, 64, 16, 64, 64, 32, 32, 2], range(2, 8), [(2, 0), (3, 1)], need[1])):
+        for o in outs:
+            for k in range(len(entries)):
+                for by in (0, 4 * (entries[k] - 1)):
+                    if k == o or (by == 0 and (o, k) in same):
+                        continue
+                    p = PTRS[:len(entries)]
+                    p[o] = p[k] + by
+                    assert call(d, p) == -2, (call.__name__, o, k, by)
+            p = PTRS[:len(entries)]
+            p[o] = PTRS[10] + ws - 4
+            assert call(d, p) == -2, o
+        for k in range(len(entries)):
+            p = PTRS[:len(entries)]
+            p[k] = PTRS[10]
+            assert call(d, p) == -2, k
+
+
 @pytest.mark.parametrize("kw,n,code", [
     (dict(layers=-1), 4, -2), (dict(num_pages=0), 4, -2), (dict(n_kv_heads=0), 4, -2), (dict(page_size=-1), 4, -2), (dict(head_dim=0), 4, -2),
     (dict(), -1, -2), (dict(dtype=5), 4, -3), (dict(head_dim=12), 4, -6), (dict(head_dim=6, dtype=0), 4, -6),
