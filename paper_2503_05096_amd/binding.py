@@ -251,9 +251,16 @@ _ws_cache = {}
 _ws_retired = []
 
 
+def _on_device(t, device, what: str) -> None:
+    """A caller's buffer that kernels write to: an address of another device, or of the host, would be written to all the same."""
+    if t.device != device:
+        raise ValueError(f"{what} is on {t.device}, the call's tensors are on {device}")
+
+
 def _workspace(nbytes: int, device, workspace, family: str):
     import torch
     if workspace is not None:
+        _on_device(workspace, device, "workspace=")
         return workspace
     key = (str(device), family)
     ws = _ws_cache.get(key)
@@ -322,7 +329,10 @@ def verify_attn(q, k_pages, v_pages, block_table, ctx_lens, spec_lens, out=None,
         assert t.is_cuda and t.is_contiguous()
     assert block_table.dtype == torch.int32 and ctx_lens.dtype == torch.int32 and spec_lens.dtype == torch.int32
     assert v_pages.shape == k_pages.shape and v_pages.dtype == k_pages.dtype == q.dtype
-    if out is None and plan != "build":
+    assert k_pages.shape[3] == q.shape[2]
+    if out is not None:
+        _on_device(out, q.device, "out")
+    elif plan != "build":
         out = torch.empty(q.shape, dtype=_torch_dtype(dims.out_dtype), device=q.device)
     L = lib()
     if window is not None:

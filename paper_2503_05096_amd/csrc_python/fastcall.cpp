@@ -164,7 +164,11 @@ void *stream_of(PyObject *stream)
 // the caller's workspace, or the default one of this device and call family
 at::Tensor workspace(PyObject *given, size_t nbytes, Family family, const at::Tensor &like)
 {
-    if (given != Py_None) return tensor(given);
+    if (given != Py_None) {
+        const at::Tensor &t = tensor(given);
+        need(device_index(t) == device_index(like));
+        return t;
+    }
     auto &all = workspaces[family];
     const size_t dev = (size_t)device_index(like);
     if (dev < all.size() && all[dev].defined() && (size_t)all[dev].numel() >= nbytes) return all[dev];
@@ -258,7 +262,7 @@ PyObject *verify_attn(PyObject *, PyObject *const *a, Py_ssize_t nargs)
         const at::Tensor &q = tensor(a[0]), &k = tensor(a[1]), &v = tensor(a[2]);
         const at::Tensor &bt = dense(a[3], at::kInt), &ctx = dense(a[4], at::kInt), &spec = dense(a[5], at::kInt);
         need(q.dim() == 3 && k.dim() == 4 && bt.dim() == 2 && q.is_contiguous() && k.is_contiguous() && v.is_contiguous());
-        need(v.sizes() == k.sizes() && q.scalar_type() == k.scalar_type() && v.scalar_type() == k.scalar_type());
+        need(v.sizes() == k.sizes() && k.size(3) == q.size(2) && q.scalar_type() == k.scalar_type() && v.scalar_type() == k.scalar_type());
         adaspec_attn_dims d = {};
         d.batch = size32(bt.size(0));
         d.total_q = size32(q.size(0));
@@ -300,6 +304,7 @@ PyObject *verify_attn(PyObject *, PyObject *const *a, Py_ssize_t nargs)
             Py_RETURN_NONE;
         }
         const Output out(a[6], q.sizes(), scalar_type(d.out_dtype), q);
+        need(device_index(out.t) == device_index(q));
         run(ptr(out.t));
         return out.result();
     });
@@ -314,7 +319,7 @@ PyObject *verify_attn_window(PyObject *, PyObject *const *a, Py_ssize_t nargs)
         const at::Tensor &bt = dense(a[3], at::kInt), &ctx = dense(a[4], at::kInt), &spec = dense(a[5], at::kInt);
         need(q.dim() == 3 && k.dim() == 4 && bt.dim() == 2 && ctx.dim() == 1 && spec.dim() == 1);
         need(q.is_contiguous() && k.is_contiguous() && v.is_contiguous() && ctx.size(0) == bt.size(0) && spec.size(0) == bt.size(0));
-        need(v.sizes() == k.sizes() && q.scalar_type() == k.scalar_type() && v.scalar_type() == k.scalar_type());
+        need(v.sizes() == k.sizes() && k.size(3) == q.size(2) && q.scalar_type() == k.scalar_type() && v.scalar_type() == k.scalar_type());
         adaspec_attn_dims d = {};
         d.batch = size32(bt.size(0));
         d.total_q = size32(q.size(0));
@@ -334,7 +339,7 @@ PyObject *verify_attn_window(PyObject *, PyObject *const *a, Py_ssize_t nargs)
         need(nbytes > 0);
         on_current_device({&q, &k, &v, &bt, &ctx, &spec});
         const Output out(a[6], q.sizes(), scalar_type(d.out_dtype), q);
-        need(out.t.is_contiguous() && out.t.sizes() == q.sizes() && out.t.scalar_type() == scalar_type(d.out_dtype));
+        need(out.t.is_contiguous() && out.t.sizes() == q.sizes() && out.t.scalar_type() == scalar_type(d.out_dtype) && device_index(out.t) == device_index(q));
         const at::Tensor ws = workspace(a[11], nbytes, kAttn, q);
         void *s = stream_of(a[12]);
         call("adaspec_verify_attn_window", api.attn_window, ptr(q), ptr(k), ptr(v), ptr<int32_t>(bt), ptr<int32_t>(ctx), ptr<int32_t>(spec), ptr(out.t), &d,
