@@ -241,8 +241,8 @@ def _stream_ptr(stream) -> int:
     return int(s.cuda_stream)
 
 
-# Default workspaces: one per (device, call family), grown on demand.  Attention, acceptance and draft
-# sampling never share one (a planned attention pass keeps its metadata in its workspace across calls).
+# Default workspaces of attention, acceptance and draft sampling: one per (device, call family), grown on demand.
+# The three never share one (a planned attention pass keeps its metadata in its workspace across calls).
 # A buffer that is outgrown stays referenced until the process ends: a kernel on a caller-supplied,
 # non-current stream may still be using it, and torch's allocator would hand a freed block to the next
 # tensor at once.  Callers that issue calls on several streams must pass their own `workspace` per
@@ -270,6 +270,20 @@ def _workspace(nbytes: int, device, workspace, family: str):
         ws = torch.empty(max(nbytes, 1 << 20), dtype=torch.uint8, device=device)
         _ws_cache[key] = ws
     return ws
+
+
+def _scratch(nbytes: int, device, workspace, stream):
+    """The caller's workspace, or memory of this call alone: what its kernels leave there for each other is safe from calls on other
+    streams, from other threads and from graphs that are replayed meanwhile.  It is allocated on the call's stream, to whose memory it
+    goes back when the call has been made, behind its kernels."""
+    import torch
+    if workspace is not None:
+        _on_device(workspace, device, "workspace=")
+        return workspace
+    if stream is not None and not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(int(stream.cuda_stream), device=device)
+    with torch.cuda.stream(stream):                     # (None: the current one)
+        return torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
 
 
 def _with_timing(dims, timing):
@@ -305,7 +319,9 @@ def verify_attn(q, k_pages, v_pages, block_table, ctx_lens, spec_lens, out=None,
     parents [TQ] int32 (a draft tree): adaspec_verify_attn_tree instead.
     window, sinks: adaspec_verify_attn_window instead: a row sees the last `window` tokens up to its own and the request's
     first `sinks`; block_table entries of pages that no row sees are never read.  Not with parents.  Such a call has no plan of
-    its own and overwrites its workspace: not the one that holds a plan for calls without a window."""
+    its own and overwrites its workspace: not the one that holds a plan for calls without a window.
+    workspace: calls without a window share a default one per device, and have to be ordered on one stream; on several streams each
+    needs its own.  Windowed calls without workspace= may overlap: each that keeps something there has its own."""
     if window is not None or sinks != 0:
         if window is None:
             raise ValueError("verify_attn(sinks=...) needs a window: without one every token is visible")
@@ -381,7 +397,8 @@ def _verify_attn_window(q, k_pages, v_pages, block_table, ctx_lens, spec_lens, o
     if plan != "run" and workspace is None:
         raise ValueError("verify_attn(plan='build' / 'reuse') needs an explicit workspace= tensor that the "
                          "caller keeps for the whole pass")
-    ws = _workspace(need, q.device, workspace, "attn")
+    # (256 bytes: the call is not cut into parts, and writes none of them)
+    ws = _scratch(need, q.device, workspace, stream) if need > 256 else _workspace(need, q.device, workspace, "attn")
     rc = L.adaspec_verify_attn_window(q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), block_table.data_ptr(),
                                       ctx_lens.data_ptr(), spec_lens.data_ptr(), None if out is None else out.data_ptr(),
                                       C.byref(dims), window, sinks, ws.data_ptr(), ws.numel(), _stream_ptr(stream))
@@ -425,7 +442,8 @@ def accept_resolved_path(target_logits, draft_probs, draft_tokens, spec_lens, *,
 def accept(target_logits, draft_probs, draft_tokens, uniforms, spec_lens, temperature, *,
            max_spec_len: int, out_tokens=None, out_accept_len=None, out_stride: Optional[int] = None,
            path: str = "auto", workspace=None, stream=None, timing=None) -> Tuple[object, object]:
-    """adaspec_accept on device tensors; returns (out_tokens [B][out_stride], out_accept_len [B])."""
+    """adaspec_accept on device tensors; returns (out_tokens [B][out_stride], out_accept_len [B]).
+    workspace: the default one is shared by all calls of a device, which have to be ordered on one stream (accept_tree too)."""
     if path == "auto" and timing is None:
         r = (_fast or _native()).accept(target_logits, draft_probs, draft_tokens, uniforms, spec_lens, temperature,
                                         max_spec_len, out_tokens, out_accept_len, out_stride, workspace, stream)
@@ -677,7 +695,8 @@ def kv_remap(block_table, page_refs, sources, lens, new_lens, *, window: Optiona
 
     block_table [old_batch][max_pages], page_refs [num_pages], sources [batch], lens [old_batch], new_lens [batch], all int32.
     window, sinks: pages that no later row of verify_attn(window=, sinks=) sees are given back as well.  out_refs may be
-    page_refs; out_table must not overlap block_table.  Results that are not given are new tensors, of one allocation."""
+    page_refs; out_table must not overlap block_table.  Results that are not given are new tensors of one allocation, which lasts, with
+    the call's workspace behind them, until the last of them is gone.  Calls without workspace= may overlap: each has its own."""
     if window is None and sinks != 0:
         raise ValueError("kv_remap(sinks=...) needs a window: without one every token is visible")
     if window is not None and window < 1:
@@ -699,7 +718,7 @@ def kv_remap(block_table, page_refs, sources, lens, new_lens, *, window: Optiona
     status = _ints_like(status, (2,), block_table)
     dims = PagesDims(batch, old_batch, max_pages, num_pages, int(page_size), window, sinks, 0)
     L = lib()
-    ws = _workspace(L.adaspec_kv_remap_workspace_bytes(C.byref(dims)), block_table.device, workspace, "pages")
+    ws = _scratch(L.adaspec_kv_remap_workspace_bytes(C.byref(dims)), block_table.device, workspace, stream)
     rc = L.adaspec_kv_remap(block_table.data_ptr(), page_refs.data_ptr(), sources.data_ptr(), lens.data_ptr(), new_lens.data_ptr(),
                             out_table.data_ptr(), out_refs.data_ptr(), copy_src.data_ptr(), copy_dst.data_ptr(), status.data_ptr(),
                             C.byref(dims), ws.data_ptr(), ws.numel(), _stream_ptr(stream))
@@ -712,8 +731,7 @@ def kv_compact_pages(block_table, page_refs, *, max_moves: Optional[int] = None,
                      copy_src=None, copy_dst=None, status=None, page_size: int = 16, workspace=None, stream=None):
     """adaspec_kv_compact_pages: used pages to the front of the pool; returns (out_table, out_refs, page_map [num_pages],
     copy_src [max_moves], copy_dst [max_moves], status [2]).  max_moves: half of the pool's pages unless given, which is always
-    enough.  out_table may be block_table, out_refs may be page_refs.  Results that are not given are new tensors, of one
-    allocation."""
+    enough.  out_table may be block_table, out_refs may be page_refs.  Results and workspace as for kv_remap."""
     batch, max_pages = block_table.shape
     num_pages = page_refs.shape[0]
     max_moves = max(1, num_pages // 2) if max_moves is None else int(max_moves)
@@ -734,7 +752,7 @@ def kv_compact_pages(block_table, page_refs, *, max_moves: Optional[int] = None,
     status = _ints_like(status, (2,), block_table)
     dims = PagesDims(0, batch, max_pages, num_pages, int(page_size), 0, 0, max_moves)
     L = lib()
-    ws = _workspace(L.adaspec_kv_compact_pages_workspace_bytes(C.byref(dims)), block_table.device, workspace, "pages")
+    ws = _scratch(L.adaspec_kv_compact_pages_workspace_bytes(C.byref(dims)), block_table.device, workspace, stream)
     rc = L.adaspec_kv_compact_pages(block_table.data_ptr(), page_refs.data_ptr(), out_table.data_ptr(), out_refs.data_ptr(),
                                     page_map.data_ptr(), copy_src.data_ptr(), copy_dst.data_ptr(), status.data_ptr(), C.byref(dims),
                                     ws.data_ptr(), ws.numel(), _stream_ptr(stream))
@@ -767,7 +785,8 @@ def kv_copy_pages(k_pages, v_pages, copy_src, copy_dst, *, stream=None) -> None:
 def draft_sample(draft_logits, temperature, uniforms, *, probs_dtype=None, draft_probs=None, out_rows=None,
                  draft_tokens=None, confidence=None, path: str = "auto", workspace=None, stream=None, timing=None):
     """adaspec_draft_sample; returns (draft_probs, draft_tokens [R] int32, confidence [R] float32).
-    path "split" (ADASPEC_PATH_TWO_PASS for this call) shares long rows between workgroups."""
+    path "split" (ADASPEC_PATH_TWO_PASS for this call) shares long rows between workgroups.
+    workspace: the default one is shared by all calls of a device, which have to be ordered on one stream."""
     if path == "auto" and timing is None:
         r = (_fast or _native()).draft_sample(draft_logits, temperature, uniforms, probs_dtype, draft_probs, out_rows,
                                               draft_tokens, confidence, workspace, stream)

@@ -12,8 +12,10 @@
 // workspaces are binding.py's as well (one owner for both ways into the library), held here by reference.
 #include <ATen/ATen.h>
 #include <ATen/PythonTorchFunctionTLS.h>
+#include <c10/core/StreamGuard.h>
 #include <c10/core/impl/TorchDispatchModeTLS.h>
 #include <torch/csrc/Dtype.h>
+#include <torch/csrc/Stream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <array>
@@ -72,8 +74,8 @@ PyObject *error_class;                                   // binding.AdaspecError
 bool ready = false;
 
 // the default workspaces in use: [family][device], the tensors of binding._ws_cache
-enum Family { kAttn, kAccept, kDraft, kPages, kFamilies };
-const char *const kFamilyName[kFamilies] = {"attn", "accept", "draft", "pages"};
+enum Family { kAttn, kAccept, kDraft, kFamilies };
+const char *const kFamilyName[kFamilies] = {"attn", "accept", "draft"};
 // (never destroyed: at process exit the allocator may be gone before a static's destructor runs)
 auto &workspaces = *new std::array<std::vector<at::Tensor>, kFamilies>;
 
@@ -161,14 +163,17 @@ void *stream_of(PyObject *stream)
     return p;
 }
 
+const at::Tensor &given_workspace(PyObject *given, const at::Tensor &like)
+{
+    const at::Tensor &t = tensor(given);
+    need(device_index(t) == device_index(like));
+    return t;
+}
+
 // the caller's workspace, or the default one of this device and call family
 at::Tensor workspace(PyObject *given, size_t nbytes, Family family, const at::Tensor &like)
 {
-    if (given != Py_None) {
-        const at::Tensor &t = tensor(given);
-        need(device_index(t) == device_index(like));
-        return t;
-    }
+    if (given != Py_None) return given_workspace(given, like);
     auto &all = workspaces[family];
     const size_t dev = (size_t)device_index(like);
     if (dev < all.size() && all[dev].defined() && (size_t)all[dev].numel() >= nbytes) return all[dev];
@@ -189,6 +194,19 @@ at::Tensor workspace(PyObject *given, size_t nbytes, Family family, const at::Te
 at::Tensor empty(at::IntArrayRef shape, at::ScalarType dt, const at::Tensor &like)
 {
     return at::empty(shape, at::TensorOptions().dtype(dt).device(like.device()));
+}
+// The caller's workspace, or memory of this call alone (binding._scratch): allocated on the call's stream, to whose memory it goes
+// back when the call has been made, behind its kernels.
+at::Tensor scratch(PyObject *given, size_t nbytes, PyObject *stream, const at::Tensor &like)
+{
+    if (given != Py_None) return given_workspace(given, like);
+    if (stream == Py_None) return empty({(int64_t)nbytes}, at::kByte, like);
+    need(THPStream_Check(stream));
+    const THPStream *s = reinterpret_cast<const THPStream *>(stream);
+    const c10::Stream on = c10::Stream::unpack3(s->stream_id, (c10::DeviceIndex)s->device_index, (c10::DeviceType)s->device_type);
+    need(on.device() == like.device());
+    const c10::StreamGuard guard(on);
+    return empty({(int64_t)nbytes}, at::kByte, like);
 }
 // an output argument: the caller's object (checked by nobody but the library, as in Python) or a new tensor, whose Python
 // object exists before the call is made: after it nothing may fail that could send the call to Python again
@@ -310,6 +328,8 @@ PyObject *verify_attn(PyObject *, PyObject *const *a, Py_ssize_t nargs)
     });
 }
 
+constexpr size_t kNothingKept = 256;                  // bytes that a windowed call asks for where it is not cut into parts: it writes none of them
+
 // (q, k_pages, v_pages, block_table, ctx_lens, spec_lens, out, max_spec_len, scale, out_dtype, plan, workspace, stream, window, sinks)
 PyObject *verify_attn_window(PyObject *, PyObject *const *a, Py_ssize_t nargs)
 {
@@ -340,7 +360,7 @@ PyObject *verify_attn_window(PyObject *, PyObject *const *a, Py_ssize_t nargs)
         on_current_device({&q, &k, &v, &bt, &ctx, &spec});
         const Output out(a[6], q.sizes(), scalar_type(d.out_dtype), q);
         need(out.t.is_contiguous() && out.t.sizes() == q.sizes() && out.t.scalar_type() == scalar_type(d.out_dtype) && device_index(out.t) == device_index(q));
-        const at::Tensor ws = workspace(a[11], nbytes, kAttn, q);
+        const at::Tensor ws = nbytes > kNothingKept ? scratch(a[11], nbytes, a[12], q) : workspace(a[11], nbytes, kAttn, q);
         void *s = stream_of(a[12]);
         call("adaspec_verify_attn_window", api.attn_window, ptr(q), ptr(k), ptr(v), ptr<int32_t>(bt), ptr<int32_t>(ctx), ptr<int32_t>(spec), ptr(out.t), &d,
              window, sinks, ptr(ws), (size_t)ws.numel(), s);
@@ -349,21 +369,33 @@ PyObject *verify_attn_window(PyObject *, PyObject *const *a, Py_ssize_t nargs)
 }
 
 // Integer outputs: the caller's tensors of exactly these shapes; the new ones share one allocation, from which each begins at
-// 256 bytes (an allocation of its own costs each of them 0.7 us, and these calls have five or six).
+// 256 bytes (an allocation of its own costs each of them 0.7 us, and these calls have five or six).  The workspace of a call on the
+// current stream is the end of it, unless the caller gave one.
 template <int N> struct Ints {
     struct Spec { PyObject *given; c10::SmallVector<int64_t, 2> shape; };
-    at::Tensor t[N];
+    at::Tensor t[N], whole, ws;
+    void *ws_ptr = nullptr;
+    size_t ws_bytes;
     PyObject *object[N] = {};
-    Ints(const at::Tensor &like, std::initializer_list<Spec> all)
+    Ints(const at::Tensor &like, std::initializer_list<Spec> all, PyObject *workspace, size_t nbytes, PyObject *stream) : ws_bytes(nbytes)
     {
+        const bool shares = workspace == Py_None && stream == Py_None;
         int64_t total = 0, at_[N];
         int i = 0;
         for (const Spec &w : all) {
             at_[i++] = total;
             if (w.given == Py_None) total += (c10::multiply_integers(w.shape) + 63) / 64 * 64;
         }
-        at::Tensor whole;
+        const int64_t results = total;
+        if (shares) total += ((int64_t)nbytes + 3) / 4;
         if (total > 0) whole = empty({total}, at::kInt, like);
+        if (shares) {
+            ws_ptr = static_cast<char *>(whole.data_ptr()) + results * 4;
+        } else {
+            ws = scratch(workspace, nbytes, stream, like);
+            ws_ptr = ptr(ws);
+            ws_bytes = (size_t)ws.numel();
+        }
         i = 0;
         for (const Spec &w : all) {
             if (w.given != Py_None) {
@@ -419,11 +451,11 @@ PyObject *kv_remap(PyObject *, PyObject *const *a, Py_ssize_t nargs)
         const size_t nbytes = api.remap_ws(&d);
         need(nbytes > 0);
         on_current_device({&bt, &refs, &src, &lens, &more});
-        const Ints<5> out(bt, {{a[8], {d.batch, d.max_pages_per_req}}, {a[9], {d.num_pages}}, {a[10], {d.batch}}, {a[11], {d.batch}}, {a[12], {2}}});
-        const at::Tensor ws = workspace(a[13], nbytes, kPages, bt);
+        const Ints<5> out(bt, {{a[8], {d.batch, d.max_pages_per_req}}, {a[9], {d.num_pages}}, {a[10], {d.batch}}, {a[11], {d.batch}}, {a[12], {2}}},
+                          a[13], nbytes, a[14]);
         void *s = stream_of(a[14]);
         call("adaspec_kv_remap", api.remap, ptr<int32_t>(bt), ptr<int32_t>(refs), ptr<int32_t>(src), ptr<int32_t>(lens), ptr<int32_t>(more),
-             out[0], out[1], out[2], out[3], out[4], &d, ptr(ws), (size_t)ws.numel(), s);
+             out[0], out[1], out[2], out[3], out[4], &d, out.ws_ptr, out.ws_bytes, s);
         return out.result();
     });
 }
@@ -446,10 +478,10 @@ PyObject *kv_compact_pages(PyObject *, PyObject *const *a, Py_ssize_t nargs)
         on_current_device({&bt, &refs});
         need(d.max_moves >= 0);
         const Ints<6> out(bt, {{a[4], {d.old_batch, d.max_pages_per_req}}, {a[5], {d.num_pages}}, {a[6], {d.num_pages}},
-                               {a[7], {d.max_moves}}, {a[8], {d.max_moves}}, {a[9], {2}}});
-        const at::Tensor ws = workspace(a[10], nbytes, kPages, bt);
+                               {a[7], {d.max_moves}}, {a[8], {d.max_moves}}, {a[9], {2}}},
+                          a[10], nbytes, a[11]);
         void *s = stream_of(a[11]);
-        call("adaspec_kv_compact_pages", api.compact, ptr<int32_t>(bt), ptr<int32_t>(refs), out[0], out[1], out[2], out[3], out[4], out[5], &d, ptr(ws), (size_t)ws.numel(), s);
+        call("adaspec_kv_compact_pages", api.compact, ptr<int32_t>(bt), ptr<int32_t>(refs), out[0], out[1], out[2], out[3], out[4], out[5], &d, out.ws_ptr, out.ws_bytes, s);
         return out.result();
     });
 }
