@@ -412,7 +412,7 @@ int adaspec_commit(const int32_t *out_tokens, const int32_t *out_accept_len,
  * shared: the caller makes room and calls again with the new table, every row
  * its own source.  Such a row must not be written to meanwhile.
  * Lengths are cut to [0, max_pages_per_req * page_size], at most 2^30; ids outside
- * the pool hold nothing.  batch + old_batch <= 65535, and
+ * the pool hold nothing.  batch + old_batch <= 65535, num_pages <= 2^24 and
  * batch * (max_pages_per_req + 1) below 2^30.  No call reads K or V.
  * ---------------------------------------------------------------------- */
 typedef struct {

@@ -792,7 +792,8 @@ static int validate_pages_dims(const adaspec_pages_dims *d, bool remap)
     if (d->old_batch < 0 || d->max_pages_per_req <= 0 || d->num_pages <= 0 || d->page_size <= 0) return ADASPEC_ERR_DIM;
     if (remap && (d->batch < 0 || d->window < 0 || d->sinks < 0)) return ADASPEC_ERR_DIM;
     if (!remap && (d->max_moves < 1 || d->max_moves > d->num_pages)) return ADASPEC_ERR_DIM;
-    if (!remap && d->num_pages > 1 << 21) return ADASPEC_ERR_UNSUPPORTED;       // (the bases of its parts fit the kernels' LDS)
+    // (compaction: the bases of its parts fit the kernels' LDS.  Remap: every workgroup adds up the free pages of all chunks of 1024)
+    if (d->num_pages > (remap ? 1 << 24 : 1 << 21)) return ADASPEC_ERR_UNSUPPORTED;
     if ((int64_t)d->max_pages_per_req * d->page_size > (1 << 30)) return ADASPEC_ERR_UNSUPPORTED;
     if (remap && (int64_t)d->old_batch + d->batch > 65535) return ADASPEC_ERR_UNSUPPORTED;
     if (remap && d->batch * ((int64_t)d->max_pages_per_req + 1) >= (1 << 30)) return ADASPEC_ERR_UNSUPPORTED;       // (wants are counted in 32 bits)
