@@ -218,6 +218,7 @@ struct WindowArgs {
 WindowPlan make_window_plan(const adaspec_attn_dims &d, int window, int sinks);
 bool window_fast_supported(const adaspec_attn_dims &d);
 hipError_t launch_attn_window(const WindowArgs &a);
+hipError_t launch_attn_window_combine(const WindowArgs &a);         // behind it, where units are cut into parts
 
 // ---- accept workspace ------------------------------------------------------
 struct AcceptPlan {

@@ -494,6 +494,7 @@ int adaspec_verify_attn_window(const void *q, const void *k_pages, const void *v
     if (!record_event(dims->timing_start, dims->timing_stop, true, a.stream)) return ADASPEC_ERR_HIP;
     if (launch_attn_window(a) != hipSuccess) return ADASPEC_ERR_HIP;
     if (!record_event(dims->timing_start, dims->timing_stop, false, a.stream)) return ADASPEC_ERR_HIP;
+    if (a.plan.splits > 1 && launch_attn_window_combine(a) != hipSuccess) return ADASPEC_ERR_HIP;
     return ADASPEC_OK;
 }
 

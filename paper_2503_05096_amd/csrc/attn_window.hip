@@ -345,24 +345,33 @@ WindowPlan make_window_plan(const adaspec_attn_dims &d, int window, int sinks)
     return p;
 }
 
+static WindowDims window_dims(const WindowArgs &a)
+{
+    const adaspec_attn_dims &d = a.dims;
+    return {a.block_table, a.ctx_lens, a.spec_lens, d.batch, d.total_q, d.max_spec_len, d.max_pages_per_req, d.n_q_heads, d.n_kv_heads, a.window,
+            a.sinks, a.plan.groups, a.plan.rows_per_group};
+}
+
+hipError_t launch_attn_window_combine(const WindowArgs &a)
+{
+    const adaspec_attn_dims &d = a.dims;
+    const WindowPlan &p = a.plan;
+    auto combine = [&](auto dim) {
+        hipLaunchKernelGGL((attn_window_combine_kernel<decltype(dim)::value>),
+                           dim3((unsigned)(d.batch * p.groups), d.n_kv_heads, p.rows_per_group / 4), dim3(256), 0, a.stream, window_dims(a), (const float *)(a.ws + p.off_part_ml), (const float *)(a.ws + p.off_part_o), a.out, p.splits,
+                           p.block_pages, d.out_dtype);
+    };
+    if (d.head_dim == 128) combine(std::integral_constant<int, 128>{});
+    else combine(std::integral_constant<int, 64>{});
+    return hipGetLastError();
+}
+
 hipError_t launch_attn_window(const WindowArgs &a)
 {
     const adaspec_attn_dims &d = a.dims;
-    const WindowDims w{a.block_table, a.ctx_lens, a.spec_lens, d.batch, d.total_q, d.max_spec_len, d.max_pages_per_req, d.n_q_heads,
-                       d.n_kv_heads, a.window, a.sinks, a.plan.groups, a.plan.rows_per_group};
+    const WindowDims w = window_dims(a);
     const WindowPlan &p = a.plan;
-    if (p.kind == WindowKind::kMfma) {
-        const hipError_t e = d.dtype == ADASPEC_F32 ? launch_attn_window_f32(a, w) : launch_attn_window_mfma(a, w);
-        if (e != hipSuccess || p.splits == 1) return e;
-        auto combine = [&](auto dim) {
-            hipLaunchKernelGGL((attn_window_combine_kernel<decltype(dim)::value>),
-                               dim3((unsigned)(d.batch * p.groups), d.n_kv_heads, p.rows_per_group / 4), dim3(256), 0, a.stream, w, (const float *)(a.ws + p.off_part_ml), (const float *)(a.ws + p.off_part_o), a.out, p.splits,
-                               p.block_pages, d.out_dtype);
-        };
-        if (d.head_dim == 128) combine(std::integral_constant<int, 128>{});
-        else combine(std::integral_constant<int, 64>{});
-        return hipGetLastError();
-    }
+    if (p.kind == WindowKind::kMfma) return d.dtype == ADASPEC_F32 ? launch_attn_window_f32(a, w) : launch_attn_window_mfma(a, w);
     auto launch = [&](auto tag, auto pairs, auto rows) {
         hipLaunchKernelGGL((attn_window_vector_kernel<decltype(tag), decltype(pairs)::value, decltype(rows)::value>),
                            dim3((unsigned)(d.batch * a.plan.groups), d.n_kv_heads), dim3(64 * kWinWaves), 0, a.stream, w, a.q, a.k_pages, a.v_pages, a.out,
