@@ -177,14 +177,30 @@ __global__ __launch_bounds__(kPagesThreads) void remap_count_kernel(RemapArgs a)
     if (tid == 0) a.tile_wants[tile] = total;
 }
 
-// Everything up to here in one launch, where the old table and both batches are small (every workgroup reads the whole old
-// table; whole calls of 64 requests, this way / in three launches: 8.8/13.5 us with 2112 entries, 11.6/13.5 with 32832, 14.0/13.6 with
-// 65664, 18.1/13.6 with 131200; of 256 requests 12.5/13.7 with 32768, 14.5/13.6 with 65536): a workgroup per 1024 pages goes through
-// the whole old table and keeps the counts of its own pages in LDS, so that nobody has to wait for anybody.  It also decides
-// what those rows want that are about to write into one of its pages (the first workgroup: into none that holds tokens).  The
+// Everything up to here in one launch, where the old table and both batches are small: a workgroup per 1024 pages goes through the
+// whole old table and keeps the counts of its own pages in LDS, so that nobody has to wait for anybody.  It also decides what
+// those rows want that are about to write into one of its pages (the first workgroup: into none that holds tokens).  The
 // workgroups behind write a new row each.
+//
+// Up to 512 of these workgroups, two per compute unit, run at once, and the table's length decides; beyond that each further
+// round of them reads the table again, and its length times the number of workgroups does.  Rows count a little: every workgroup
+// looks up where each of them writes.  Whole calls (us), this way / in three launches, all rows in use as far as the pool goes:
+//   table entries                   2048       12288      24576      36864      49152      65536
+//     64 rows, pool of   65536   8.8/14.5   8.8/14.2   9.2/14.1  10.5/14.8  10.8/14.9  12.7/14.6
+//     64 rows, pool of  524288   8.8/14.5   9.7/14.3  10.0/14.4  12.0/14.4  12.9/14.6  15.0/14.5
+//     64 rows, pool of 1048576  11.1/16.2  13.4/15.8  15.3/16.0  18.8/16.1  20.8/16.1  24.5/16.5
+//     64 rows, pool of 2097152  17.3/21.6  21.8/22.3  25.1/22.2  31.6/22.1  35.4/22.5  42.5/23.1
+//     64 rows, pool of 8388608  67.8/69.6  85.5/69.7  95.9/69.7   117/70.2   131/69.7   158/70.2
+//   1024 rows, pool of   65536   9.2/13.9   9.4/14.0  10.4/14.0  11.6/14.0  12.5/14.4  13.6/14.7
+//   1024 rows, pool of  524288  11.0/15.2  12.2/14.7  13.6/15.3  15.7/15.1  16.8/14.9  18.4/15.1
+//   1024 rows, pool of 1048576  14.7/18.6  17.7/18.5  20.5/18.6  24.4/18.7  26.8/18.6  29.9/18.5
 constexpr int kSmallRows = 1024;
-constexpr int64_t kSmallEntries = 49152;
+constexpr int64_t kSmallEntries = 49152, kSmallReads = 26 << 20;
+static bool remap_is_small(const adaspec_pages_dims &d, int chunks)
+{
+    const int64_t entries = (int64_t)d.old_batch * d.max_pages_per_req;
+    return d.old_batch <= kSmallRows && d.batch <= kSmallRows && entries <= kSmallEntries && chunks * entries + 8192 * (int64_t)d.batch <= kSmallReads;
+}
 constexpr int kScan = 2;                    // loads of four entries that a thread has under way
 static_assert(kSmallRows == kChunk, "a thread per row");
 __global__ __launch_bounds__(kChunk) void remap_small_kernel(RemapArgs a)
@@ -402,7 +418,7 @@ size_t remap_workspace(const adaspec_pages_dims &d, RemapArgs *a, char *ws)
 hipError_t launch_kv_remap(const RemapArgs &a, hipStream_t stream)
 {
     const adaspec_pages_dims &d = a.dims;
-    if (d.old_batch <= kSmallRows && d.batch <= kSmallRows && (int64_t)d.old_batch * d.max_pages_per_req <= kSmallEntries) {
+    if (remap_is_small(d, a.chunks)) {
         hipLaunchKernelGGL(remap_small_kernel, dim3(a.chunks + d.batch), dim3(kChunk), 0, stream, a);
     } else {
         hipLaunchKernelGGL(remap_start_kernel, dim3(a.chunks), dim3(kPagesThreads), 0, stream, a);

@@ -48,8 +48,10 @@ d = Dims()
 for item in sys.argv[4].split(","):
     name, value = item.split("=")
     setattr(d, name, int(value))
-p = [C.c_void_p(0x100000000 * (k + 1)) for k in range(8)]
-if sys.argv[5] == "window":
+p = [C.c_void_p(0x100000000 * (k + 1)) for k in range(11)]
+if sys.argv[5] == "remap":
+    rc = L.adaspec_kv_remap(*p[:10], C.byref(d), p[10], C.c_size_t(1 << 40), C.c_void_p(0x77))
+elif sys.argv[5] == "window":
     rc = L.adaspec_verify_attn_window(*p[:7], C.byref(d), C.c_int32(3000), C.c_int32(4), p[7], C.c_size_t(1 << 30), C.c_void_p(0x77))
 else:
     rc = L.adaspec_verify_attn(*p[:7], C.byref(d), p[7], C.c_size_t(1 << 30), C.c_void_p(0x77))
@@ -65,16 +67,20 @@ def runtime(tmp_path_factory):
     return str(at / "libhip_stub.so")
 
 
+def lines(runtime, which, fields, dims):
+    """what the library's call of these dims enqueues"""
+    r = subprocess.run([sys.executable, "-c", CALL, runtime, LIB_PATH, ",".join(n for n, _ in fields), ",".join(f"{k}={v}" for k, v in dims.items()),
+                        which], capture_output=True, text=True, timeout=120, env={**os.environ, "PYTHONPATH": ""})
+    assert r.returncode == 0, r.stderr
+    return [line for line in r.stdout.split("\n") if line]
+
+
 def enqueued(runtime, which, **kw):
     base = dict(batch=1, total_q=6, max_spec_len=5, n_q_heads=32, n_kv_heads=8, head_dim=128, page_size=16, num_pages=4096, max_pages_per_req=4000,
                 dtype=binding.BF16, out_dtype=binding.BF16, timing_start=0xa0, timing_stop=0xb0)
     base.update(kw)
-    names = ",".join(n for n, _ in binding.AttnDims._fields_)
-    r = subprocess.run([sys.executable, "-c", CALL, runtime, LIB_PATH, names, ",".join(f"{k}={v}" for k, v in base.items()), which],
-                       capture_output=True, text=True, timeout=120, env={**os.environ, "PYTHONPATH": ""})
-    assert r.returncode == 0, r.stderr
     return [line if line.startswith("event") else "combine" if "combine" in line else "plan" if "plan" in line else "main" if "attn" in line else line
-            for line in r.stdout.split("\n") if line]
+            for line in lines(runtime, which, binding.AttnDims._fields_, base)]
 
 
 START, STOP = "event 0xa0 on 0x77", "event 0xb0 on 0x77"
@@ -96,3 +102,16 @@ def test_events_of_calls_without_a_window(runtime):
     got = enqueued(runtime, "plain", batch=4, total_q=24)
     assert got.index(START) + 1 == got.index("main") == got.index(STOP) - 1 and set(got[:got.index(START)]) <= {"plan"}
     assert set(got[got.index(STOP) + 1:]) <= {"combine"}
+
+
+@pytest.mark.parametrize("pages,rows,width,small", [
+    (65536, 64, 768, True), (65536, 64, 769, False), (65536, 1024, 48, True), (65536, 1025, 4, False),
+    (1 << 19, 64, 768, True), (1 << 19, 1024, 36, True), (1 << 19, 1024, 40, False),
+    (1 << 20, 64, 400, True), (1 << 20, 64, 500, False), (1 << 21, 64, 180, True), (1 << 21, 64, 256, False), (1 << 21, 16, 3000, False),
+    (1 << 24, 64, 16, True), (1 << 24, 64, 32, False), (1 << 24, 1, 2000, False),
+])
+def test_form_of_remap(runtime, pages, rows, width, small):
+    """Two launches, of which every workgroup of the first reads the whole old table: only where that is not read too often."""
+    dims = dict(batch=rows, old_batch=rows, max_pages_per_req=width, num_pages=pages, page_size=16, window=0, sinks=0)
+    got = [next(n for n in ("small", "start", "rows", "count", "assign") if n in line) for line in lines(runtime, "remap", binding.PagesDims._fields_, dims)]
+    assert got == (["small", "assign"] if small else ["start", "rows", "count", "assign"])

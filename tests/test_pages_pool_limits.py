@@ -50,3 +50,22 @@ def test_remap_of_the_largest_pool(old):
     refs[5] = 0
     refs[expected[served].long()] = 1
     assert torch.equal(new_refs, refs) and (src == -1).all() and (dst == -1).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("width", [400, 500])           # (in two launches, in four)
+def test_remap_in_a_large_pool(width):
+    import numpy as np
+
+    from tests.test_gpu_kv_pages import check_remap, state
+    r = np.random.default_rng(width)
+    table, refs, held = state(r, 64, width, 16, slack=0)
+    ids = np.sort(r.permutation(1 << 20)[:len(refs)])   # the same batch with its pages all over a larger pool
+    table = np.where(table >= 0, ids[np.maximum(table, 0)], -1).astype(np.int32)
+    pool = (r.random(1 << 20) < 0.9).astype(np.int32)
+    pool[ids] = refs
+    lens = np.minimum(r.integers(0, width * 16 + 1, 64), held * 16)
+    sources = r.integers(-1, 64, 64)
+    new_lens = np.where(sources >= 0, lens[np.maximum(sources, 0)], 0) + r.integers(0, 60, 64)
+    print(f"[case] remap pool={len(pool)} width={width}", flush=True)
+    check_remap(pkg, table, pool, sources, lens, new_lens, window=900, sinks=20)
