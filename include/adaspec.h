@@ -404,13 +404,17 @@ int adaspec_commit(const int32_t *out_tokens, const int32_t *out_accept_len,
  *   out_table [batch][max_pages_per_req]   not block_table
  *   out_refs  [num_pages]                  the counts; may be page_refs itself
  *   copy_src, copy_dst [batch]             the pages of step 3: copy_dst[i] has to
- *                                          become a copy of copy_src[i] before it
+ *                                          become a copy of copy_src[i] before either
  *                                          is written (adaspec_kv_copy_pages), or -1
  *   status [2]                             free pages left; wants that could not
  *                                          be served
  * Where wants are left over, their entries stay -1 and pages of step 3 stay
- * shared: the caller makes room and calls again with the new table, every row
- * its own source.  Such a row must not be written to meanwhile.
+ * shared: the caller makes the copies that were served, makes room and calls
+ * again with the new table, every row its own source, lens as they are then.
+ * Meanwhile a row must not be written to unless all its entries are there and
+ * the page of its token n has one holder (out_refs): where rows of different
+ * lengths share that page, even the row that may keep it would write over
+ * tokens of another one, which still waits for its copy.
  * Lengths are cut to [0, max_pages_per_req * page_size], at most 2^30; ids outside
  * the pool hold nothing.  batch + old_batch <= 65535, num_pages <= 2^24 and
  * batch * (max_pages_per_req + 1) below 2^30.  No call reads K or V.
