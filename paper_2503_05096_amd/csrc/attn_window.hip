@@ -8,8 +8,8 @@
 // and is left out of that row's sum, not multiplied by zero: whatever it holds cannot reach the row.
 //
 // Its vector units bound it: 16 multiply-adds per value of K and of V that arrives, twice as many instructions with unpacking
-// and LDS; with few units the latency of a wavefront's turns does.  Window 1024, 32 requests of 16 rows at 8 kv heads: 72 us for
-// 102 MB (bf16, head_dim 96; one wavefront per unit, a value row at a time: 1125), 150 us for 273 MB (head_dim 256; 2236), 83 us
+// and LDS; with few units the latency of a wavefront's turns does.  Window 1024, 32 requests of 16 rows at 8 kv heads: 81 us for
+// 102 MB (bf16, head_dim 96; one wavefront per unit, a value row at a time: 1125), 172 us for 273 MB (head_dim 256; 2236), 92 us
 // for 204 MB (fp32, 96; 855).
 #include <type_traits>
 

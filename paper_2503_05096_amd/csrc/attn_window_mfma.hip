@@ -19,7 +19,9 @@
 // Memory bounds it, and around that the start of a generation of workgroups (7-8 us: launch, lengths, page ids, first block,
 // merge, store, one after the other).  128 requests of 128-4096 tokens, 32 query on 8 kv heads, up to 6 drafts, window 1024,
 // head_dim 128: 84 us for 495 MB (5.9 TB/s); 64 requests, 64 query heads, window 4096: 172 us, 6.3 TB/s, the rate of a large
-// read.  64 rows: 5.6 TB/s at window 4096, 4.8 at 1024 (matrix products and softmax of four row tiles by 8 wavefronts).
+// read (in a stream that has been busy for some hundred calls; up to 187 us before that).  64 rows: 5.7 TB/s at window 4096, 4.8 at
+// 1024 (matrix products and softmax of four row tiles by 8 wavefronts).  More rows: groups of equal numbers of tiles, of which a unit does
+// all, whether it has rows for them or not (72 rows are 48 and 24, both with three tiles).
 #include "attn_window_merge.h"
 
 namespace adaspec {
@@ -406,7 +408,7 @@ hipError_t launch_attn_window_mfma(const WindowArgs &a, const WindowDims &w)
                            a.scale_log2, d.out_dtype);
     };
     // Two row groups read the same pages: loads that leave them in the L2 (128 requests of 72 rows at 8 kv heads, head_dim 128,
-    // window 1024: 138 us, streaming loads 160; window 4096, 64 requests: 223 and 282).  Head_dim 64 gains nothing (93 us either
+    // window 1024: 139 us, streaming loads 160; window 4096, 64 requests: 222 and 282).  Head_dim 64 gains nothing (93 us either
     // way), and one group alone loses by them (32 rows, window 1024: 102 us instead of 91).
     auto with_rt = [&](auto tag, auto dim) {
         constexpr bool kMay = decltype(dim)::value == 128;

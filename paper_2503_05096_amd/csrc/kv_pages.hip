@@ -6,8 +6,9 @@
 //
 // The id calls move little (remap of 128 requests 0.8 MB, compaction of 262144 pages 5.2 MB): launches and chains of dependent
 // accesses bound them, so they are few launches with everything in flight that can be.  Whole calls from Python: remap of
-// 128 requests of up to 8192 tokens 13-16 us (four kernels of 2.6, 3.6, 2.4 and 4.2), of 16 into 256 forks 10.8 (5.4 and 5.5),
-// compaction of 2048 pages 6 us (one of 5.3), of 262144 pages 9.7 us (2.3 and 8.7).
+// 128 requests of up to 8192 tokens 13-16 us (four kernels of 3.0, 4.0, 2.8 and 4.8), of 16 into 256 forks 10.7 (5.8 and 5.4),
+// compaction of 2048 pages 5.3-5.9 us (one of 5.3), of 262144 pages 9.5-9.8 us (2.4 and 8.5).  (Kernels under the profiler, in a busy
+// stream: about 3 us of each are its boundary, and they overlap a little.)
 #include "adaspec_internal.h"
 #include "device_utils.h"
 
@@ -184,7 +185,9 @@ __global__ __launch_bounds__(kPagesThreads) void remap_count_kernel(RemapArgs a)
 //
 // Up to 512 of these workgroups, two per compute unit, run at once, and the table's length decides; beyond that each further
 // round of them reads the table again, and its length times the number of workgroups does.  Rows count a little: every workgroup
-// looks up where each of them writes.  Whole calls (us), this way / in three launches, all rows in use as far as the pool goes:
+// looks up where each of them writes.  The look-ups of one workgroup are shared out by the table's places: short rows in a wide
+// table, all in one workgroup's pages, crowd in few threads (64 rows of 8 pages in 512 entries, a pool of 1024: 17.8/14.1).
+// Whole calls (us), this way / in three launches, all rows in use as far as the pool goes:
 //   table entries                   2048       12288      24576      36864      49152      65536
 //     64 rows, pool of   65536   8.8/14.5   8.8/14.2   9.2/14.1  10.5/14.8  10.8/14.9  12.7/14.6
 //     64 rows, pool of  524288   8.8/14.5   9.7/14.3  10.0/14.4  12.0/14.4  12.9/14.6  15.0/14.5
@@ -463,7 +466,7 @@ __global__ __launch_bounds__(kPagesThreads) void compact_words_kernel(CompactArg
 
 // Workgroups 0 .. chunks - 1: counts, map and moves of a chunk of pages; those behind: the table.  Every count is read and
 // written by one thread each, so that the new counts may lie over the old ones (not with kSelf).
-// kSelf: small pools, whose words every workgroup works out itself, from 16 loads of a thread: one launch (whole calls 5.2 us for
+// kSelf: small pools, whose words every workgroup works out itself, from 16 loads of a thread: one launch (whole calls 5.3 us for
 // 2048 pages, 6.8 for 16384) instead of two (8.0, 9.2).  The new counts must not lie over the old ones then.
 constexpr int kSelfPages = 16384;
 template <bool kSelf>
