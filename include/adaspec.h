@@ -331,6 +331,95 @@ int adaspec_kv_append(const void *k_new, const void *v_new, void *k_pages, void 
                       const int32_t *block_table, const int32_t *ctx_lens,
                       const int32_t *spec_lens, const adaspec_attn_dims *dims, void *stream);
 
+/* ------------------------------------------------------------------------
+ * Positions (rotary), and the append that applies them on the way.
+ *
+ * Row j of request i stands at position p = ctx_lens[i] - n_i + j; with parents
+ * (a draft tree, see below) node j stands at ctx_lens[i] - n_i + its depth, while
+ * its K/V go to the slot of j as always.  Of every head the first rot_dim entries
+ * are turned: pair f, which is (x[f], x[f + rot_dim / 2]), or interleaved
+ * (x[2f], x[2f + 1]), becomes
+ *     (a cos - b sin, b cos + a sin),  angle = p * inv_freq[f],
+ * cosine and sine times attn_factor (0 means 1).  The product of position and
+ * frequency is taken in 64 bits; the result is rounded once, from fp32, to the
+ * type it is stored in.  The entries behind rot_dim stay as they are.
+ *
+ * adaspec_rope - x [TQ][n_q_heads][head_dim] to out, which may be x itself (same
+ * pointer and row stride); otherwise the two must not overlap.  Uses of dims: batch,
+ * total_q, max_spec_len, n_q_heads, head_dim, dtype, rot_dim, interleaved,
+ * attn_factor, q_row_stride, q_out_row_stride.
+ *
+ * adaspec_kv_append_rope - queries turned as by adaspec_rope (q NULL: none), keys
+ * turned and written with the values into the pages, as adaspec_kv_append would
+ * (inv_freq NULL: not turned, q must be NULL too).
+ *   k_scales, v_scales NULL   k_pages, v_pages [num_pages][Hkv][16][d] of dims->dtype
+ *   both given                the pages are held in 8 bits: k_pages, v_pages
+ *                             [num_pages][Hkv][16][d] of e4m3 (OCP, one byte),
+ *                             k_scales, v_scales [num_pages][Hkv] fp32; an entry
+ *                             stands for e4m3 * scale of its page and kv head
+ * Scales.  New tokens of a page need the least power of two s (at least 2^-100) with
+ * which no |entry| exceeds 448 s; of a key's turned pairs the length counts, times
+ * attn_factor, which no turning changes.  The scale of a page without earlier tokens
+ * of the request becomes s; otherwise it becomes the larger of s and what it is, and
+ * where that is a change the earlier tokens are rounded to it again.  Entries that
+ * are not finite are stored as NaN and count for no scale.  A page that is written
+ * to has one holder (adaspec_kv_remap sees to that); its slots behind the request's
+ * last token are left as they are.
+ *
+ * Rows of q, k_new, v_new, q_out may be apart (strides in elements, multiples of 8,
+ * at least heads * head_dim): slices of one projection's output.  All tensors 16-byte
+ * aligned.  head_dim is a multiple of 8 up to 256, rot_dim even, in [2, head_dim];
+ * page_size 16; at most 2^23 (request, 16 rows) pairs at max_spec_len.  Needs no
+ * workspace.  A request whose lengths make no sense is left alone, an entry of
+ * block_table outside the pool is not written to.
+ * ---------------------------------------------------------------------- */
+typedef struct {
+    int32_t batch;              /* B                                                   */
+    int32_t total_q;            /* TQ = sum(spec_lens[i] + 1)                          */
+    int32_t max_spec_len;       /* upper bound on spec_lens[i]; with parents at most 63 */
+    int32_t n_q_heads;          /* Hq                                                  */
+    int32_t n_kv_heads;         /* Hkv, divides Hq (adaspec_kv_append_rope)            */
+    int32_t head_dim;           /* d                                                   */
+    int32_t page_size;          /* 16                                                  */
+    int32_t num_pages;
+    int32_t max_pages_per_req;  /* row stride of block_table                           */
+    int32_t dtype;              /* adaspec_dtype of q, k_new, v_new, q_out             */
+    int32_t rot_dim;            /* entries of a head that are turned                   */
+    int32_t interleaved;        /* 0: halves are paired, 1: neighbours                 */
+    float   attn_factor;        /* finite, >= 0; 0 means 1                             */
+    int32_t reserved;
+    int64_t q_row_stride, k_row_stride, v_row_stride, q_out_row_stride;
+} adaspec_rope_dims;
+
+int adaspec_rope(const void *x, const float *inv_freq, void *out,
+                 const int32_t *ctx_lens, const int32_t *spec_lens, const int32_t *parents /* or NULL */,
+                 const adaspec_rope_dims *dims, void *stream);
+
+int adaspec_kv_append_rope(const void *q, const void *k_new, const void *v_new, const float *inv_freq,
+                           void *q_out, void *k_pages, void *v_pages, float *k_scales, float *v_scales,
+                           const int32_t *block_table, const int32_t *ctx_lens, const int32_t *spec_lens,
+                           const int32_t *parents /* or NULL */, const adaspec_rope_dims *dims, void *stream);
+
+/* ------------------------------------------------------------------------
+ * adaspec_verify_attn_scaled - verification attention over a cache of 8 bits, as
+ * adaspec_kv_append_rope leaves it: k_pages, v_pages of e4m3 (dims->dtype is the
+ * type of q), k_scales, v_scales [num_pages][Hkv] fp32 of any finite value.
+ * parents NULL: a chain, as adaspec_verify_attn; else a tree, as
+ * adaspec_verify_attn_tree.  Same dims, plan modes and error rules; a workspace
+ * of its own size.  A token influences only rows that see it, whatever it holds.
+ * path: FAST is the matrix-core form (q of 16 bits, head_dim 64 or 128), VECTOR
+ * the portable one, AUTO the former where it fits.
+ * A plan that one of the two calls has built is of no use to the other.
+ * ---------------------------------------------------------------------- */
+size_t adaspec_verify_attn_scaled_workspace_bytes(const adaspec_attn_dims *dims);
+
+int adaspec_verify_attn_scaled(const void *q, const void *k_pages, const void *v_pages,
+                               const float *k_scales, const float *v_scales,
+                               const int32_t *block_table, const int32_t *ctx_lens,
+                               const int32_t *spec_lens, const int32_t *parents /* or NULL */, void *out,
+                               const adaspec_attn_dims *dims,
+                               void *workspace, size_t workspace_bytes, void *stream);
+
 /*
  * adaspec_commit - AFTER acceptance: keep what was accepted, drop the rest.
  * Request i had L_i = ctx_lens[i] cached tokens including its n_i = k_i + 1 new
@@ -480,6 +569,12 @@ typedef struct {
 int adaspec_kv_copy_pages(void *k_pages, void *v_pages, const int32_t *copy_src, const int32_t *copy_dst,
                           int32_t n_copies, const adaspec_copy_dims *dims, void *stream);
 
+/* The same for a cache of 8 bits (adaspec_kv_append_rope), whose scales go with the pages: k_scales, v_scales
+ * [layers][num_pages][n_kv_heads] fp32; head_dim a multiple of 8; dims->dtype is not looked at. */
+int adaspec_kv_copy_pages_scaled(void *k_pages, void *v_pages, float *k_scales, float *v_scales,
+                                 const int32_t *copy_src, const int32_t *copy_dst,
+                                 int32_t n_copies, const adaspec_copy_dims *dims, void *stream);
+
 /* ------------------------------------------------------------------------
  * Tree verification: the drafts of a request form a token TREE instead of a
  * chain.  The paper verifies chains and runs the tree-based system it compares
@@ -580,6 +675,14 @@ int adaspec_kv_compact_path(void *k_pages, void *v_pages, const int32_t *block_t
                             const int32_t *ctx_lens, const int32_t *spec_lens,
                             const int32_t *out_path, const int32_t *out_accept_len,
                             const adaspec_attn_dims *dims, int32_t path_stride, void *stream);
+
+/* The same for a cache of 8 bits (adaspec_kv_append_rope).  The scale of a page that rows move into becomes the
+ * largest of its own and those that they come from; rows (the page's earlier ones, too) are rounded again where
+ * their scale changes.  page_size 16, head_dim a multiple of 8, max_spec_len at most 63; dims->dtype is not looked at. */
+int adaspec_kv_compact_path_scaled(void *k_pages, void *v_pages, float *k_scales, float *v_scales,
+                                   const int32_t *block_table, const int32_t *ctx_lens, const int32_t *spec_lens,
+                                   const int32_t *out_path, const int32_t *out_accept_len,
+                                   const adaspec_attn_dims *dims, int32_t path_stride, void *stream);
 
 /* ------------------------------------------------------------------------
  * Draft-side sampling: the producer of draft_probs, draft_tokens and of the

@@ -29,6 +29,8 @@ EXPORTS = (
     "adaspec_verify_attn_window_workspace_bytes", "adaspec_verify_attn_window", "adaspec_check_window_inputs",
     "adaspec_kv_remap_workspace_bytes", "adaspec_kv_remap", "adaspec_kv_compact_pages_workspace_bytes", "adaspec_kv_compact_pages",
     "adaspec_kv_copy_pages",
+    "adaspec_rope", "adaspec_kv_append_rope", "adaspec_verify_attn_scaled_workspace_bytes", "adaspec_verify_attn_scaled",
+    "adaspec_kv_copy_pages_scaled", "adaspec_kv_compact_path_scaled",
     "adaspec_draft_sample_workspace_bytes", "adaspec_draft_sample",
     "adaspec_status_string", "adaspec_version",
 )
@@ -74,6 +76,14 @@ class CopyDims(C.Structure):
                 ("head_dim", C.c_int32), ("dtype", C.c_int32)]
 
 
+class RopeDims(C.Structure):
+    _fields_ = [("batch", C.c_int32), ("total_q", C.c_int32), ("max_spec_len", C.c_int32), ("n_q_heads", C.c_int32),
+                ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("page_size", C.c_int32), ("num_pages", C.c_int32),
+                ("max_pages_per_req", C.c_int32), ("dtype", C.c_int32), ("rot_dim", C.c_int32), ("interleaved", C.c_int32),
+                ("attn_factor", C.c_float), ("reserved", C.c_int32),
+                ("q_row_stride", C.c_int64), ("k_row_stride", C.c_int64), ("v_row_stride", C.c_int64), ("q_out_row_stride", C.c_int64)]
+
+
 class AdaspecError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -89,7 +99,8 @@ _FAST_ENTRIES = ("adaspec_verify_attn_workspace_bytes", "adaspec_verify_attn", "
                  "adaspec_kv_compact_path", "adaspec_commit", "adaspec_draft_sample_workspace_bytes",
                  "adaspec_draft_sample",
                  "adaspec_verify_attn_window_workspace_bytes", "adaspec_verify_attn_window", "adaspec_kv_remap_workspace_bytes",
-                 "adaspec_kv_remap", "adaspec_kv_compact_pages_workspace_bytes", "adaspec_kv_compact_pages", "adaspec_kv_copy_pages")
+                 "adaspec_kv_remap", "adaspec_kv_compact_pages_workspace_bytes", "adaspec_kv_compact_pages", "adaspec_kv_copy_pages",
+                 "adaspec_rope", "adaspec_kv_append_rope", "adaspec_verify_attn_scaled_workspace_bytes", "adaspec_verify_attn_scaled")
 
 
 def _native():
@@ -121,6 +132,7 @@ class _PythonOnly:
         return NotImplemented
     verify_attn = accept = accept_tree = kv_append = kv_compact_path = commit = draft_sample = _decline
     verify_attn_window = kv_remap = kv_compact_pages = kv_copy_pages = _decline
+    rope = kv_append_rope = verify_attn_scaled = _decline
 
 
 def lib() -> C.CDLL:
@@ -192,6 +204,18 @@ def _open(path: str) -> C.CDLL:
     L.adaspec_kv_compact_pages.argtypes = [vp] * 8 + [C.POINTER(PagesDims), vp, C.c_size_t, vp]
     L.adaspec_kv_copy_pages.restype = C.c_int
     L.adaspec_kv_copy_pages.argtypes = [vp] * 4 + [C.c_int32, C.POINTER(CopyDims), vp]
+    L.adaspec_rope.restype = C.c_int
+    L.adaspec_rope.argtypes = [vp] * 6 + [C.POINTER(RopeDims), vp]
+    L.adaspec_kv_append_rope.restype = C.c_int
+    L.adaspec_kv_append_rope.argtypes = [vp] * 13 + [C.POINTER(RopeDims), vp]
+    L.adaspec_verify_attn_scaled_workspace_bytes.restype = C.c_size_t
+    L.adaspec_verify_attn_scaled_workspace_bytes.argtypes = [C.POINTER(AttnDims)]
+    L.adaspec_verify_attn_scaled.restype = C.c_int
+    L.adaspec_verify_attn_scaled.argtypes = [vp] * 10 + [C.POINTER(AttnDims), vp, C.c_size_t, vp]
+    L.adaspec_kv_copy_pages_scaled.restype = C.c_int
+    L.adaspec_kv_copy_pages_scaled.argtypes = [vp] * 6 + [C.c_int32, C.POINTER(CopyDims), vp]
+    L.adaspec_kv_compact_path_scaled.restype = C.c_int
+    L.adaspec_kv_compact_path_scaled.argtypes = [vp] * 9 + [C.POINTER(AttnDims), C.c_int32, vp]
     L.adaspec_status_string.restype = C.c_char_p
     L.adaspec_status_string.argtypes = [C.c_int]
     L.adaspec_version.restype = C.c_int
@@ -309,7 +333,7 @@ def attn_dims(q, k_pages, block_table, *, max_spec_len: int, scale: float = 0.0,
 def verify_attn(q, k_pages, v_pages, block_table, ctx_lens, spec_lens, out=None, *,
                 max_spec_len: int, scale: float = 0.0, out_dtype: Optional[int] = None,
                 path: str = "auto", plan: str = "run", workspace=None, stream=None, parents=None, timing=None,
-                window: Optional[int] = None, sinks: int = 0):
+                window: Optional[int] = None, sinks: int = 0, k_scales=None, v_scales=None):
     """adaspec_verify_attn on device tensors; returns `out` [TQ][Hq][d].
 
     plan: "run" (build the ragged metadata, then run), "build" (metadata only; returns None) or
@@ -321,7 +345,14 @@ def verify_attn(q, k_pages, v_pages, block_table, ctx_lens, spec_lens, out=None,
     first `sinks`; block_table entries of pages that no row sees are never read.  Not with parents.  Such a call has no plan of
     its own and overwrites its workspace: not the one that holds a plan for calls without a window.
     workspace: calls without a window share a default one per device, and have to be ordered on one stream; on several streams each
-    needs its own.  Windowed calls without workspace= may overlap: each that keeps something there has its own."""
+    needs its own.  Windowed calls without workspace= may overlap: each that keeps something there has its own.
+    k_scales, v_scales [num_pages][Hkv] float32: adaspec_verify_attn_scaled instead, over k_pages and v_pages of
+    torch.float8_e4m3fn.  Not with a window.  Calls without workspace= may overlap: each has its own."""
+    if k_scales is not None or v_scales is not None:
+        if window is not None or sinks != 0:
+            raise ValueError("verify_attn(k_scales=, v_scales=) takes no window")
+        return _verify_attn_scaled(q, k_pages, v_pages, k_scales, v_scales, block_table, ctx_lens, spec_lens, out, max_spec_len, scale,
+                                   out_dtype, path, plan, workspace, stream, parents, timing)
     if window is not None or sinks != 0:
         if window is None:
             raise ValueError("verify_attn(sinks=...) needs a window: without one every token is visible")
@@ -405,6 +436,60 @@ def _verify_attn_window(q, k_pages, v_pages, block_table, ctx_lens, spec_lens, o
     if rc != 0:
         raise AdaspecError(rc, "adaspec_verify_attn_window")
     return out
+
+
+def _verify_attn_scaled(q, k_pages, v_pages, k_scales, v_scales, block_table, ctx_lens, spec_lens, out, max_spec_len, scale, out_dtype,
+                        path, plan, workspace, stream, parents, timing):
+    """verify_attn over a cache of 8 bits"""
+    if path == "auto" and timing is None:
+        r = (_fast or _native()).verify_attn_scaled(q, k_pages, v_pages, k_scales, v_scales, block_table, ctx_lens, spec_lens, out,
+                                                    max_spec_len, scale, out_dtype, plan, workspace, stream, parents)
+        if r is not NotImplemented:
+            return r
+    import torch
+    for t in (q, block_table, ctx_lens, spec_lens):
+        assert t.is_cuda and t.is_contiguous()
+    assert q.dim() == 3 and k_pages.dim() == 4 and block_table.dim() == 2
+    _scaled_cache(k_pages, v_pages, k_scales, v_scales)
+    _dense_ints(block_table, ctx_lens, spec_lens)
+    _on_current_device(q)
+    assert k_pages.device == block_table.device == q.device
+    assert ctx_lens.shape == spec_lens.shape == block_table.shape[:1] and k_pages.shape[3] == q.shape[2]
+    dims = _with_timing(attn_dims(q, k_pages, block_table, max_spec_len=max_spec_len, scale=scale, out_dtype=out_dtype, path=path,
+                                  plan=plan), timing)
+    if parents is not None:
+        _dense_ints(block_table, parents)
+        assert parents.shape == (q.shape[0],)
+    if plan != "run" and workspace is None:
+        raise ValueError("verify_attn(plan='build' / 'reuse') needs an explicit workspace= tensor that the "
+                         "caller keeps for the whole pass")
+    if out is not None:
+        _on_device(out, q.device, "out")
+        assert out.is_contiguous() and out.shape == q.shape and _dtype_code(out) == dims.out_dtype
+    elif plan != "build":
+        out = torch.empty(q.shape, dtype=_torch_dtype(dims.out_dtype), device=q.device)
+    L = lib()
+    need = L.adaspec_verify_attn_scaled_workspace_bytes(C.byref(dims))
+    ptr = lambda t: None if t is None else t.data_ptr()
+    args = [ptr(t) for t in (q, k_pages, v_pages, k_scales, v_scales, block_table, ctx_lens, spec_lens, parents, out)]
+    if need == 0 and dims.batch > 0:
+        raise AdaspecError(L.adaspec_verify_attn_scaled(*args, C.byref(dims), None, 0, None) or -2, "adaspec_verify_attn_scaled (dims)")
+    ws = _scratch(need, q.device, workspace, stream)
+    rc = L.adaspec_verify_attn_scaled(*args, C.byref(dims), ws.data_ptr(), ws.numel(), _stream_ptr(stream))
+    if rc != 0:
+        raise AdaspecError(rc, "adaspec_verify_attn_scaled")
+    return out
+
+
+def _scaled_cache(k_pages, v_pages, k_scales, v_scales) -> None:
+    """a cache of 8 bits: pages [..., num_pages][Hkv][P][d] of e4m3, scales [..., num_pages][Hkv]"""
+    import torch
+    if k_scales is None or v_scales is None:
+        raise ValueError("k_scales= and v_scales= go together")
+    for t in (k_pages, v_pages, k_scales, v_scales):
+        assert t.is_cuda and t.is_contiguous() and t.device == k_pages.device
+    assert k_pages.dtype == v_pages.dtype == torch.float8_e4m3fn and k_scales.dtype == v_scales.dtype == torch.float32
+    assert v_pages.shape == k_pages.shape and v_scales.shape == k_scales.shape == k_pages.shape[:-2]
 
 
 def accept_dims(target_logits, draft_probs, draft_tokens, spec_lens, max_spec_len, out_stride, path):
@@ -532,8 +617,12 @@ def accept_tree(target_logits, draft_probs, draft_tokens, parents, uniforms, spe
 
 
 def kv_compact_path(k_pages, v_pages, block_table, ctx_lens, spec_lens, out_path, out_accept_len, *,
-                    max_spec_len: int, stream=None) -> None:
-    """adaspec_kv_compact_path: moves the accepted nodes' K/V rows to chain positions, in place."""
+                    max_spec_len: int, stream=None, k_scales=None, v_scales=None) -> None:
+    """adaspec_kv_compact_path: moves the accepted nodes' K/V rows to chain positions, in place.
+    k_scales, v_scales [num_pages][Hkv]: adaspec_kv_compact_path_scaled instead, for a cache of 8 bits."""
+    if k_scales is not None or v_scales is not None:
+        return _kv_compact_path_scaled(k_pages, v_pages, k_scales, v_scales, block_table, ctx_lens, spec_lens, out_path, out_accept_len,
+                                       max_spec_len, stream)
     if (_fast or _native()).kv_compact_path(k_pages, v_pages, block_table, ctx_lens, spec_lens, out_path, out_accept_len,
                                             max_spec_len, stream) is not NotImplemented:
         return
@@ -553,6 +642,24 @@ def kv_compact_path(k_pages, v_pages, block_table, ctx_lens, spec_lens, out_path
                                        _stream_ptr(stream))
     if rc != 0:
         raise AdaspecError(rc, "adaspec_kv_compact_path")
+
+
+def _kv_compact_path_scaled(k_pages, v_pages, k_scales, v_scales, block_table, ctx_lens, spec_lens, out_path, out_accept_len, max_spec_len,
+                            stream) -> None:
+    assert k_pages.dim() == 4 and block_table.dim() == 2 and out_path.dim() == 2
+    _scaled_cache(k_pages, v_pages, k_scales, v_scales)
+    _dense_ints(block_table, ctx_lens, spec_lens, out_path, out_accept_len)
+    _on_current_device(k_pages)
+    assert block_table.device == k_pages.device
+    assert ctx_lens.shape == spec_lens.shape == out_accept_len.shape == block_table.shape[:1] == out_path.shape[:1]
+    num_pages, Hkv, P, d = k_pages.shape
+    B, max_pages = block_table.shape
+    dims = AttnDims(B, B, int(max_spec_len), Hkv, Hkv, d, P, num_pages, max_pages, BF16, BF16, PATH_AUTO, 0.0)
+    rc = lib().adaspec_kv_compact_path_scaled(k_pages.data_ptr(), v_pages.data_ptr(), k_scales.data_ptr(), v_scales.data_ptr(),
+                                              block_table.data_ptr(), ctx_lens.data_ptr(), spec_lens.data_ptr(), out_path.data_ptr(),
+                                              out_accept_len.data_ptr(), C.byref(dims), out_path.shape[1], _stream_ptr(stream))
+    if rc != 0:
+        raise AdaspecError(rc, "adaspec_kv_compact_path_scaled")
 
 
 def check_accept_inputs(draft_tokens, spec_lens, temperature, *, vocab: int, max_spec_len: int, stream=None) -> int:
@@ -606,9 +713,115 @@ def check_ragged_inputs(block_table, ctx_lens, spec_lens, dims: AttnDims, stream
     return int(flags.item())
 
 
+def _rope_dims(rows, heads, kv_heads, d, table_shape, num_pages, max_spec_len, dtype, inv_freq, interleaved, attn_factor) -> RopeDims:
+    import torch
+    rot = 0
+    if inv_freq is not None:
+        assert inv_freq.is_cuda and inv_freq.is_contiguous() and inv_freq.dtype == torch.float32 and inv_freq.dim() == 1
+        rot = 2 * inv_freq.shape[0]
+    if not attn_factor > 0:
+        raise ValueError("attn_factor= is more than 0")
+    B, max_pages = table_shape
+    return RopeDims(B, rows, int(max_spec_len), heads, kv_heads, d, 16, num_pages, max_pages, dtype, rot, int(bool(interleaved)),
+                    float(attn_factor), 0, 0, 0, 0, 0)
+
+
+def _ragged_rows(x, like=None):
+    """rows [TQ][heads][d] whose heads lie side by side; the rows may be apart, as slices of a wider array are"""
+    assert x.is_cuda and x.dim() == 3 and x.stride(2) == 1 and (x.stride(1) == x.shape[2] or x.shape[1] == 1)
+    if like is not None:
+        assert x.dtype == like.dtype and x.device == like.device and x.shape[0] == like.shape[0] and x.shape[2] == like.shape[2]
+    return x.stride(0) if x.shape[0] > 1 else max(x.stride(0), x.shape[1] * x.shape[2]) // 8 * 8
+
+
+def rope(x, inv_freq, ctx_lens, spec_lens, *, max_spec_len: int, interleaved: bool = False, attn_factor: float = 1.0, parents=None,
+         out=None, stream=None):
+    """adaspec_rope: the rows x [TQ][heads][d] turned by the angles of their positions; returns `out` (new and contiguous unless
+    given; may be x itself).  inv_freq [rot_dim / 2] float32 (rope_frequencies makes it).  parents [TQ] int32: nodes of draft trees
+    stand at the depth they have.  x (and out) may be slices of wider rows, e.g. of a projection's output."""
+    r = (_fast or _native()).rope(x, inv_freq, ctx_lens, spec_lens, max_spec_len, interleaved, attn_factor, parents, out, stream)
+    if r is not NotImplemented:
+        return r
+    import torch
+    stride = _ragged_rows(x)
+    _dense_ints(ctx_lens, spec_lens, *([] if parents is None else [parents]))
+    _on_current_device(x)
+    assert ctx_lens.device == inv_freq.device == x.device and spec_lens.dim() == 1 and ctx_lens.shape == spec_lens.shape
+    assert parents is None or parents.shape == x.shape[:1]
+    if out is None:
+        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    else:
+        _on_device(out, x.device, "out")
+        assert out.shape == x.shape
+    dims = _rope_dims(x.shape[0], x.shape[1], 0, x.shape[2], (spec_lens.shape[0], 0), 0, max_spec_len, _dtype_code(x), inv_freq,
+                      interleaved, attn_factor)
+    dims.q_row_stride, dims.q_out_row_stride = stride, _ragged_rows(out, x)
+    rc = lib().adaspec_rope(x.data_ptr(), inv_freq.data_ptr(), out.data_ptr(), ctx_lens.data_ptr(), spec_lens.data_ptr(),
+                            None if parents is None else parents.data_ptr(), C.byref(dims), _stream_ptr(stream))
+    if rc != 0:
+        raise AdaspecError(rc, "adaspec_rope")
+    return out
+
+
+def kv_append_rope(q, k_new, v_new, inv_freq, k_pages, v_pages, block_table, ctx_lens, spec_lens, *, max_spec_len: int, k_scales=None,
+                   v_scales=None, interleaved: bool = False, attn_factor: float = 1.0, parents=None, q_out=None, stream=None):
+    """adaspec_kv_append_rope: keys k_new [TQ][Hkv][d] turned by the angles of their positions and written into the pages with v_new,
+    in place; returns the queries q [TQ][Hq][d] turned likewise (q_out if given, which may be q itself; None where q is None).
+    k_scales, v_scales [num_pages][Hkv] float32: the pages are held in 8 bits (torch.float8_e4m3fn) with these scales, which are
+    updated.  inv_freq, interleaved, attn_factor, parents, and rows that are slices: as for rope; inv_freq None: nothing is turned
+    (then q is None too)."""
+    r = (_fast or _native()).kv_append_rope(q, k_new, v_new, inv_freq, k_pages, v_pages, block_table, ctx_lens, spec_lens, max_spec_len,
+                                            k_scales, v_scales, interleaved, attn_factor, parents, q_out, stream)
+    if r is not NotImplemented:
+        return r
+    import torch
+    if q is not None and inv_freq is None:
+        raise ValueError("kv_append_rope(q=...) needs inv_freq: without it nothing is turned")
+    if q is None and q_out is not None:
+        raise ValueError("kv_append_rope(q_out=...) needs q")
+    TQ, Hkv, d = k_new.shape
+    strides = [0, _ragged_rows(k_new), _ragged_rows(v_new, k_new), 0]
+    assert v_new.shape == k_new.shape and k_pages.dim() == 4 and block_table.dim() == 2
+    if k_scales is not None or v_scales is not None:
+        _scaled_cache(k_pages, v_pages, k_scales, v_scales)
+    else:
+        for t in (k_pages, v_pages):
+            assert t.is_cuda and t.is_contiguous() and t.dtype == k_new.dtype
+    assert v_pages.shape == k_pages.shape and v_pages.device == k_pages.device == k_new.device
+    num_pages, Hkv2, P, d2 = k_pages.shape
+    assert (Hkv2, d2) == (Hkv, d)
+    _dense_ints(block_table, ctx_lens, spec_lens, *([] if parents is None else [parents]))
+    _on_current_device(k_new)
+    assert block_table.device == k_new.device and (inv_freq is None or inv_freq.device == k_new.device)
+    assert ctx_lens.shape == spec_lens.shape == block_table.shape[:1] and (parents is None or parents.shape == (TQ,))
+    if q is not None:
+        strides[0] = _ragged_rows(q, k_new)
+        if q_out is None:
+            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        else:
+            _on_device(q_out, q.device, "q_out")
+            assert q_out.shape == q.shape
+        strides[3] = _ragged_rows(q_out, q)
+    dims = _rope_dims(TQ, 0 if q is None else q.shape[1], Hkv, d, tuple(block_table.shape), num_pages, max_spec_len, _dtype_code(k_new),
+                      inv_freq, interleaved, attn_factor)
+    dims.page_size = P
+    dims.q_row_stride, dims.k_row_stride, dims.v_row_stride, dims.q_out_row_stride = strides
+    ptr = lambda t: None if t is None else t.data_ptr()
+    rc = lib().adaspec_kv_append_rope(*[ptr(t) for t in (q, k_new, v_new, inv_freq, q_out, k_pages, v_pages, k_scales, v_scales,
+                                                         block_table, ctx_lens, spec_lens, parents)], C.byref(dims), _stream_ptr(stream))
+    if rc != 0:
+        raise AdaspecError(rc, "adaspec_kv_append_rope")
+    return q_out
+
+
 def kv_append(k_new, v_new, k_pages, v_pages, block_table, ctx_lens, spec_lens, *, max_spec_len: int,
-              stream=None) -> None:
-    """adaspec_kv_append: writes the new tokens' K/V rows [TQ][Hkv][d] into the pages, in place."""
+              stream=None, k_scales=None, v_scales=None) -> None:
+    """adaspec_kv_append: writes the new tokens' K/V rows [TQ][Hkv][d] into the pages, in place.
+    k_scales, v_scales [num_pages][Hkv]: into a cache of 8 bits (kv_append_rope without turning)."""
+    if k_scales is not None or v_scales is not None:
+        kv_append_rope(None, k_new, v_new, None, k_pages, v_pages, block_table, ctx_lens, spec_lens, max_spec_len=max_spec_len,
+                       k_scales=k_scales, v_scales=v_scales, stream=stream)
+        return
     if (_fast or _native()).kv_append(k_new, v_new, k_pages, v_pages, block_table, ctx_lens, spec_lens, max_spec_len,
                                       stream) is not NotImplemented:
         return
@@ -761,9 +974,12 @@ def kv_compact_pages(block_table, page_refs, *, max_moves: Optional[int] = None,
     return out_table, out_refs, page_map, copy_src, copy_dst, status
 
 
-def kv_copy_pages(k_pages, v_pages, copy_src, copy_dst, *, stream=None) -> None:
+def kv_copy_pages(k_pages, v_pages, copy_src, copy_dst, *, stream=None, k_scales=None, v_scales=None) -> None:
     """adaspec_kv_copy_pages: pages copy_src[c] -> copy_dst[c] of K and V, in place; pairs with -1 are left out.
-    k_pages, v_pages: the pages of one layer [num_pages][Hkv][P][d], or of several [layers][num_pages][Hkv][P][d]."""
+    k_pages, v_pages: the pages of one layer [num_pages][Hkv][P][d], or of several [layers][num_pages][Hkv][P][d].
+    k_scales, v_scales [num_pages][Hkv] or [layers][num_pages][Hkv]: adaspec_kv_copy_pages_scaled instead, for a cache of 8 bits."""
+    if k_scales is not None or v_scales is not None:
+        return _kv_copy_pages_scaled(k_pages, v_pages, k_scales, v_scales, copy_src, copy_dst, stream)
     if (_fast or _native()).kv_copy_pages(k_pages, v_pages, copy_src, copy_dst, stream) is not NotImplemented:
         return
     assert k_pages.dim() in (4, 5)
@@ -780,6 +996,22 @@ def kv_copy_pages(k_pages, v_pages, copy_src, copy_dst, *, stream=None) -> None:
                                      copy_src.shape[0], C.byref(dims), _stream_ptr(stream))
     if rc != 0:
         raise AdaspecError(rc, "adaspec_kv_copy_pages")
+
+
+def _kv_copy_pages_scaled(k_pages, v_pages, k_scales, v_scales, copy_src, copy_dst, stream) -> None:
+    assert k_pages.dim() in (4, 5)
+    layers = k_pages.shape[0] if k_pages.dim() == 5 else 1
+    num_pages, Hkv, P, d = k_pages.shape[-4:]
+    _scaled_cache(k_pages, v_pages, k_scales, v_scales)
+    _dense_ints(copy_src, copy_dst)
+    _on_current_device(k_pages)
+    assert copy_src.device == k_pages.device and copy_src.dim() == 1 and copy_dst.shape == copy_src.shape
+    dims = CopyDims(layers, num_pages, Hkv, P, d, BF16)
+    rc = lib().adaspec_kv_copy_pages_scaled(k_pages.data_ptr(), v_pages.data_ptr(), k_scales.data_ptr(), v_scales.data_ptr(),
+                                            copy_src.data_ptr(), copy_dst.data_ptr(), copy_src.shape[0], C.byref(dims),
+                                            _stream_ptr(stream))
+    if rc != 0:
+        raise AdaspecError(rc, "adaspec_kv_copy_pages_scaled")
 
 
 def draft_sample(draft_logits, temperature, uniforms, *, probs_dtype=None, draft_probs=None, out_rows=None,

@@ -139,14 +139,19 @@ __host__ __device__ inline int sched_order(int total, int W, int cus, int even_r
 }
 
 // Which kernel family a call takes.  ADASPEC_PATH_FAST names the head_dim 128 form; AUTO also reaches the others.
-enum class AttnKind { kVector, kMfma128, kMfma64, kMfmaF32 };
+enum class AttnKind { kVector, kMfma128, kMfma64, kMfmaF32, kMfmaE4m3 };
 constexpr int kAttnD64Block = 64;   // tokens per block of the head_dim 64 form (attn_d64.hip)
 AttnKind attn_kind(const adaspec_attn_dims &d);
 AttnPlan make_attn_plan(const adaspec_attn_dims &d, AttnKind kind, bool tree);
 bool attn_fast_path_supported(const adaspec_attn_dims &d);
+// over a cache of 8 bits (attn_e4m3.hip)
+bool attn_e4m3_supported(const adaspec_attn_dims &d);
+AttnKind attn_scaled_kind(const adaspec_attn_dims &d);
+constexpr int attn_e4m3_block(int head_dim) { return head_dim == 64 ? 64 : 32; }    // tokens
 
 struct AttnArgs {
     const void *q, *k_pages, *v_pages;
+    const float *k_scales = nullptr, *v_scales = nullptr;   // a cache of 8 bits, else NULL
     const int32_t *block_table, *ctx_lens, *spec_lens;
     const int32_t *parents = nullptr;   // tree verification: parent node of every query row, else NULL
     void *out;
@@ -190,6 +195,9 @@ int attn_d64_grid_slots(const AttnArgs &a, int cus);
 // fp32, head_dim 64 or 128 (attn_f32.hip)
 hipError_t launch_attn_f32(const AttnArgs &a);
 int attn_f32_grid_slots(const AttnArgs &a, int cus);
+// 8 bits, head_dim 64 or 128 (attn_e4m3.hip)
+hipError_t launch_attn_e4m3(const AttnArgs &a);
+int attn_e4m3_grid_slots(const AttnArgs &a, int cus);
 hipError_t launch_attn_combine(const AttnArgs &a);
 int attn_combine_waves(const AttnPlan &p, const adaspec_attn_dims &d);   // wavefronts per (row, head) of the combine kernel
 
@@ -346,6 +354,16 @@ hipError_t launch_draft_fast(const void *logits, const float *temperature, const
 hipError_t launch_kv_append(const void *k_new, const void *v_new, void *k_pages, void *v_pages,
                             const int32_t *block_table, const int32_t *ctx_lens,
                             const int32_t *spec_lens, const adaspec_attn_dims &d, hipStream_t stream);
+// positions, and the append that applies them (rope_append.hip)
+bool rope_grid_fits(const adaspec_rope_dims &d, bool e4m3);
+hipError_t launch_rope_append(const void *q, const void *k, const void *v, const float *inv_freq, void *q_out, void *k_pages, void *v_pages,
+                              float *k_scales, float *v_scales, const int32_t *block_table, const int32_t *ctx_lens,
+                              const int32_t *spec_lens, const int32_t *parents, const adaspec_rope_dims &d, hipStream_t stream);
+hipError_t launch_kv_copy_pages_scaled(void *k_pages, void *v_pages, float *k_scales, float *v_scales, const int32_t *copy_src,
+                                       const int32_t *copy_dst, int n_copies, const adaspec_copy_dims &d, hipStream_t stream);
+hipError_t launch_kv_compact_path_scaled(void *k_pages, void *v_pages, float *k_scales, float *v_scales, const int32_t *block_table,
+                                         const int32_t *ctx_lens, const int32_t *spec_lens, const int32_t *out_path,
+                                         const int32_t *out_accept_len, const adaspec_attn_dims &d, int path_stride, hipStream_t stream);
 hipError_t launch_commit(const int32_t *out_tokens, const int32_t *out_accept_len,
                          const int32_t *spec_lens, const int32_t *ctx_lens,
                          const int32_t *next_spec_lens, int32_t *committed_lens,

@@ -66,6 +66,7 @@ static int compute_units()
 }
 
 static bool dtype_ok(int dt) { return dt == ADASPEC_F32 || dt == ADASPEC_F16 || dt == ADASPEC_BF16; }
+static bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 static bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 static int validate_attn_dims(const adaspec_attn_dims *d)
@@ -147,6 +148,11 @@ static bool rows_split_wins(int tiles, int groups, bool tree, int batch, int64_t
     return tokens <= (!four ? (tree ? 128 : 96) : single ? (tree ? 1024 : 192) : (tree ? 512 : 320));
 }
 
+AttnKind attn_scaled_kind(const adaspec_attn_dims &d)
+{
+    return d.path != ADASPEC_PATH_VECTOR && attn_e4m3_supported(d) ? AttnKind::kMfmaE4m3 : AttnKind::kVector;
+}
+
 AttnPlan make_attn_plan(const adaspec_attn_dims &d, AttnKind kind, bool tree)
 {
     AttnPlan p;
@@ -160,7 +166,8 @@ AttnPlan make_attn_plan(const adaspec_attn_dims &d, AttnKind kind, bool tree)
     p.max_rows = (d.max_spec_len + 1) * G;
     const bool many_rows = kind == AttnKind::kMfma128 && attn_row_tiles(p.max_rows) > 2;
     if (scheduled) {
-        p.block_tokens = kind == AttnKind::kMfma64 ? kAttnD64Block : (kind == AttnKind::kMfmaF32 ? 16 : 32);
+        p.block_tokens = kind == AttnKind::kMfma64 ? kAttnD64Block : kind == AttnKind::kMfmaF32 ? 16
+                         : kind == AttnKind::kMfmaE4m3 ? attn_e4m3_block(d.head_dim) : 32;
         p.split_tokens = pairs >= 256 ? 2048 : (pairs >= 128 ? 1024 : (pairs >= 32 ? 512 : 256));
     } else {
         p.block_tokens = 64;
@@ -373,14 +380,30 @@ size_t adaspec_verify_attn_workspace_bytes(const adaspec_attn_dims *dims)
     return attn_workspace_bytes(*dims, attn_kind(*dims));
 }
 
-// chain (parents == NULL, tree == false) and tree verification share everything but the mask
-static int verify_attn_impl(const void *q, const void *k_pages, const void *v_pages,
+// scales of a cache of 8 bits; `there`: whether it is one
+struct Scales {
+    const float *k = nullptr, *v = nullptr;
+    bool there = false;
+};
+
+static int validate_attn_dims(const adaspec_attn_dims *d, bool scaled)
+{
+    if (!scaled || !d) return validate_attn_dims(d);
+    adaspec_attn_dims any = *d;                                     // (FAST has other shapes here)
+    if (any.path == ADASPEC_PATH_FAST) any.path = ADASPEC_PATH_AUTO;
+    const int rc = validate_attn_dims(&any);
+    if (rc != ADASPEC_OK) return rc;
+    return d->path == ADASPEC_PATH_FAST && !attn_e4m3_supported(*d) ? ADASPEC_ERR_UNSUPPORTED : ADASPEC_OK;
+}
+
+// chain (parents == NULL, tree == false) and tree verification share everything but the mask, caches of 8 bits all but the main kernel
+static int verify_attn_impl(const void *q, const void *k_pages, const void *v_pages, const Scales &scales,
                             const int32_t *block_table, const int32_t *ctx_lens,
                             const int32_t *spec_lens, const int32_t *parents, bool tree, void *out,
                             const adaspec_attn_dims *dims,
                             void *workspace, size_t workspace_bytes, void *stream)
 {
-    int rc = validate_attn_dims(dims);
+    int rc = validate_attn_dims(dims, scales.there);
     if (rc != ADASPEC_OK) return rc;
     if (tree && dims->max_spec_len > 63) return ADASPEC_ERR_UNSUPPORTED;
     if (dims->batch == 0) return ADASPEC_OK;
@@ -388,14 +411,17 @@ static int verify_attn_impl(const void *q, const void *k_pages, const void *v_pa
     const bool plan_only = dims->plan_mode == ADASPEC_PLAN_BUILD_ONLY;
     if (!block_table || !ctx_lens || !spec_lens || !workspace) return ADASPEC_ERR_NULL;
     if (!plan_only && (!q || !k_pages || !v_pages || !out)) return ADASPEC_ERR_NULL;
+    if (!plan_only && scales.there && (!scales.k || !scales.v)) return ADASPEC_ERR_NULL;
     if (reinterpret_cast<uintptr_t>(workspace) & 255u) return ADASPEC_ERR_ALIGN;
     if (!plan_only && (!aligned16(q) || !aligned16(k_pages) || !aligned16(v_pages) || !aligned16(out)))
         return ADASPEC_ERR_ALIGN;
+    if (!plan_only && scales.there && (!aligned4(scales.k) || !aligned4(scales.v))) return ADASPEC_ERR_ALIGN;
     AttnArgs a;
-    const AttnKind kind = attn_kind(*dims);
+    const AttnKind kind = scales.there ? attn_scaled_kind(*dims) : attn_kind(*dims);
     a.plan = make_attn_plan(*dims, kind, tree);
     if (workspace_bytes < attn_workspace_bytes(*dims, kind)) return ADASPEC_ERR_WORKSPACE;
     a.q = q; a.k_pages = k_pages; a.v_pages = v_pages;
+    a.k_scales = scales.k; a.v_scales = scales.v;
     a.block_table = block_table; a.ctx_lens = ctx_lens; a.spec_lens = spec_lens;
     a.parents = tree ? parents : nullptr;
     a.out = out; a.dims = *dims; a.ws = static_cast<char *>(workspace);
@@ -412,6 +438,7 @@ static int verify_attn_impl(const void *q, const void *k_pages, const void *v_pa
     if (plan_only) return ADASPEC_OK;
     if (!record_event(dims->timing_start, dims->timing_stop, true, a.stream)) return ADASPEC_ERR_HIP;
     hipError_t e = kind == AttnKind::kVector ? launch_attn_vector(a)
+                   : kind == AttnKind::kMfmaE4m3 ? launch_attn_e4m3(a)
                    : kind == AttnKind::kMfma64 ? launch_attn_d64(a)
                    : kind == AttnKind::kMfmaF32 ? launch_attn_f32(a) : launch_attn_mfma(a);
     if (e != hipSuccess) return ADASPEC_ERR_HIP;
@@ -425,7 +452,7 @@ int adaspec_verify_attn(const void *q, const void *k_pages, const void *v_pages,
                         const int32_t *spec_lens, void *out, const adaspec_attn_dims *dims,
                         void *workspace, size_t workspace_bytes, void *stream)
 {
-    return verify_attn_impl(q, k_pages, v_pages, block_table, ctx_lens, spec_lens, nullptr, false, out, dims,
+    return verify_attn_impl(q, k_pages, v_pages, {}, block_table, ctx_lens, spec_lens, nullptr, false, out, dims,
                             workspace, workspace_bytes, stream);
 }
 
@@ -435,8 +462,25 @@ int adaspec_verify_attn_tree(const void *q, const void *k_pages, const void *v_p
                              const adaspec_attn_dims *dims,
                              void *workspace, size_t workspace_bytes, void *stream)
 {
-    return verify_attn_impl(q, k_pages, v_pages, block_table, ctx_lens, spec_lens, parents, true, out, dims,
+    return verify_attn_impl(q, k_pages, v_pages, {}, block_table, ctx_lens, spec_lens, parents, true, out, dims,
                             workspace, workspace_bytes, stream);
+}
+
+size_t adaspec_verify_attn_scaled_workspace_bytes(const adaspec_attn_dims *dims)
+{
+    if (validate_attn_dims(dims, true) != ADASPEC_OK) return 0;
+    return attn_workspace_bytes(*dims, attn_scaled_kind(*dims));
+}
+
+int adaspec_verify_attn_scaled(const void *q, const void *k_pages, const void *v_pages,
+                               const float *k_scales, const float *v_scales,
+                               const int32_t *block_table, const int32_t *ctx_lens,
+                               const int32_t *spec_lens, const int32_t *parents, void *out,
+                               const adaspec_attn_dims *dims,
+                               void *workspace, size_t workspace_bytes, void *stream)
+{
+    return verify_attn_impl(q, k_pages, v_pages, {k_scales, v_scales, true}, block_table, ctx_lens, spec_lens, parents,
+                            parents != nullptr, out, dims, workspace, workspace_bytes, stream);
 }
 
 // dims of a windowed call; window and sinks are cut to what a block table can hold
@@ -691,6 +735,24 @@ int adaspec_kv_compact_path(void *k_pages, void *v_pages, const int32_t *block_t
     return ADASPEC_OK;
 }
 
+int adaspec_kv_compact_path_scaled(void *k_pages, void *v_pages, float *k_scales, float *v_scales, const int32_t *block_table,
+                                   const int32_t *ctx_lens, const int32_t *spec_lens, const int32_t *out_path,
+                                   const int32_t *out_accept_len, const adaspec_attn_dims *d, int32_t path_stride, void *stream)
+{
+    if (!d) return ADASPEC_ERR_NULL;
+    if (d->batch < 0 || d->max_spec_len < 0 || path_stride < d->max_spec_len + 1) return ADASPEC_ERR_DIM;
+    if (d->n_kv_heads <= 0 || d->head_dim <= 0 || d->page_size <= 0) return ADASPEC_ERR_DIM;
+    if (d->num_pages <= 0 || d->max_pages_per_req <= 0) return ADASPEC_ERR_DIM;
+    if (d->head_dim % 8 || d->head_dim > 256 || d->page_size != 16 || d->max_spec_len > 63) return ADASPEC_ERR_UNSUPPORTED;
+    if (d->batch > 65535 || d->n_kv_heads > 1 << 20) return ADASPEC_ERR_UNSUPPORTED;
+    if (d->batch == 0) return ADASPEC_OK;
+    if (!k_pages || !v_pages || !k_scales || !v_scales || !block_table || !ctx_lens || !spec_lens || !out_path || !out_accept_len)
+        return ADASPEC_ERR_NULL;
+    if (!aligned16(k_pages) || !aligned16(v_pages) || !aligned4(k_scales) || !aligned4(v_scales)) return ADASPEC_ERR_ALIGN;
+    return launch_kv_compact_path_scaled(k_pages, v_pages, k_scales, v_scales, block_table, ctx_lens, spec_lens, out_path, out_accept_len, *d,
+                                         path_stride, static_cast<hipStream_t>(stream)) == hipSuccess ? ADASPEC_OK : ADASPEC_ERR_HIP;
+}
+
 int adaspec_check_ragged_inputs(const int32_t *block_table, const int32_t *ctx_lens,
                                 const int32_t *spec_lens, const adaspec_attn_dims *dims,
                                 int32_t *err_flags, void *stream)
@@ -787,6 +849,102 @@ int adaspec_commit(const int32_t *out_tokens, const int32_t *out_accept_len,
     return ADASPEC_OK;
 }
 
+// Rows of an array: `count` of them, `width` bytes each, `stride` bytes apart.
+struct Rows {
+    const void *p;
+    int64_t width, stride, count;
+    Extent all() const { return {p, p && count > 0 ? (size_t)((count - 1) * stride + width) : 0, -1}; }
+};
+// whether rows share bytes; slices of one wider array (equal strides, places side by side) do not
+static bool rows_overlap(const Rows &a, const Rows &b)
+{
+    if (!overlap(a.all(), b.all())) return false;
+    if (a.stride != b.stride) return true;
+    const int64_t apart = (int64_t)(reinterpret_cast<uintptr_t>(b.p) - reinterpret_cast<uintptr_t>(a.p)) % a.stride;
+    const int64_t behind = apart < 0 ? apart + a.stride : apart;    // where b's rows begin, behind the beginning of a row of a
+    return behind < a.width || behind + b.width > a.stride;
+}
+
+// `append`: keys and values go into pages as well
+static int rope_impl(const void *q, const void *k_new, const void *v_new, const float *inv_freq, void *q_out, void *k_pages, void *v_pages,
+                     float *k_scales, float *v_scales, const int32_t *block_table, const int32_t *ctx_lens, const int32_t *spec_lens,
+                     const int32_t *parents, const adaspec_rope_dims *dims, bool append, void *stream)
+{
+    if (!dims) return ADASPEC_ERR_NULL;
+    adaspec_rope_dims d = *dims;
+    const bool e4m3 = k_scales || v_scales;
+    if (d.batch < 0 || d.total_q < d.batch || d.max_spec_len < 0) return ADASPEC_ERR_DIM;
+    if ((int64_t)d.total_q > (int64_t)d.batch * ((int64_t)d.max_spec_len + 1)) return ADASPEC_ERR_DIM;
+    if (d.head_dim <= 0) return ADASPEC_ERR_DIM;
+    if (append && (d.n_kv_heads <= 0 || d.page_size <= 0 || d.num_pages <= 0 || d.max_pages_per_req <= 0)) return ADASPEC_ERR_DIM;
+    if ((q || !append) && (d.n_q_heads <= 0 || (append && d.n_q_heads % d.n_kv_heads))) return ADASPEC_ERR_DIM;
+    if (!dtype_ok(d.dtype)) return ADASPEC_ERR_DTYPE;
+    if (d.head_dim % 8 || d.head_dim > 256) return ADASPEC_ERR_UNSUPPORTED;
+    if (inv_freq && (d.rot_dim < 2 || d.rot_dim % 2 || d.rot_dim > d.head_dim)) return ADASPEC_ERR_DIM;
+    if (d.interleaved != 0 && d.interleaved != 1) return ADASPEC_ERR_DIM;
+    if (!(d.attn_factor >= 0.0f) || isinf(d.attn_factor)) return ADASPEC_ERR_DIM;
+    if (append && d.page_size != 16) return ADASPEC_ERR_UNSUPPORTED;
+    if (parents && d.max_spec_len > 63) return ADASPEC_ERR_UNSUPPORTED;
+    const int64_t q_width = (int64_t)d.n_q_heads * d.head_dim, kv_width = (int64_t)d.n_kv_heads * d.head_dim;
+    // (rows of a workgroup are counted in 32 bits, a page's bytes too)
+    if (q && q_width > 1 << 23) return ADASPEC_ERR_UNSUPPORTED;
+    if (append && kv_width > 1 << 23) return ADASPEC_ERR_UNSUPPORTED;
+    if (d.max_spec_len > (1 << 30) || !rope_grid_fits(d, e4m3)) return ADASPEC_ERR_UNSUPPORTED;
+    if (q && (d.q_row_stride < q_width || d.q_out_row_stride < q_width)) return ADASPEC_ERR_DIM;
+    if (append && (d.k_row_stride < kv_width || d.v_row_stride < kv_width)) return ADASPEC_ERR_DIM;
+    if (q && (d.q_row_stride % 8 || d.q_out_row_stride % 8)) return ADASPEC_ERR_ALIGN;
+    if (append && (d.k_row_stride % 8 || d.v_row_stride % 8)) return ADASPEC_ERR_ALIGN;
+    if (d.batch == 0) return ADASPEC_OK;
+    if (!ctx_lens || !spec_lens || (q && (!q_out || !inv_freq)) || (!append && !q)) return ADASPEC_ERR_NULL;
+    if (append && (!k_new || !v_new || !k_pages || !v_pages || !block_table)) return ADASPEC_ERR_NULL;
+    if (e4m3 && (!k_scales || !v_scales)) return ADASPEC_ERR_NULL;
+    if (q && (!aligned16(q) || !aligned16(q_out))) return ADASPEC_ERR_ALIGN;
+    if (append && (!aligned16(k_new) || !aligned16(v_new) || !aligned16(k_pages) || !aligned16(v_pages))) return ADASPEC_ERR_ALIGN;
+    if (!aligned4(inv_freq) || !aligned4(k_scales) || !aligned4(v_scales)) return ADASPEC_ERR_ALIGN;
+    // Nothing that is written may lie over anything else, but q_out may be q.
+    const int64_t size = d.dtype == ADASPEC_F32 ? 4 : 2;
+    const Rows rq{q, q_width * size, d.q_row_stride * size, q ? d.total_q : 0}, ro{q ? q_out : nullptr, q_width * size, d.q_out_row_stride * size, q ? d.total_q : 0};
+    const Rows rk{append ? k_new : nullptr, kv_width * size, d.k_row_stride * size, append ? d.total_q : 0};
+    const Rows rv{append ? v_new : nullptr, kv_width * size, d.v_row_stride * size, append ? d.total_q : 0};
+    if (q && !(q == q_out && d.q_row_stride == d.q_out_row_stride) && rows_overlap(rq, ro)) return ADASPEC_ERR_DIM;
+    if (q && append && (rows_overlap(ro, rk) || rows_overlap(ro, rv))) return ADASPEC_ERR_DIM;
+    if (append) {
+        const size_t pool = (size_t)d.num_pages * d.n_kv_heads, bytes = pool * d.page_size * d.head_dim * (e4m3 ? 1 : size);
+        const size_t table = (size_t)d.batch * d.max_pages_per_req * 4, per_row = (size_t)d.batch * 4;
+        const Extent outs[] = {{k_pages, bytes, -1}, {v_pages, bytes, -1}, {k_scales, e4m3 ? pool * 4 : 0, -1}, {v_scales, e4m3 ? pool * 4 : 0, -1}};
+        const Extent ins[] = {rq.all(), ro.all(), rk.all(), rv.all(), {inv_freq, inv_freq ? (size_t)d.rot_dim * 2 : 0, -1},
+                              {block_table, table, -1}, {ctx_lens, per_row, -1}, {spec_lens, per_row, -1},
+                              {parents, parents ? (size_t)d.total_q * 4 : 0, -1}};
+        if (outputs_clash(outs, ins)) return ADASPEC_ERR_DIM;
+    }
+    if (q) {
+        const Extent out = ro.all();
+        const Extent ins[] = {{inv_freq, (size_t)d.rot_dim * 2, -1}, {ctx_lens, (size_t)d.batch * 4, -1}, {spec_lens, (size_t)d.batch * 4, -1},
+                              {block_table, append ? (size_t)d.batch * d.max_pages_per_req * 4 : 0, -1},
+                              {parents, parents ? (size_t)d.total_q * 4 : 0, -1}};
+        for (const Extent &in : ins)
+            if (overlap(out, in)) return ADASPEC_ERR_DIM;
+    }
+    if (d.attn_factor == 0.0f) d.attn_factor = 1.0f;
+    return launch_rope_append(q, append ? k_new : nullptr, v_new, inv_freq, q_out, k_pages, v_pages, k_scales, v_scales, block_table, ctx_lens,
+                              spec_lens, parents, d, static_cast<hipStream_t>(stream)) == hipSuccess ? ADASPEC_OK : ADASPEC_ERR_HIP;
+}
+
+int adaspec_rope(const void *x, const float *inv_freq, void *out, const int32_t *ctx_lens, const int32_t *spec_lens,
+                 const int32_t *parents, const adaspec_rope_dims *dims, void *stream)
+{
+    return rope_impl(x, nullptr, nullptr, inv_freq, out, nullptr, nullptr, nullptr, nullptr, nullptr, ctx_lens, spec_lens, parents, dims,
+                     false, stream);
+}
+
+int adaspec_kv_append_rope(const void *q, const void *k_new, const void *v_new, const float *inv_freq, void *q_out, void *k_pages,
+                           void *v_pages, float *k_scales, float *v_scales, const int32_t *block_table, const int32_t *ctx_lens,
+                           const int32_t *spec_lens, const int32_t *parents, const adaspec_rope_dims *dims, void *stream)
+{
+    return rope_impl(q, k_new, v_new, inv_freq, q_out, k_pages, v_pages, k_scales, v_scales, block_table, ctx_lens, spec_lens, parents,
+                     dims, true, stream);
+}
+
 static int validate_pages_dims(const adaspec_pages_dims *d, bool remap)
 {
     if (!d) return ADASPEC_ERR_NULL;
@@ -878,6 +1036,21 @@ int adaspec_kv_copy_pages(void *k_pages, void *v_pages, const int32_t *copy_src,
     if (!aligned16(k_pages) || !aligned16(v_pages)) return ADASPEC_ERR_ALIGN;
     return launch_kv_copy_pages(k_pages, v_pages, copy_src, copy_dst, n_copies, *d, static_cast<hipStream_t>(stream)) == hipSuccess
                ? ADASPEC_OK : ADASPEC_ERR_HIP;
+}
+
+int adaspec_kv_copy_pages_scaled(void *k_pages, void *v_pages, float *k_scales, float *v_scales, const int32_t *copy_src,
+                                 const int32_t *copy_dst, int32_t n_copies, const adaspec_copy_dims *d, void *stream)
+{
+    if (!d) return ADASPEC_ERR_NULL;
+    if (n_copies < 0 || d->layers < 0 || d->num_pages <= 0 || d->n_kv_heads <= 0 || d->page_size <= 0 || d->head_dim <= 0)
+        return ADASPEC_ERR_DIM;
+    if (d->head_dim % 8 || d->page_size != 16) return ADASPEC_ERR_UNSUPPORTED;
+    if ((double)d->n_kv_heads * d->page_size * d->head_dim >= 2147483648.0) return ADASPEC_ERR_UNSUPPORTED;
+    if (n_copies == 0 || d->layers == 0) return ADASPEC_OK;
+    if (!k_pages || !v_pages || !k_scales || !v_scales || !copy_src || !copy_dst) return ADASPEC_ERR_NULL;
+    if (!aligned16(k_pages) || !aligned16(v_pages) || !aligned4(k_scales) || !aligned4(v_scales)) return ADASPEC_ERR_ALIGN;
+    return launch_kv_copy_pages_scaled(k_pages, v_pages, k_scales, v_scales, copy_src, copy_dst, n_copies, *d,
+                                       static_cast<hipStream_t>(stream)) == hipSuccess ? ADASPEC_OK : ADASPEC_ERR_HIP;
 }
 
 static int validate_draft_dims(const adaspec_draft_dims *d)

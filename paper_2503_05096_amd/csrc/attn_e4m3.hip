@@ -1,0 +1,520 @@
+// Matrix-core verification attention over a cache of 8 bits (e4m3 with a scale per page and kv head): 16-bit Q, head_dim 64 or
+// 128, any number of query rows per kv head.
+//
+// The scheme of attn_mfma.hip (units, schedule, direct calls, lazily moved softmax reference, merge of four wavefronts):
+//   S^T = K Q^T,  O^T += V^T P^T,  in accumulator layouts that need no shuffle.
+// What 8 bits change:
+//   * An e4m3 value is exact in bf16 and in f16.  K becomes Q's type in registers, two elements an instruction; its scale is
+//     one factor per page, applied to the scores.  V becomes bf16; its scale is applied to the softmax weights, which are
+//     split into two bf16 pieces (16 bits): one piece, off by up to 2^-9, would be the largest error there is.
+//   * Both products contract in any order of their k-slots, as long as their two operands agree.  So a lane takes 16
+//     consecutive bytes of a key at a time, and Q is laid out to match.
+//   * No LDS tile for V^T: a lane loads D / 16 neighbouring channels of the four tokens 4g .. 4g + 3 of a page, and byte
+//     permutes put equal channels of two tokens side by side, which is what the conversion takes (two bytes in, two bf16
+//     out).  The lane then holds D / 16 whole operand columns: tile t of O^T has channel (D / 16) m + t in row m.
+// A block is 32 tokens of 128 channels or 64 of 64: 8 KB of K and V per wavefront, 32 registers, double-buffered.
+//
+// Bound: HBM.
+#include <type_traits>
+
+#include "adaspec_internal.h"
+#include "attn_mfma_common.h"
+#include "device_utils.h"
+#include "e4m3.h"
+
+namespace adaspec {
+
+// two e4m3 (bytes 0, 1 or 2, 3 of w) as two values of T
+template <class T, bool kHigh> __device__ __forceinline__ uint32_t e4m3_pair(uint32_t w)
+{
+    if constexpr (T::id == ADASPEC_BF16) return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, kHigh));
+    else return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, kHigh));
+}
+template <class T> __device__ __forceinline__ uint4 e4m3_operand(uint32_t lo, uint32_t hi)
+{
+    return make_uint4(e4m3_pair<T, false>(lo), e4m3_pair<T, true>(lo), e4m3_pair<T, false>(hi), e4m3_pair<T, true>(hi));
+}
+// the bytes of w that are NaN, as 0x80
+__device__ __forceinline__ uint32_t e4m3_nans(uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
+
+template <class T, int D, int RT, bool kTree, bool kDirect>
+__global__ __launch_bounds__(256, (RT <= 2 ? 2 : 1)) void attn_e4m3_kernel(
+    const char *__restrict__ q, const char *__restrict__ k_pages, const char *__restrict__ v_pages,
+    const float *__restrict__ k_scales, const float *__restrict__ v_scales,
+    const int32_t *__restrict__ block_table, void *__restrict__ out, const int32_t *__restrict__ header,
+    const int32_t *__restrict__ unit_meta, const int32_t *__restrict__ sched,
+    const unsigned long long *__restrict__ anc, float *__restrict__ part_ml, float *__restrict__ part_o,
+    int Hq, int Hkv, int max_pages_per_req, int max_rows, int n_row_groups, float scale_log2, int out_dtype, int cus, DirectArgs direct)
+{
+    constexpr int kRows = 16 * RT;
+    constexpr int kTokens = attn_e4m3_block(D), kPages = kTokens / 16;
+    constexpr int kKLoads = D / 64;                                 // 16-byte pieces of a key per lane
+    constexpr int kSteps = D / 32;                                  // products per 16 x 16 tile of scores
+    constexpr int kWords = D / 64;                                  // of a lane's channels of a token of V
+    constexpr int kTiles = D / 16;                                  // of O^T
+    constexpr int kHalves = kTokens / 32;
+    constexpr int kORow = D + 4;                                    // floats per row of the merge buffer (padded: conflict-free b128)
+    constexpr int kSlab = kRows * kORow * 4;
+    constexpr int kQEntries = RT * kSteps * 64, kQLoads = (kQEntries + 255) / 256;
+    __shared__ __attribute__((aligned(16))) char smem[kWaves * kSlab];
+    __shared__ __attribute__((aligned(16))) uint4 q_lds[kQEntries];   // Q^T operands, MFMA lane order
+    __shared__ float s_m[kWaves][kRows], s_l[kWaves][kRows];
+    __shared__ unsigned long long s_anc[kTree ? kRows : 1];         // ancestor mask of each row of the unit
+
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int g = lane >> 4, n16 = lane & 15;
+    const int G = Hq / Hkv;
+    const int total_units = kDirect ? 0 : header[0] * Hkv * n_row_groups;
+    float *my_state = reinterpret_cast<float *>(smem + wv * kSlab);
+
+    // K: lane (g, m) <- token 16 mt + m, channels 64 c + 16 g .. + 15.  V: lane (g, m) <- token 16 p + 4 g + i, channels (D / 16) m ..
+    struct Block {
+        uint4 k[kPages][kKLoads];
+        uint32_t v[kPages][4][kWords];
+        float ks[kPages], vs[kPages];
+    };
+    const uint32_t k_lane_off = n16 * D + 16 * g;
+    const uint32_t v_lane_off = (4 * g) * D + kTiles * n16;
+
+    const int W = gridDim.x, wg = blockIdx.x;
+    const int n_rounds = kDirect ? 0 : header[2];
+    int round = 0;
+    int idx_ahead = kDirect ? 0 : sched_position(0, wg, W, cus, header[1]);     // round 0 needs no table
+    auto next_unit = [&](Unit &u) -> bool {
+        for (; round < n_rounds; ++round) {
+            const int idx = idx_ahead;
+            idx_ahead = round + 1 < n_rounds ? sched[(int64_t)(round + 1) * W + wg] : -1;
+            if (idx < 0 || idx >= total_units) continue;
+            const int rg = idx % n_row_groups;
+            u.gkv = (idx / n_row_groups) % Hkv;
+            const int32_t *mt = unit_meta + 8 * (int64_t)(idx / (n_row_groups * Hkv));
+            u.i = mt[0];
+            const int sp = mt[1];
+            u.ns = mt[2]; u.L = mt[3]; u.n = mt[4]; u.qrow0 = mt[5]; u.item = mt[6];
+            u.rows = u.n * G; u.r0 = rg * kRows;
+            if (u.r0 >= u.rows) continue;
+            const int slen = split_len_of(u.L, u.ns, kTokens);
+            u.t0 = sp * slen; u.t1 = min(u.L, u.t0 + slen);
+            u.nblk = (u.t1 - u.t0 + kTokens - 1) / kTokens;
+            u.bt_off = (int64_t)u.i * max_pages_per_req;
+            ++round;
+            return true;
+        }
+        return false;
+    };
+
+    // Page ids and scales by scalar loads; pages past the split's end are replaced by the block's first (masks and the tail code
+    // keep what they hold out of the result), so that every block issues the same loads.
+    auto load_block = [&](const Unit &u, int bi, Block &b) {
+        const int tb = u.t0 + bi * kTokens;
+        const int64_t at = u.bt_off + (tb >> 4);
+        int64_t block[kPages];
+#pragma unroll
+        for (int p = 0; p < kPages; ++p) {
+            const int64_t page = block_table[tb + 16 * p < u.t1 ? at + p : at];
+            block[p] = page * Hkv + u.gkv;
+        }
+#pragma unroll
+        for (int p = 0; p < kPages; ++p)
+#pragma unroll
+            for (int c = 0; c < kKLoads; ++c) b.k[p][c] = ld16_stream(k_pages + block[p] * (16 * D) + k_lane_off + 64 * c);
+#pragma unroll
+        for (int p = 0; p < kPages; ++p)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const char *at_v = v_pages + block[p] * (16 * D) + v_lane_off + i * D;
+                if constexpr (kWords == 2) {
+                    const u32x2v w = __builtin_nontemporal_load(reinterpret_cast<const u32x2v *>(at_v));
+                    b.v[p][i][0] = w.x;
+                    b.v[p][i][1] = w.y;
+                } else {
+                    b.v[p][i][0] = __builtin_nontemporal_load(reinterpret_cast<const uint32_t *>(at_v));
+                }
+            }
+#pragma unroll
+        for (int p = 0; p < kPages; ++p) {
+            b.ks[p] = k_scales[block[p]];
+            b.vs[p] = v_scales[block[p]];
+        }
+    };
+    // this thread's share of the unit's Q^T operands: entry (row tile, s, lane)
+    auto load_q = [&](const Unit &u, uint4 (&qv)[kQLoads]) {
+#pragma unroll
+        for (int k = 0; k < kQLoads; ++k) {
+            const int e = tid + 256 * k, s = (e >> 6) % kSteps;
+            const int row = u.r0 + 16 * (e / (64 * kSteps)) + n16;
+            qv[k] = make_uint4(0, 0, 0, 0);
+            if (e < kQEntries && row < u.rows)
+                qv[k] = ld16(q + (((u.qrow0 + row / G) * Hq + u.gkv * G + row % G) * D + 64 * (s >> 1) + 16 * g + 8 * (s & 1)) * 2);
+        }
+    };
+    auto load_anc = [&](const Unit &u) -> unsigned long long {
+        const int row = u.r0 + tid;
+        return (tid < kRows && row < u.rows) ? anc[u.qrow0 + row / G] : 0ull;
+    };
+
+    Unit cur, nxt;
+    bool have;
+    uint4 qv[kQLoads];
+    unsigned long long av = 0ull;
+    Block b0, b1;
+    if constexpr (kDirect) have = direct_unit(cur, direct, block_table, G, Hkv, n_row_groups, kRows, kTokens, max_pages_per_req, wv, lane);
+    else have = next_unit(cur);
+    if (have) {
+        load_q(cur, qv);
+        if constexpr (kTree) av = load_anc(cur);
+        if (wv < cur.nblk) load_block(cur, wv, b0);
+    }
+
+    while (have) {
+        const Unit u = cur;
+        const bool have_next = kDirect ? false : next_unit(nxt);
+        const int first_masked = u.L - u.n + 1;                    // tokens >= this are hidden from some row
+#pragma unroll
+        for (int k = 0; k < kQLoads; ++k)
+            if (kQEntries % 256 == 0 || tid + 256 * k < kQEntries) q_lds[tid + 256 * k] = qv[k];
+        if constexpr (kTree) { if (tid < kRows) s_anc[tid] = av; }
+        int pos[RT];
+#pragma unroll
+        for (int nt = 0; nt < RT; ++nt) {
+            const int row = u.r0 + 16 * nt + n16;
+            pos[nt] = row < u.rows ? (u.L - u.n + row / G) : -1;
+        }
+        lds_barrier();
+
+        float m[RT], lsum[RT];
+        f32x4 o[RT][kTiles];
+#pragma unroll
+        for (int nt = 0; nt < RT; ++nt) {
+            m[nt] = kLowestRef; lsum[nt] = 0.f;
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t) o[nt][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+
+        auto block = [&](int bi, Block &b) {
+            const int tb = u.t0 + bi * kTokens;
+            constexpr int kE = 4 * kPages;                          // scores per lane and row tile
+            // ---- S^T = K Q^T ------------------------------------------------------------
+            float p[RT][kE];
+#pragma unroll
+            for (int mt = 0; mt < kPages; ++mt) {
+                uint4 kop[kSteps];
+#pragma unroll
+                for (int s = 0; s < kSteps; ++s) {
+                    const uint4 raw = b.k[mt][s >> 1];
+                    kop[s] = (s & 1) ? e4m3_operand<T>(raw.z, raw.w) : e4m3_operand<T>(raw.x, raw.y);
+                }
+                const float factor = b.ks[mt] * scale_log2;
+#pragma unroll
+                for (int nt = 0; nt < RT; ++nt) {
+                    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int s = 0; s < kSteps; ++s) acc = Mma<T>::run(kop[s], q_lds[(nt * kSteps + s) * 64 + lane], acc);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) p[nt][4 * mt + r] = acc[r] * factor;
+                }
+            }
+
+            // ---- online softmax (per lane: row n16 of each row tile, kE of the tokens), in log2 units ----
+            const bool need_mask = (tb + kTokens > first_masked) || (tb + kTokens > u.t1);
+            uint32_t seen[RT];                                      // where there is a mask: bit e = the row sees token e
+            float vs[kPages];
+#pragma unroll
+            for (int mt = 0; mt < kPages; ++mt) vs[mt] = b.vs[mt];
+#pragma unroll
+            for (int nt = 0; nt < RT; ++nt) {
+                if (need_mask) {
+                    seen[nt] = 0;
+                    const unsigned long long am = kTree ? s_anc[16 * nt + n16] : 0ull;
+                    const int base = u.L - u.n, lim = min(pos[nt], u.t1 - 1);
+#pragma unroll
+                    for (int e = 0; e < kE; ++e) {
+                        const int t = tb + 16 * (e >> 2) + 4 * g + (e & 3), rel = t - base;
+                        bool vis;
+                        if constexpr (kTree) vis = t < u.t1 && (rel < 0 ? pos[nt] >= 0 : ((am >> (rel & 63)) & 1ull) != 0);
+                        else vis = t <= lim;
+                        p[nt][e] = vis ? p[nt][e] : -INFINITY;
+                        seen[nt] |= vis ? 1u << e : 0u;
+                    }
+                }
+                float mx = p[nt][0];
+#pragma unroll
+                for (int e = 1; e < kE; ++e) mx = fmaxf(mx, p[nt][e]);
+                mx = max_over_row_groups(mx);
+                // lazy reference: moves only when the block's maximum exceeds it by more than kLazyLog2
+                const bool grow = mx > m[nt] + kLazyLog2;
+                if (__builtin_expect(__builtin_amdgcn_ballot_w64(grow) != 0, 0)) {
+                    const float m_new = grow ? mx : m[nt];
+                    const float alpha = __builtin_amdgcn_exp2f(m[nt] - m_new);
+                    m[nt] = m_new;
+                    lsum[nt] *= alpha;
+#pragma unroll
+                    for (int t = 0; t < kTiles; ++t) o[nt][t] *= alpha;
+                }
+                float psum = 0.f;
+#pragma unroll
+                for (int e = 0; e < kE; ++e) {
+                    p[nt][e] = __builtin_amdgcn_exp2f(p[nt][e] - m[nt]);
+                    psum += p[nt][e];
+                    p[nt][e] *= vs[e >> 2];
+                }
+                lsum[nt] += psum;
+            }
+
+            // ---- what hidden tokens hold stays out: no weight, whatever their scale; no value behind the request's end; NaN
+            // values only in rows that see them -------------------------------------------------------------------------------
+            if (need_mask) {
+                uint32_t nans = 0;
+#pragma unroll
+                for (int pg = 0; pg < kPages; ++pg)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+#pragma unroll
+                        for (int w = 0; w < kWords; ++w) {
+                            if (tb + 16 * pg + 4 * g + i >= u.t1) b.v[pg][i][w] = 0;
+                            nans |= e4m3_nans(b.v[pg][i][w]);
+                        }
+#pragma unroll
+                for (int nt = 0; nt < RT; ++nt)
+#pragma unroll
+                    for (int e = 0; e < kE; ++e)
+                        if (!((seen[nt] >> e) & 1)) p[nt][e] = 0.f;
+                if (__builtin_expect(__builtin_amdgcn_ballot_w64(nans != 0) != 0, 0)) {
+                    // rows that see a NaN, channel by channel: a product of what is NaN with what is seen
+#pragma unroll
+                    for (int hf = 0; hf < kHalves; ++hf)
+#pragma unroll
+                        for (int t = 0; t < kTiles; ++t) {
+                            uint32_t bad[8];
+#pragma unroll
+                            for (int e = 0; e < 8; ++e)
+                                bad[e] = (e4m3_nans(b.v[2 * hf + (e >> 2)][e & 3][t >> 2]) >> (8 * (t & 3))) & 0x80u ? 0x3f80u : 0u;
+                            const uint4 a = make_uint4(bad[0] | bad[1] << 16, bad[2] | bad[3] << 16, bad[4] | bad[5] << 16, bad[6] | bad[7] << 16);
+#pragma unroll
+                            for (int nt = 0; nt < RT; ++nt) {
+                                uint32_t see[8];
+#pragma unroll
+                                for (int e = 0; e < 8; ++e) see[e] = (seen[nt] >> (8 * hf + e)) & 1 ? 0x3f80u : 0u;
+                                const uint4 x = make_uint4(see[0] | see[1] << 16, see[2] | see[3] << 16, see[4] | see[5] << 16, see[6] | see[7] << 16);
+                                const f32x4 hit = Mma<BF16>::run(a, x, f32x4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+                                for (int r = 0; r < 4; ++r)
+                                    if (hit[r] > 0.f) o[nt][t][r] = __uint_as_float(0x7fc00000u);
+                            }
+                        }
+#pragma unroll
+                    for (int pg = 0; pg < kPages; ++pg)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+#pragma unroll
+                            for (int w = 0; w < kWords; ++w) {
+                                const uint32_t x = e4m3_nans(b.v[pg][i][w]);
+                                b.v[pg][i][w] &= ~(x | (x - (x >> 7)));         // NaN bytes become 0
+                            }
+                }
+            }
+
+            // ---- O^T += V^T P^T, 32 tokens at a time ------------------------------
+#pragma unroll
+            for (int hf = 0; hf < kHalves; ++hf) {
+                uint4 hi[RT], lo[RT];
+#pragma unroll
+                for (int nt = 0; nt < RT; ++nt)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const float x = p[nt][8 * hf + 2 * j], y = p[nt][8 * hf + 2 * j + 1];
+                        const uint32_t w = Mma<BF16>::pack2(x, y);
+                        (&hi[nt].x)[j] = w;
+                        (&lo[nt].x)[j] = Mma<BF16>::pack2(x - __uint_as_float(w << 16), y - __uint_as_float(w & 0xffff0000u));
+                    }
+#pragma unroll
+                for (int w = 0; w < kWords; ++w)
+#pragma unroll
+                    for (int up = 0; up < 2; ++up) {                // channels 0, 1 and 2, 3 of the word
+                        uint32_t pair[4];                           // two tokens, two channels: (t0 c0, t1 c0, t0 c1, t1 c1)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const uint32_t(&v)[4][kWords] = b.v[2 * hf + (j >> 1)];
+                            pair[j] = __builtin_amdgcn_perm(v[2 * (j & 1) + 1][w], v[2 * (j & 1)][w], up ? 0x07030602u : 0x05010400u);
+                        }
+                        const uint4 even = make_uint4(e4m3_pair<BF16, false>(pair[0]), e4m3_pair<BF16, false>(pair[1]),
+                                                      e4m3_pair<BF16, false>(pair[2]), e4m3_pair<BF16, false>(pair[3]));
+                        const uint4 odd = make_uint4(e4m3_pair<BF16, true>(pair[0]), e4m3_pair<BF16, true>(pair[1]),
+                                                     e4m3_pair<BF16, true>(pair[2]), e4m3_pair<BF16, true>(pair[3]));
+                        const int t = 4 * w + 2 * up;
+#pragma unroll
+                        for (int nt = 0; nt < RT; ++nt) {
+                            o[nt][t] = Mma<BF16>::run(even, hi[nt], o[nt][t]);
+                            o[nt][t + 1] = Mma<BF16>::run(odd, hi[nt], o[nt][t + 1]);
+                            o[nt][t] = Mma<BF16>::run(even, lo[nt], o[nt][t]);
+                            o[nt][t + 1] = Mma<BF16>::run(odd, lo[nt], o[nt][t + 1]);
+                        }
+                    }
+            }
+        };
+
+        // Two buffers: the loads of the next block are issued before this one is worked on, without a branch around them, so
+        // that the compiler's waits count exactly.
+        if (wv < u.nblk) {
+            int bi = wv;
+            for (; bi + 2 * kWaves < u.nblk; bi += 2 * kWaves) {
+                load_block(u, bi + kWaves, b1);
+                block(bi, b0);
+                load_block(u, bi + 2 * kWaves, b0);
+                block(bi + kWaves, b1);
+            }
+            if (bi + kWaves < u.nblk) {
+                load_block(u, bi + kWaves, b1);
+                block(bi, b0);
+                block(bi + kWaves, b1);
+            } else {
+                block(bi, b0);
+            }
+        }
+
+        // ---- next unit: its first block and its Q rows travel while this unit's states are merged
+        if (have_next) {
+            load_q(nxt, qv);
+            if constexpr (kTree) av = load_anc(nxt);
+            if (wv < nxt.nblk) load_block(nxt, wv, b0);
+        }
+        // ---- merge the four wavefronts' states through LDS (as in attn_mfma.hip) ----------
+#pragma unroll
+        for (int nt = 0; nt < RT; ++nt) {
+            lsum[nt] += __shfl_xor(lsum[nt], 16, kWave);
+            lsum[nt] += __shfl_xor(lsum[nt], 32, kWave);
+            if (g == 0) { s_m[wv][16 * nt + n16] = m[nt]; s_l[wv][16 * nt + n16] = lsum[nt]; }
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int t = 0; t < kTiles; t += 4)
+                    *reinterpret_cast<f32x4 *>(my_state + (16 * nt + n16) * kORow + kTiles * (4 * g + r) + t) =
+                        f32x4{o[nt][t][r], o[nt][t + 1][r], o[nt][t + 2][r], o[nt][t + 3][r]};
+        }
+        lds_barrier();
+        // 256 threads: 16 RT rows x D / 4 float4 columns
+        constexpr int kCols = D / 4;
+#pragma unroll
+        for (int it = 0; it < kRows * kCols / 256; ++it) {
+            const int idx = tid + 256 * it;
+            const int rl = idx / kCols, c4 = idx % kCols;
+            const int row = u.r0 + rl;
+            if (row >= u.rows) continue;
+            float ms = s_m[0][rl], ltot = 0.f;
+#pragma unroll
+            for (int w = 1; w < kWaves; ++w) ms = fmaxf(ms, s_m[w][rl]);
+            f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) {
+                const float sc = __builtin_amdgcn_exp2f(s_m[w][rl] - ms);
+                ltot += sc * s_l[w][rl];
+                acc += sc * *reinterpret_cast<const f32x4 *>(smem + w * kSlab + 4 * (rl * kORow + 4 * c4));
+            }
+            if (u.ns == 1) {
+                const float inv = 1.0f / ltot;
+                const int64_t obase = ((u.qrow0 + row / G) * Hq + u.gkv * G + row % G) * (int64_t)D + 4 * c4;
+                if (out_dtype == ADASPEC_F32) {
+                    *reinterpret_cast<f32x4 *>(reinterpret_cast<float *>(out) + obase) = acc * inv;
+                } else {
+                    uint2 pk = make_uint2(Mma<T>::pack2(acc[0] * inv, acc[1] * inv), Mma<T>::pack2(acc[2] * inv, acc[3] * inv));
+                    *reinterpret_cast<uint2 *>(reinterpret_cast<uint16_t *>(out) + obase) = pk;
+                }
+            } else {
+                const int64_t idx_row = ((int64_t)u.item * Hkv + u.gkv) * max_rows + row;
+                if (kDirect && attn_merge_fits(D, RT) && direct.flags) {
+                    store_state(part_o + idx_row * D + 4 * c4, acc);
+                    if (c4 == 0) store_ml(part_ml + idx_row * 2, ms, ltot);
+                } else {
+                    *reinterpret_cast<f32x4 *>(part_o + idx_row * D + 4 * c4) = acc;
+                    if (c4 == 0) {
+                        part_ml[idx_row * 2] = ms;
+                        part_ml[idx_row * 2 + 1] = ltot;
+                    }
+                }
+            }
+        }
+        if constexpr (kDirect) {
+            if constexpr (attn_merge_fits(D, RT)) {
+                if (u.ns > 1 && direct.flags)
+                    merge_splits<T, D, kRows>(direct, u, part_ml, part_o, out, out_dtype, Hq, Hkv, G, max_rows, tid);
+            }
+            break;
+        }
+        // the next loop iteration overwrites q_lds, the states and s_m: everyone must be done reading them
+        lds_barrier();
+        cur = nxt;
+        have = have_next;
+    }
+}
+
+// ---- host side -----------------------------------------------------------------------------------------------
+bool attn_e4m3_supported(const adaspec_attn_dims &d)
+{
+    return (d.head_dim == 64 || d.head_dim == 128) && (d.dtype == ADASPEC_F16 || d.dtype == ADASPEC_BF16);
+}
+
+template <typename F>
+static void with_e4m3_instance(const AttnArgs &a, F &&f)
+{
+    const int rt = attn_row_tiles(a.plan.max_rows);
+    auto with_mode = [&](auto tag, auto d, auto rt_tag) {
+        if (a.direct) f(tag, d, rt_tag, std::false_type{}, std::true_type{});
+        else if (a.parents) f(tag, d, rt_tag, std::true_type{}, std::false_type{});
+        else f(tag, d, rt_tag, std::false_type{}, std::false_type{});
+    };
+    auto with_rt = [&](auto tag, auto d) {
+        if (rt == 1) with_mode(tag, d, std::integral_constant<int, 1>{});
+        else if (rt == 2) with_mode(tag, d, std::integral_constant<int, 2>{});
+        else if (rt == 3) with_mode(tag, d, std::integral_constant<int, 3>{});
+        else with_mode(tag, d, std::integral_constant<int, 4>{});
+    };
+    auto with_d = [&](auto tag) {
+        if (a.dims.head_dim == 64) with_rt(tag, std::integral_constant<int, 64>{});
+        else with_rt(tag, std::integral_constant<int, 128>{});
+    };
+    if (a.dims.dtype == ADASPEC_F16) with_d(F16{});
+    else with_d(BF16{});
+}
+
+template <typename T, int D, int RT, bool kTree, bool kDirect>
+static int attn_e4m3_slots(int cus)
+{
+    static int slots = 0;
+    if (slots == 0) {
+        int per_cu = 1;
+        if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&per_cu, attn_e4m3_kernel<T, D, RT, kTree, kDirect>, 256, 0) != hipSuccess)
+            per_cu = 1;
+        const int n = cus * (per_cu > 0 ? per_cu : 1);
+        slots = n < kMaxSchedW ? n : kMaxSchedW;
+    }
+    return slots;
+}
+
+int attn_e4m3_grid_slots(const AttnArgs &a, int cus)
+{
+    int slots = 1;
+    with_e4m3_instance(a, [&](auto tag, auto d, auto rt, auto tree, auto direct) {
+        slots = attn_e4m3_slots<decltype(tag), decltype(d)::value, decltype(rt)::value, decltype(tree)::value, decltype(direct)::value>(cus);
+    });
+    return slots;
+}
+
+hipError_t launch_attn_e4m3(const AttnArgs &a)
+{
+    const AttnPlan &p = a.plan;
+    const adaspec_attn_dims &d = a.dims;
+    if (a.sched_w <= 0) return hipSuccess;                          // no work item can exist
+    with_e4m3_instance(a, [&](auto tag, auto dim, auto rt, auto tree, auto direct) {
+        hipLaunchKernelGGL((attn_e4m3_kernel<decltype(tag), decltype(dim)::value, decltype(rt)::value, decltype(tree)::value, decltype(direct)::value>),
+                           dim3(a.sched_w), dim3(256), 0, a.stream, (const char *)a.q, (const char *)a.k_pages,
+                           (const char *)a.v_pages, a.k_scales, a.v_scales, a.block_table, a.out, (const int32_t *)(a.ws + p.off_header),
+                           (const int32_t *)(a.ws + p.off_unit_meta), (const int32_t *)(a.ws + p.off_sched),
+                           (const unsigned long long *)(a.ws + p.off_anc), (float *)(a.ws + p.off_part_ml),
+                           (float *)(a.ws + p.off_part_o), d.n_q_heads, d.n_kv_heads, d.max_pages_per_req, p.max_rows,
+                           a.n_row_groups, a.scale_log2, d.out_dtype, a.sched_cus, direct_args(a));
+    });
+    return hipGetLastError();
+}
+
+}  // namespace adaspec

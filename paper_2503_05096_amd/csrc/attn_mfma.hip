@@ -473,6 +473,8 @@ void attn_mfma_shape(AttnArgs &a, AttnKind kind)
         slots = attn_f32_grid_slots(a, device_cus());
     } else if (kind == AttnKind::kMfma64) {
         slots = attn_d64_grid_slots(a, device_cus());
+    } else if (kind == AttnKind::kMfmaE4m3) {
+        slots = attn_e4m3_grid_slots(a, device_cus());
     } else if (rt > 2) {
         slots = p.row_split ? attn_rows_grid_slots(a, device_cus()) : attn_ring_grid_slots(a, device_cus());
     } else {

@@ -1,4 +1,4 @@
-// Portable vector-ALU verification attention: any of the three storage types,
+// Portable vector-ALU verification attention: any of the three storage types, or (kScaled) a cache of 8 bits,
 // any head_dim that is a multiple of 8 up to 256.  One wavefront per
 // (work item, kv head, chunk of 8 query rows).  It is the path for head dims the
 // matrix-core kernels do not take (they take 64 and 128); speed is secondary
@@ -7,18 +7,34 @@
 // Per 64-token block:  lane <-> token for the scores (each lane walks its key
 // row, the query rows are broadcast from LDS), wavefront reductions for the
 // online-softmax statistics, then lane <-> channel for P.V (the 64 weights of a
-// row are broadcast from LDS while the lanes read a value row coalesced).
+// row are broadcast from LDS while the lanes read a value row coalesced).  The scale of a page's keys is applied to their
+// scores, the scale of its values to their weights.
 #include "adaspec_internal.h"
 #include "device_utils.h"
+#include "e4m3.h"
 
 namespace adaspec {
 
 constexpr int kRC = 8;      // query rows per unit
 constexpr int kMaxD = 256;
+constexpr uint32_t kHidden = 0x7fcabcdeu;       // weight of a token that a row does not see
 
-template <class T>
+template <class T, bool kScaled>
+__device__ __forceinline__ float load_cached(const void *pages, int64_t at)
+{
+    if constexpr (kScaled) {
+        float x, unused;
+        e4m3_to_float2<false>(static_cast<const uint8_t *>(pages)[at], x, unused);
+        return x;
+    } else {
+        return load_as_float<T>(pages, at);
+    }
+}
+
+template <class T, bool kScaled>
 __global__ __launch_bounds__(64) void attn_vector_kernel(
     const void *__restrict__ q, const void *__restrict__ k_pages, const void *__restrict__ v_pages,
+    const float *__restrict__ k_scales, const float *__restrict__ v_scales,
     const int32_t *__restrict__ block_table, const int32_t *__restrict__ ctx_lens,
     const int32_t *__restrict__ spec_lens, void *__restrict__ out, const int32_t *__restrict__ header,
     const int32_t *__restrict__ cu_q, const int32_t *__restrict__ split_base,
@@ -77,20 +93,26 @@ __global__ __launch_bounds__(64) void attn_vector_kernel(
         for (int tb = t0; tb < t1; tb += 64) {
             const int t = tb + lane;
             const bool valid = t < t1;
-            float sc[kRC];
+            float sc[kRC], vs = 0.f;
 #pragma unroll
             for (int r = 0; r < kRC; ++r) sc[r] = 0.f;
             if (valid) {
                 const int64_t page = block_table[(int64_t)i * max_pages_per_req + t / P];
+                if constexpr (kScaled) vs = v_scales[page * Hkv + g];
                 const int64_t koff = ((page * Hkv + g) * P + t % P) * (int64_t)d;
                 for (int c = 0; c < d; c += 8) {
                     float kv[8];
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) kv[e] = load_as_float<T>(k_pages, koff + c + e);
+                    for (int e = 0; e < 8; ++e) kv[e] = load_cached<T, kScaled>(k_pages, koff + c + e);
 #pragma unroll
                     for (int r = 0; r < kRC; ++r)
 #pragma unroll
                         for (int e = 0; e < 8; ++e) sc[r] = fmaf(qs[r][c + e], kv[e], sc[r]);
+                }
+                if constexpr (kScaled) {
+                    const float ks = k_scales[page * Hkv + g];
+#pragma unroll
+                    for (int r = 0; r < kRC; ++r) sc[r] *= ks;
                 }
             }
             __syncthreads();   // previous block's ps[] fully consumed
@@ -112,7 +134,9 @@ __global__ __launch_bounds__(64) void attn_vector_kernel(
                 m[r] = mn;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) acc[r][e] *= alpha;
-                ps[r][lane] = p;
+                // (a token that the row does not see has no weight, whatever its value: NaN marks it)
+                if constexpr (kScaled) ps[r][lane] = vis ? p * vs : __uint_as_float(kHidden);
+                else ps[r][lane] = p;
             }
             __syncthreads();
             const int cnt = min(64, t1 - tb);
@@ -124,11 +148,12 @@ __global__ __launch_bounds__(64) void attn_vector_kernel(
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const int c = lane + 64 * e;
-                    vv[e] = c < d ? load_as_float<T>(v_pages, voff + c) : 0.f;
+                    vv[e] = c < d ? load_cached<T, kScaled>(v_pages, voff + c) : 0.f;
                 }
 #pragma unroll
                 for (int r = 0; r < kRC; ++r) {
                     const float p = ps[r][tt];
+                    if (kScaled && __float_as_uint(p) == kHidden) continue;
 #pragma unroll
                     for (int e = 0; e < 4; ++e) acc[r][e] = fmaf(p, vv[e], acc[r][e]);
                 }
@@ -169,10 +194,10 @@ hipError_t launch_attn_vector(const AttnArgs &a)
     const int64_t max_units = (int64_t)p.max_items * d.n_kv_heads * n_row_chunks;
     if (max_units == 0) return hipSuccess;
     const int grid = (int)(max_units < 256 * 16 ? max_units : 256 * 16);
-    auto launch = [&](auto tag) {
+    auto launch_as = [&](auto tag, auto scaled) {
         using T = decltype(tag);
-        hipLaunchKernelGGL(attn_vector_kernel<T>, dim3(grid), dim3(64), 0, a.stream, a.q, a.k_pages,
-                           a.v_pages, a.block_table, a.ctx_lens, a.spec_lens, a.out,
+        hipLaunchKernelGGL((attn_vector_kernel<T, decltype(scaled)::value>), dim3(grid), dim3(64), 0, a.stream, a.q, a.k_pages,
+                           a.v_pages, a.k_scales, a.v_scales, a.block_table, a.ctx_lens, a.spec_lens, a.out,
                            (const int32_t *)(a.ws + p.off_header), (const int32_t *)(a.ws + p.off_cu_q),
                            (const int32_t *)(a.ws + p.off_split_base),
                            (const int32_t *)(a.ws + p.off_item_req),
@@ -182,6 +207,10 @@ hipError_t launch_attn_vector(const AttnArgs &a)
                            (float *)(a.ws + p.off_part_o), d.n_q_heads, d.n_kv_heads, d.head_dim,
                            d.page_size, d.max_pages_per_req, p.max_rows, n_row_chunks, p.split_tokens,
                            p.block_tokens, a.scale_log2, d.out_dtype);
+    };
+    auto launch = [&](auto tag) {
+        if (a.k_scales) launch_as(tag, std::true_type{});
+        else launch_as(tag, std::false_type{});
     };
     if (d.dtype == ADASPEC_F32) launch(F32{});
     else if (d.dtype == ADASPEC_F16) launch(F16{});

@@ -730,13 +730,47 @@ __global__ __launch_bounds__(kPagesThreads) void copy_pages_kernel(uint4 *__rest
     }
 }
 
-hipError_t launch_kv_copy_pages(void *k_pages, void *v_pages, const int32_t *copy_src, const int32_t *copy_dst, int n_copies,
-                                const adaspec_copy_dims &d, hipStream_t stream)
+// The scales of a cache of 8 bits go with its pages: page_scales of K and of V per page.
+__global__ __launch_bounds__(kPagesThreads) void copy_scales_kernel(float *__restrict__ k_scales, float *__restrict__ v_scales,
+                                                                    const int32_t *__restrict__ copy_src,
+                                                                    const int32_t *__restrict__ copy_dst, int n_copies, int layers,
+                                                                    int num_pages, int page_scales)
 {
-    const int64_t page_vecs = (int64_t)d.n_kv_heads * d.page_size * d.head_dim * (d.dtype == ADASPEC_F32 ? 4 : 2) / 16;
+    const int64_t work = (int64_t)n_copies * layers * page_scales;
+    for (int64_t w = (int64_t)blockIdx.x * kPagesThreads + threadIdx.x; w < work; w += (int64_t)gridDim.x * kPagesThreads) {
+        const int h = (int)(w % page_scales), layer = (int)(w / page_scales % layers), i = (int)(w / page_scales / layers);
+        const int s = copy_src[i], t = copy_dst[i];
+        if (s < 0 || t < 0 || s >= num_pages || t >= num_pages) continue;
+        const int64_t from = ((int64_t)layer * num_pages + s) * page_scales + h, to = ((int64_t)layer * num_pages + t) * page_scales + h;
+        k_scales[to] = k_scales[from];
+        v_scales[to] = v_scales[from];
+    }
+}
+
+static hipError_t copy_pages(void *k_pages, void *v_pages, const int32_t *copy_src, const int32_t *copy_dst, int n_copies,
+                             const adaspec_copy_dims &d, int element, hipStream_t stream)
+{
+    const int64_t page_vecs = (int64_t)d.n_kv_heads * d.page_size * d.head_dim * element / 16;
     const int64_t work = (int64_t)n_copies * d.layers;
     hipLaunchKernelGGL(copy_pages_kernel, dim3((unsigned)(work < 4096 ? work : 4096)), dim3(kPagesThreads), 0, stream, (uint4 *)k_pages,
                        (uint4 *)v_pages, copy_src, copy_dst, n_copies, d.layers, d.num_pages, page_vecs);
+    return hipGetLastError();
+}
+
+hipError_t launch_kv_copy_pages(void *k_pages, void *v_pages, const int32_t *copy_src, const int32_t *copy_dst, int n_copies,
+                                const adaspec_copy_dims &d, hipStream_t stream)
+{
+    return copy_pages(k_pages, v_pages, copy_src, copy_dst, n_copies, d, d.dtype == ADASPEC_F32 ? 4 : 2, stream);
+}
+
+hipError_t launch_kv_copy_pages_scaled(void *k_pages, void *v_pages, float *k_scales, float *v_scales, const int32_t *copy_src,
+                                       const int32_t *copy_dst, int n_copies, const adaspec_copy_dims &d, hipStream_t stream)
+{
+    const hipError_t e = copy_pages(k_pages, v_pages, copy_src, copy_dst, n_copies, d, 1, stream);
+    if (e != hipSuccess) return e;
+    const int64_t groups = ((int64_t)n_copies * d.layers * d.n_kv_heads + kPagesThreads - 1) / kPagesThreads;
+    hipLaunchKernelGGL(copy_scales_kernel, dim3((unsigned)(groups < 1024 ? groups : 1024)), dim3(kPagesThreads), 0, stream, k_scales, v_scales,
+                       copy_src, copy_dst, n_copies, d.layers, d.num_pages, d.n_kv_heads);
     return hipGetLastError();
 }
 

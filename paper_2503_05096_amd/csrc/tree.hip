@@ -10,6 +10,7 @@
 // the same float operations in the same order as the portable chain kernel.
 #include "adaspec_internal.h"
 #include "device_utils.h"
+#include "e4m3.h"
 #include "tree_masks.h"
 
 namespace adaspec {
@@ -426,6 +427,81 @@ hipError_t launch_kv_compact_path(void *k_pages, void *v_pages, const int32_t *b
                        (char *)k_pages, (char *)v_pages, block_table, ctx_lens, spec_lens, out_path,
                        out_accept_len, d.max_spec_len, d.n_kv_heads, row_bytes, d.page_size,
                        d.max_pages_per_req, path_stride);
+    return hipGetLastError();
+}
+
+// The same in a cache of 8 bits, where a row's bytes mean something only with the scale of its page.  One wavefront per (request, kv
+// head, K or V).  First the scale of every page that rows move into: the largest of its own and of those that they come from, so
+// that no byte overflows; then the page's earlier rows, where that is a change, and the moved rows, in rising order (path[j] >= j + 1:
+// a destination is never a source that is still to be read), are rounded from their old scale to the new one.  New scales are put
+// down last: rows still to be read are in the old ones.
+__global__ __launch_bounds__(64) void kv_compact_path_scaled_kernel(
+    uint8_t *__restrict__ k_pages, uint8_t *__restrict__ v_pages, float *__restrict__ k_scales, float *__restrict__ v_scales,
+    const int32_t *__restrict__ block_table, const int32_t *__restrict__ ctx_lens, const int32_t *__restrict__ spec_lens,
+    const int32_t *__restrict__ out_path, const int32_t *__restrict__ out_accept_len,
+    int max_spec_len, int Hkv, int d, int num_pages, int max_pages_per_req, int path_stride)
+{
+    constexpr int kP = kPageTokens, kMostPages = 64 / kP + 1;       // that 64 nodes may lie in
+    const int i = blockIdx.y, h = blockIdx.x >> 1, lane = threadIdx.x;
+    const int k = min(max(spec_lens[i], 0), min(max_spec_len, 63));
+    const int a = min(max(out_accept_len[i], 0), k);
+    const int base = ctx_lens[i] - (k + 1);
+    if (base < 0 || a == 0) return;
+    // lane j: accepted node j (they rise; what does not ends the path)
+    const int node = lane < a ? out_path[(int64_t)i * path_stride + lane] : 0;
+    int before = __shfl_up(node, 1, kWave);
+    if (lane == 0) before = 0;
+    const unsigned long long bad = __ballot(lane < a && (node <= before || node > k));
+    const int len = bad ? (int)__builtin_ctzll(bad) : a;
+    // lane p: page p of those that the nodes lie in
+    const int first = base / kP, last = (base + k) / kP;
+    int page = -1;
+    if (lane <= last - first && first + lane < max_pages_per_req) page = block_table[(int64_t)i * max_pages_per_req + first + lane];
+    if (__ballot(lane <= last - first && (page < 0 || page >= num_pages))) return;
+    const int64_t at = (int64_t)max(page, 0) * Hkv + h;
+    float *scales = (blockIdx.x & 1) ? v_scales : k_scales;
+    uint8_t *pages = (blockIdx.x & 1) ? v_pages : k_pages;
+    const float old = page >= 0 ? scales[at] : 0.f;
+    // Every destination page: the largest scale of it and of its rows' sources.
+    const int src_page = (base + node) / kP - first, dst_page = (base + 1 + lane) / kP - first;
+    const float from = __shfl(old, src_page, kWave);
+    float now = old;
+    for (int p = 0; p < kMostPages; ++p) {
+        const float most = wave_max(lane < len && dst_page == p ? from : 0.f);
+        if (lane == p && most > old) now = most;
+    }
+    // rows before the first destination, in the pages whose scale changes
+    for (int p = 0; p <= last - first; ++p) {
+        const float s0 = __shfl(old, p, kWave), s1 = __shfl(now, p, kWave);
+        const int kept = min(max(base + 1 - (first + p) * kP, 0), kP);
+        if (s0 == s1) continue;
+        uint8_t *block = pages + __shfl(at, p, kWave) * kP * d;
+        const float ratio = s0 / s1;
+        for (int c = lane; c < kept * d / 8; c += kWave) e4m3_rescale8(block + 8 * c, block + 8 * c, ratio);
+    }
+    for (int j = 0; j < len; ++j) {
+        const int src = base + __shfl(node, j, kWave), dst = base + 1 + j;
+        const int sp = src / kP - first, dp = dst / kP - first;
+        const float s0 = __shfl(old, sp, kWave), s1 = __shfl(now, dp, kWave);
+        const bool rescaled = s0 != s1;
+        if (src == dst && !rescaled) continue;
+        const uint8_t *r = pages + (__shfl(at, sp, kWave) * kP + src % kP) * d;
+        uint8_t *w = pages + (__shfl(at, dp, kWave) * kP + dst % kP) * d;
+        for (int c = lane; c < d / 8; c += kWave) {
+            if (rescaled) e4m3_rescale8(r + 8 * c, w + 8 * c, s0 / s1);
+            else *reinterpret_cast<uint2 *>(w + 8 * c) = *reinterpret_cast<const uint2 *>(r + 8 * c);
+        }
+    }
+    if (now != old) scales[at] = now;
+}
+
+hipError_t launch_kv_compact_path_scaled(void *k_pages, void *v_pages, float *k_scales, float *v_scales, const int32_t *block_table,
+                                         const int32_t *ctx_lens, const int32_t *spec_lens, const int32_t *out_path,
+                                         const int32_t *out_accept_len, const adaspec_attn_dims &d, int path_stride, hipStream_t stream)
+{
+    hipLaunchKernelGGL(kv_compact_path_scaled_kernel, dim3(2 * d.n_kv_heads, d.batch), dim3(64), 0, stream, (uint8_t *)k_pages,
+                       (uint8_t *)v_pages, k_scales, v_scales, block_table, ctx_lens, spec_lens, out_path, out_accept_len, d.max_spec_len,
+                       d.n_kv_heads, d.head_dim, d.num_pages, d.max_pages_per_req, path_stride);
     return hipGetLastError();
 }
 

@@ -67,8 +67,13 @@ struct Api {
     decltype(&adaspec_kv_compact_pages_workspace_bytes) compact_ws;
     decltype(&adaspec_kv_compact_pages) compact;
     decltype(&adaspec_kv_copy_pages) copy_pages;
+    // (and from here on again)
+    decltype(&adaspec_rope) rope;
+    decltype(&adaspec_kv_append_rope) append_rope;
+    decltype(&adaspec_verify_attn_scaled_workspace_bytes) attn_scaled_ws;
+    decltype(&adaspec_verify_attn_scaled) attn_scaled;
 } api;
-constexpr Py_ssize_t kEntries = sizeof(Api) / sizeof(void *), kRequired = kEntries - 7;
+constexpr Py_ssize_t kEntries = sizeof(Api) / sizeof(void *), kPages = kEntries - 4, kRequired = kPages - 7;
 PyObject *get_workspace, *raw_stream, *current_device;   // binding._workspace, torch._C._cuda_getCurrentRawStream / _getDevice
 PyObject *error_class;                                   // binding.AdaspecError
 bool ready = false;
@@ -509,6 +514,168 @@ PyObject *kv_copy_pages(PyObject *, PyObject *const *a, Py_ssize_t nargs)
     });
 }
 
+// rows [TQ][heads][d] whose heads lie side by side; binding._ragged_rows
+int64_t ragged_rows(const at::Tensor &x, const at::Tensor &like)
+{
+    need(x.dim() == 3 && x.stride(2) == 1 && (x.stride(1) == x.size(2) || x.size(1) == 1));
+    need(x.scalar_type() == like.scalar_type() && device_index(x) == device_index(like) && x.size(0) == like.size(0) && x.size(2) == like.size(2));
+    return x.size(0) > 1 ? x.stride(0) : std::max(x.stride(0), x.size(1) * x.size(2)) / 8 * 8;
+}
+// a tensor of integers, or none
+const int32_t *ints_or_null(PyObject *o, int64_t n, const at::Tensor &like)
+{
+    if (o == Py_None) return nullptr;
+    const at::Tensor &t = dense(o, at::kInt);
+    need(t.dim() == 1 && t.size(0) == n && device_index(t) == device_index(like));
+    return ptr<int32_t>(t);
+}
+// what rope and kv_append_rope share: positions
+struct Turns {
+    adaspec_rope_dims d = {};
+    const float *inv_freq = nullptr;
+    Turns(const at::Tensor &x, PyObject *freq, const at::Tensor &ctx, const at::Tensor &spec, PyObject *max_spec_len, PyObject *interleaved, PyObject *factor)
+    {
+        need(ctx.dim() == 1 && spec.dim() == 1 && ctx.size(0) == spec.size(0) && x.dim() == 3);
+        d.batch = size32(spec.size(0));
+        d.total_q = size32(x.size(0));
+        d.max_spec_len = small_int(max_spec_len);
+        d.head_dim = size32(x.size(2));
+        d.page_size = 16;
+        d.dtype = dtype_code(x.scalar_type());
+        if (freq != Py_None) {
+            const at::Tensor &f = dense(freq, at::kFloat);
+            need(f.dim() == 1 && device_index(f) == device_index(x));
+            d.rot_dim = size32(2 * f.size(0));
+            inv_freq = ptr<float>(f);
+        }
+        need((interleaved == Py_True || interleaved == Py_False) && PyFloat_CheckExact(factor) && PyFloat_AS_DOUBLE(factor) > 0);
+        d.interleaved = interleaved == Py_True;
+        d.attn_factor = (float)PyFloat_AS_DOUBLE(factor);
+        need(d.attn_factor > 0);
+    }
+};
+
+// (x, inv_freq, ctx_lens, spec_lens, max_spec_len, interleaved, attn_factor, parents, out, stream)
+PyObject *rope(PyObject *, PyObject *const *a, Py_ssize_t nargs)
+{
+    return guarded(nargs, 10, [&]() -> PyObject * {
+        need(api.rope && a[1] != Py_None);
+        const at::Tensor &x = tensor(a[0]), &ctx = dense(a[2], at::kInt), &spec = dense(a[3], at::kInt);
+        Turns t(x, a[1], ctx, spec, a[4], a[5], a[6]);
+        t.d.n_q_heads = size32(x.size(1));
+        t.d.q_row_stride = ragged_rows(x, x);
+        const int32_t *parents = ints_or_null(a[7], x.size(0), x);
+        on_current_device({&x, &ctx, &spec});
+        const Output out(a[8], x.sizes(), x.scalar_type(), x);
+        need(out.t.sizes() == x.sizes());
+        t.d.q_out_row_stride = ragged_rows(out.t, x);
+        void *s = stream_of(a[9]);
+        call("adaspec_rope", api.rope, ptr(x), t.inv_freq, ptr(out.t), ptr<int32_t>(ctx), ptr<int32_t>(spec), parents, &t.d, s);
+        return out.result();
+    });
+}
+
+// a cache of 8 bits: binding._scaled_cache
+void scaled_cache(const at::Tensor &k, const at::Tensor &v, const at::Tensor &ks, const at::Tensor &vs)
+{
+    need(k.scalar_type() == at::kFloat8_e4m3fn && v.scalar_type() == at::kFloat8_e4m3fn && k.dim() == 4 && v.sizes() == k.sizes());
+    need(ks.dim() == 2 && ks.size(0) == k.size(0) && ks.size(1) == k.size(1) && vs.sizes() == ks.sizes());
+    for (const at::Tensor *t : {&k, &v}) need(t->is_contiguous());
+}
+
+// (q, k_new, v_new, inv_freq, k_pages, v_pages, block_table, ctx_lens, spec_lens, max_spec_len, k_scales, v_scales, interleaved,
+//  attn_factor, parents, q_out, stream)
+PyObject *kv_append_rope(PyObject *, PyObject *const *a, Py_ssize_t nargs)
+{
+    return guarded(nargs, 17, [&]() -> PyObject * {
+        need(api.append_rope != nullptr);
+        const at::Tensor &kn = tensor(a[1]), &vn = tensor(a[2]), &k = tensor(a[4]), &v = tensor(a[5]);
+        const at::Tensor &bt = dense(a[6], at::kInt), &ctx = dense(a[7], at::kInt), &spec = dense(a[8], at::kInt);
+        Turns t(kn, a[3], ctx, spec, a[9], a[12], a[13]);
+        need(k.dim() == 4 && bt.dim() == 2 && bt.size(0) == ctx.size(0) && vn.sizes() == kn.sizes() && v.sizes() == k.sizes());
+        need(k.size(1) == kn.size(1) && k.size(3) == kn.size(2));
+        on_current_device({&kn, &vn, &k, &v, &bt, &ctx, &spec});
+        float *k_scales = nullptr, *v_scales = nullptr;
+        if (a[10] != Py_None || a[11] != Py_None) {
+            const at::Tensor &ks = dense(a[10], at::kFloat), &vs = dense(a[11], at::kFloat);
+            scaled_cache(k, v, ks, vs);
+            on_current_device({&ks, &vs});
+            k_scales = ptr<float>(ks);
+            v_scales = ptr<float>(vs);
+        } else {
+            for (const at::Tensor *p : {&k, &v}) need(p->is_contiguous() && p->scalar_type() == kn.scalar_type());
+        }
+        t.d.n_kv_heads = size32(kn.size(1));
+        t.d.page_size = size32(k.size(2));
+        t.d.num_pages = size32(k.size(0));
+        t.d.max_pages_per_req = size32(bt.size(1));
+        t.d.k_row_stride = ragged_rows(kn, kn);
+        t.d.v_row_stride = ragged_rows(vn, kn);
+        const int32_t *parents = ints_or_null(a[14], kn.size(0), kn);
+        need((a[0] != Py_None) || a[15] == Py_None);
+        need(a[0] == Py_None || a[3] != Py_None);
+        void *s = stream_of(a[16]);
+        const auto run = [&](const void *q, void *q_out) {
+            call("adaspec_kv_append_rope", api.append_rope, q, ptr(kn), ptr(vn), t.inv_freq, q_out, ptr(k), ptr(v), k_scales, v_scales, ptr<int32_t>(bt),
+                 ptr<int32_t>(ctx), ptr<int32_t>(spec), parents, &t.d, s);
+        };
+        if (a[0] == Py_None) {
+            run(nullptr, nullptr);
+            Py_RETURN_NONE;
+        }
+        const at::Tensor &q = tensor(a[0]);
+        t.d.q_row_stride = ragged_rows(q, kn);
+        t.d.n_q_heads = size32(q.size(1));
+        const Output out(a[15], q.sizes(), q.scalar_type(), q);
+        need(out.t.sizes() == q.sizes());
+        t.d.q_out_row_stride = ragged_rows(out.t, q);
+        run(ptr(q), ptr(out.t));
+        return out.result();
+    });
+}
+
+// (q, k_pages, v_pages, k_scales, v_scales, block_table, ctx_lens, spec_lens, out, max_spec_len, scale, out_dtype, plan, workspace,
+//  stream, parents)
+PyObject *verify_attn_scaled(PyObject *, PyObject *const *a, Py_ssize_t nargs)
+{
+    return guarded(nargs, 16, [&]() -> PyObject * {
+        need(api.attn_scaled != nullptr);
+        const at::Tensor &q = tensor(a[0]), &k = tensor(a[1]), &v = tensor(a[2]), &ks = dense(a[3], at::kFloat), &vs = dense(a[4], at::kFloat);
+        const at::Tensor &bt = dense(a[5], at::kInt), &ctx = dense(a[6], at::kInt), &spec = dense(a[7], at::kInt);
+        need(q.dim() == 3 && bt.dim() == 2 && ctx.dim() == 1 && spec.dim() == 1 && ctx.size(0) == bt.size(0) && spec.size(0) == bt.size(0));
+        scaled_cache(k, v, ks, vs);
+        need(q.is_contiguous() && k.size(3) == q.size(2));
+        adaspec_attn_dims d = {};
+        d.batch = size32(bt.size(0));
+        d.total_q = size32(q.size(0));
+        d.max_spec_len = small_int(a[9]);
+        d.n_q_heads = size32(q.size(1));
+        d.n_kv_heads = size32(k.size(1));
+        d.head_dim = size32(q.size(2));
+        d.page_size = size32(k.size(2));
+        d.num_pages = size32(k.size(0));
+        d.max_pages_per_req = size32(bt.size(1));
+        d.dtype = dtype_code(q.scalar_type());
+        d.out_dtype = a[11] == Py_None ? d.dtype : small_int(a[11]);
+        need(PyFloat_CheckExact(a[10]));
+        d.scale = (float)PyFloat_AS_DOUBLE(a[10]);
+        const bool reuse = is_word(a[12], "reuse");
+        need((reuse && a[13] != Py_None) || is_word(a[12], "run"));
+        d.plan_mode = reuse ? ADASPEC_PLAN_REUSE : ADASPEC_PLAN_BUILD_AND_RUN;
+        const size_t nbytes = api.attn_scaled_ws(&d);
+        need(nbytes > 0);
+        const int32_t *parents = ints_or_null(a[15], q.size(0), q);
+        on_current_device({&q, &k, &v, &ks, &vs, &bt, &ctx, &spec});
+        const Output out(a[8], q.sizes(), scalar_type(d.out_dtype), q);
+        need(out.t.is_contiguous() && out.t.sizes() == q.sizes() && out.t.scalar_type() == scalar_type(d.out_dtype) && device_index(out.t) == device_index(q));
+        const at::Tensor ws = scratch(a[13], nbytes, a[14], q);
+        void *s = stream_of(a[14]);
+        call("adaspec_verify_attn_scaled", api.attn_scaled, ptr(q), ptr(k), ptr(v), ptr<float>(ks), ptr<float>(vs), ptr<int32_t>(bt), ptr<int32_t>(ctx),
+             ptr<int32_t>(spec), parents, ptr(out.t), &d, ptr(ws), (size_t)ws.numel(), s);
+        return out.result();
+    });
+}
+
 struct Rows {                                          // what accept and accept_tree share
     adaspec_accept_dims d = {};
     const void *probs = nullptr;
@@ -695,8 +862,8 @@ PyObject *setup(PyObject *, PyObject *args)
     if (!PyArg_ParseTuple(args, "O!OOOO", &PyTuple_Type, &table, &ws, &stream, &device, &error)) return nullptr;
     void **slot = reinterpret_cast<void **>(&api);
     const Py_ssize_t n = PyTuple_GET_SIZE(table);
-    if (n != kRequired && n != kEntries) {
-        PyErr_Format(PyExc_ValueError, "expected %zd or %zd entry points", kRequired, kEntries);
+    if (n != kRequired && n != kPages && n != kEntries) {
+        PyErr_Format(PyExc_ValueError, "expected %zd, %zd or %zd entry points", kRequired, kPages, kEntries);
         return nullptr;
     }
     api = {};
@@ -724,6 +891,7 @@ PyObject *set_meta_index(PyObject *, PyObject *i)
 PyMethodDef methods[] = {FASTCALL(verify_attn), FASTCALL(accept), FASTCALL(accept_tree), FASTCALL(kv_append),
                          FASTCALL(kv_compact_path), FASTCALL(commit), FASTCALL(draft_sample), FASTCALL(verify_attn_window),
                          FASTCALL(kv_remap), FASTCALL(kv_compact_pages), FASTCALL(kv_copy_pages),
+                         FASTCALL(rope), FASTCALL(kv_append_rope), FASTCALL(verify_attn_scaled),
 #ifdef ADASPEC_FASTCALL_ON_META
                          {"set_meta_index", set_meta_index, METH_O, nullptr},
 #endif
