@@ -12,7 +12,7 @@
 //   * No LDS tile for V^T: a lane loads D / 16 neighbouring channels of the four tokens 4g .. 4g + 3 of a page, and byte
 //     permutes put equal channels of two tokens side by side, which is what the conversion takes (two bytes in, two bf16
 //     out).  The lane then holds D / 16 whole operand columns: tile t of O^T has channel (D / 16) m + t in row m.
-// A block is 32 tokens of 128 channels or 64 of 64: 8 KB of K and V per wavefront, 32 registers, double-buffered.
+// A block is 32 tokens of 128 channels or 64 of 64: 8 KB of K and V per wavefront, 32 registers.
 //
 // Bound: HBM.
 #include <type_traits>
@@ -38,7 +38,7 @@ template <class T> __device__ __forceinline__ uint4 e4m3_operand(uint32_t lo, ui
 __device__ __forceinline__ uint32_t e4m3_nans(uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
 
 template <class T, int D, int RT, bool kTree, bool kDirect>
-__global__ __launch_bounds__(256, (RT <= 2 ? 2 : 1)) void attn_e4m3_kernel(
+__global__ __launch_bounds__(256, (RT == 1 ? 3 : 2)) void attn_e4m3_kernel(
     const char *__restrict__ q, const char *__restrict__ k_pages, const char *__restrict__ v_pages,
     const float *__restrict__ k_scales, const float *__restrict__ v_scales,
     const int32_t *__restrict__ block_table, void *__restrict__ out, const int32_t *__restrict__ header,
@@ -54,11 +54,11 @@ __global__ __launch_bounds__(256, (RT <= 2 ? 2 : 1)) void attn_e4m3_kernel(
     constexpr int kTiles = D / 16;                                  // of O^T
     constexpr int kHalves = kTokens / 32;
     constexpr int kORow = D + 4;                                    // floats per row of the merge buffer (padded: conflict-free b128)
-    constexpr int kSlab = kRows * kORow * 4;
+    constexpr int kSlab = 16 * kORow * 4;                           // a row tile's state of one wavefront
     constexpr int kQEntries = RT * kSteps * 64, kQLoads = (kQEntries + 255) / 256;
     __shared__ __attribute__((aligned(16))) char smem[kWaves * kSlab];
     __shared__ __attribute__((aligned(16))) uint4 q_lds[kQEntries];   // Q^T operands, MFMA lane order
-    __shared__ float s_m[kWaves][kRows], s_l[kWaves][kRows];
+    __shared__ float s_m[kWaves][16], s_l[kWaves][16];
     __shared__ unsigned long long s_anc[kTree ? kRows : 1];         // ancestor mask of each row of the unit
 
     const int tid = threadIdx.x, lane = tid & 63;
@@ -69,11 +69,9 @@ __global__ __launch_bounds__(256, (RT <= 2 ? 2 : 1)) void attn_e4m3_kernel(
     float *my_state = reinterpret_cast<float *>(smem + wv * kSlab);
 
     // K: lane (g, m) <- token 16 mt + m, channels 64 c + 16 g .. + 15.  V: lane (g, m) <- token 16 p + 4 g + i, channels (D / 16) m ..
-    struct Block {
-        uint4 k[kPages][kKLoads];
-        uint32_t v[kPages][4][kWords];
-        float ks[kPages], vs[kPages];
-    };
+    uint4 kreg[kPages][kKLoads];
+    uint32_t vreg[kPages][4][kWords];
+    float ks[kPages], vs[kPages];                                   // scales of the block in registers
     const uint32_t k_lane_off = n16 * D + 16 * g;
     const uint32_t v_lane_off = (4 * g) * D + kTiles * n16;
 
@@ -106,36 +104,47 @@ __global__ __launch_bounds__(256, (RT <= 2 ? 2 : 1)) void attn_e4m3_kernel(
 
     // Page ids and scales by scalar loads; pages past the split's end are replaced by the block's first (masks and the tail code
     // keep what they hold out of the result), so that every block issues the same loads.
-    auto load_block = [&](const Unit &u, int bi, Block &b) {
+    auto page_blocks = [&](const Unit &u, int bi, int64_t (&b)[kPages]) {
         const int tb = u.t0 + bi * kTokens;
         const int64_t at = u.bt_off + (tb >> 4);
-        int64_t block[kPages];
 #pragma unroll
-        for (int p = 0; p < kPages; ++p) {
-            const int64_t page = block_table[tb + 16 * p < u.t1 ? at + p : at];
-            block[p] = page * Hkv + u.gkv;
-        }
+        for (int p = 0; p < kPages; ++p) b[p] = (int64_t)block_table[tb + 16 * p < u.t1 ? at + p : at] * Hkv + u.gkv;
+    };
+    auto load_k = [&](const int64_t (&b)[kPages]) {
 #pragma unroll
         for (int p = 0; p < kPages; ++p)
 #pragma unroll
-            for (int c = 0; c < kKLoads; ++c) b.k[p][c] = ld16_stream(k_pages + block[p] * (16 * D) + k_lane_off + 64 * c);
+            for (int c = 0; c < kKLoads; ++c) kreg[p][c] = ld16_stream(k_pages + b[p] * (16 * D) + k_lane_off + 64 * c);
+    };
+    auto load_v = [&](const int64_t (&b)[kPages]) {
 #pragma unroll
         for (int p = 0; p < kPages; ++p)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const char *at_v = v_pages + block[p] * (16 * D) + v_lane_off + i * D;
+                const char *at = v_pages + b[p] * (16 * D) + v_lane_off + i * D;
                 if constexpr (kWords == 2) {
-                    const u32x2v w = __builtin_nontemporal_load(reinterpret_cast<const u32x2v *>(at_v));
-                    b.v[p][i][0] = w.x;
-                    b.v[p][i][1] = w.y;
+                    const u32x2v w = __builtin_nontemporal_load(reinterpret_cast<const u32x2v *>(at));
+                    vreg[p][i][0] = w.x;
+                    vreg[p][i][1] = w.y;
                 } else {
-                    b.v[p][i][0] = __builtin_nontemporal_load(reinterpret_cast<const uint32_t *>(at_v));
+                    vreg[p][i][0] = __builtin_nontemporal_load(reinterpret_cast<const uint32_t *>(at));
                 }
             }
+    };
+    auto load_scales = [&](const int64_t (&b)[kPages]) {
 #pragma unroll
         for (int p = 0; p < kPages; ++p) {
-            b.ks[p] = k_scales[block[p]];
-            b.vs[p] = v_scales[block[p]];
+            ks[p] = k_scales[b[p]];
+            vs[p] = v_scales[b[p]];
+        }
+    };
+    auto first_loads = [&](const Unit &u) {
+        if (wv < u.nblk) {
+            int64_t b[kPages];
+            page_blocks(u, wv, b);
+            load_k(b);
+            load_v(b);
+            load_scales(b);
         }
     };
     // this thread's share of the unit's Q^T operands: entry (row tile, s, lane)
@@ -158,13 +167,12 @@ __global__ __launch_bounds__(256, (RT <= 2 ? 2 : 1)) void attn_e4m3_kernel(
     bool have;
     uint4 qv[kQLoads];
     unsigned long long av = 0ull;
-    Block b0, b1;
     if constexpr (kDirect) have = direct_unit(cur, direct, block_table, G, Hkv, n_row_groups, kRows, kTokens, max_pages_per_req, wv, lane);
     else have = next_unit(cur);
     if (have) {
         load_q(cur, qv);
         if constexpr (kTree) av = load_anc(cur);
-        if (wv < cur.nblk) load_block(cur, wv, b0);
+        first_loads(cur);
     }
 
     while (have) {
@@ -175,12 +183,6 @@ __global__ __launch_bounds__(256, (RT <= 2 ? 2 : 1)) void attn_e4m3_kernel(
         for (int k = 0; k < kQLoads; ++k)
             if (kQEntries % 256 == 0 || tid + 256 * k < kQEntries) q_lds[tid + 256 * k] = qv[k];
         if constexpr (kTree) { if (tid < kRows) s_anc[tid] = av; }
-        int pos[RT];
-#pragma unroll
-        for (int nt = 0; nt < RT; ++nt) {
-            const int row = u.r0 + 16 * nt + n16;
-            pos[nt] = row < u.rows ? (u.L - u.n + row / G) : -1;
-        }
         lds_barrier();
 
         float m[RT], lsum[RT];
@@ -192,9 +194,17 @@ __global__ __launch_bounds__(256, (RT <= 2 ? 2 : 1)) void attn_e4m3_kernel(
             for (int t = 0; t < kTiles; ++t) o[nt][t] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
 
-        auto block = [&](int bi, Block &b) {
-            const int tb = u.t0 + bi * kTokens;
+        // One block.  kInner: every row sees all of it, and another one follows, whose K and V are requested as soon as their
+        // registers are free (without a branch around the loads, so that the compiler's waits count exactly).
+        auto block = [&](int bi, auto inner_tag) {
+            constexpr bool kInner = decltype(inner_tag)::value;
             constexpr int kE = 4 * kPages;                          // scores per lane and row tile
+            const int tb = u.t0 + bi * kTokens;
+            int64_t nb[kPages];
+            const bool next = kInner || bi + kWaves < u.nblk;
+            const bool masked = !kInner && (tb + kTokens > first_masked || tb + kTokens > u.t1);
+            if (next) page_blocks(u, bi + kWaves, nb);
+
             // ---- S^T = K Q^T ------------------------------------------------------------
             float p[RT][kE];
 #pragma unroll
@@ -202,10 +212,11 @@ __global__ __launch_bounds__(256, (RT <= 2 ? 2 : 1)) void attn_e4m3_kernel(
                 uint4 kop[kSteps];
 #pragma unroll
                 for (int s = 0; s < kSteps; ++s) {
-                    const uint4 raw = b.k[mt][s >> 1];
+                    const uint4 raw = kreg[mt][s >> 1];
                     kop[s] = (s & 1) ? e4m3_operand<T>(raw.z, raw.w) : e4m3_operand<T>(raw.x, raw.y);
                 }
-                const float factor = b.ks[mt] * scale_log2;
+                const float factor = ks[mt] * scale_log2;
+                if constexpr (RT > 2) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                 for (int nt = 0; nt < RT; ++nt) {
                     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
@@ -213,31 +224,33 @@ __global__ __launch_bounds__(256, (RT <= 2 ? 2 : 1)) void attn_e4m3_kernel(
                     for (int s = 0; s < kSteps; ++s) acc = Mma<T>::run(kop[s], q_lds[(nt * kSteps + s) * 64 + lane], acc);
 #pragma unroll
                     for (int r = 0; r < 4; ++r) p[nt][4 * mt + r] = acc[r] * factor;
+                    if constexpr (RT > 3) __builtin_amdgcn_sched_barrier(0);
                 }
             }
+            __builtin_amdgcn_sched_barrier(0);
+            if (next) load_k(nb);
+            __builtin_amdgcn_sched_barrier(0);
 
             // ---- online softmax (per lane: row n16 of each row tile, kE of the tokens), in log2 units ----
-            const bool need_mask = (tb + kTokens > first_masked) || (tb + kTokens > u.t1);
-            uint32_t seen[RT];                                      // where there is a mask: bit e = the row sees token e
-            float vs[kPages];
-#pragma unroll
-            for (int mt = 0; mt < kPages; ++mt) vs[mt] = b.vs[mt];
+            uint32_t seen[RT];                                      // masked: bit e = the row sees token e
 #pragma unroll
             for (int nt = 0; nt < RT; ++nt) {
-                if (need_mask) {
+                if (masked) {
                     seen[nt] = 0;
                     const unsigned long long am = kTree ? s_anc[16 * nt + n16] : 0ull;
-                    const int base = u.L - u.n, lim = min(pos[nt], u.t1 - 1);
+                    const int row = u.r0 + 16 * nt + n16, base = u.L - u.n;
+                    const int pos = row < u.rows ? base + row / G : -1, lim = min(pos, u.t1 - 1);
 #pragma unroll
                     for (int e = 0; e < kE; ++e) {
                         const int t = tb + 16 * (e >> 2) + 4 * g + (e & 3), rel = t - base;
                         bool vis;
-                        if constexpr (kTree) vis = t < u.t1 && (rel < 0 ? pos[nt] >= 0 : ((am >> (rel & 63)) & 1ull) != 0);
+                        if constexpr (kTree) vis = t < u.t1 && (rel < 0 ? pos >= 0 : ((am >> (rel & 63)) & 1ull) != 0);
                         else vis = t <= lim;
                         p[nt][e] = vis ? p[nt][e] : -INFINITY;
                         seen[nt] |= vis ? 1u << e : 0u;
                     }
                 }
+                if constexpr (RT > 2) __builtin_amdgcn_sched_barrier(0);
                 float mx = p[nt][0];
 #pragma unroll
                 for (int e = 1; e < kE; ++e) mx = fmaxf(mx, p[nt][e]);
@@ -258,13 +271,14 @@ __global__ __launch_bounds__(256, (RT <= 2 ? 2 : 1)) void attn_e4m3_kernel(
                     p[nt][e] = __builtin_amdgcn_exp2f(p[nt][e] - m[nt]);
                     psum += p[nt][e];
                     p[nt][e] *= vs[e >> 2];
+                    // what hidden tokens hold stays out: no weight, whatever their scale
+                    if (masked) p[nt][e] = (seen[nt] >> e) & 1 ? p[nt][e] : 0.f;
                 }
                 lsum[nt] += psum;
             }
 
-            // ---- what hidden tokens hold stays out: no weight, whatever their scale; no value behind the request's end; NaN
-            // values only in rows that see them -------------------------------------------------------------------------------
-            if (need_mask) {
+            // ---- no value behind the request's end, and NaN values only in rows that see them ----
+            if (masked) {
                 uint32_t nans = 0;
 #pragma unroll
                 for (int pg = 0; pg < kPages; ++pg)
@@ -272,24 +286,20 @@ __global__ __launch_bounds__(256, (RT <= 2 ? 2 : 1)) void attn_e4m3_kernel(
                     for (int i = 0; i < 4; ++i)
 #pragma unroll
                         for (int w = 0; w < kWords; ++w) {
-                            if (tb + 16 * pg + 4 * g + i >= u.t1) b.v[pg][i][w] = 0;
-                            nans |= e4m3_nans(b.v[pg][i][w]);
+                            if (tb + 16 * pg + 4 * g + i >= u.t1) vreg[pg][i][w] = 0;
+                            nans |= e4m3_nans(vreg[pg][i][w]);
                         }
-#pragma unroll
-                for (int nt = 0; nt < RT; ++nt)
-#pragma unroll
-                    for (int e = 0; e < kE; ++e)
-                        if (!((seen[nt] >> e) & 1)) p[nt][e] = 0.f;
                 if (__builtin_expect(__builtin_amdgcn_ballot_w64(nans != 0) != 0, 0)) {
                     // rows that see a NaN, channel by channel: a product of what is NaN with what is seen
 #pragma unroll
                     for (int hf = 0; hf < kHalves; ++hf)
 #pragma unroll
                         for (int t = 0; t < kTiles; ++t) {
+                            __builtin_amdgcn_sched_barrier(0);
                             uint32_t bad[8];
 #pragma unroll
                             for (int e = 0; e < 8; ++e)
-                                bad[e] = (e4m3_nans(b.v[2 * hf + (e >> 2)][e & 3][t >> 2]) >> (8 * (t & 3))) & 0x80u ? 0x3f80u : 0u;
+                                bad[e] = (e4m3_nans(vreg[2 * hf + (e >> 2)][e & 3][t >> 2]) >> (8 * (t & 3))) & 0x80u ? 0x3f80u : 0u;
                             const uint4 a = make_uint4(bad[0] | bad[1] << 16, bad[2] | bad[3] << 16, bad[4] | bad[5] << 16, bad[6] | bad[7] << 16);
 #pragma unroll
                             for (int nt = 0; nt < RT; ++nt) {
@@ -309,12 +319,13 @@ __global__ __launch_bounds__(256, (RT <= 2 ? 2 : 1)) void attn_e4m3_kernel(
                         for (int i = 0; i < 4; ++i)
 #pragma unroll
                             for (int w = 0; w < kWords; ++w) {
-                                const uint32_t x = e4m3_nans(b.v[pg][i][w]);
-                                b.v[pg][i][w] &= ~(x | (x - (x >> 7)));         // NaN bytes become 0
+                                const uint32_t x = e4m3_nans(vreg[pg][i][w]);
+                                vreg[pg][i][w] &= ~(x | (x - (x >> 7)));        // NaN bytes become 0
                             }
                 }
             }
 
+            __builtin_amdgcn_sched_barrier(0);
             // ---- O^T += V^T P^T, 32 tokens at a time ------------------------------
 #pragma unroll
             for (int hf = 0; hf < kHalves; ++hf) {
@@ -335,9 +346,10 @@ __global__ __launch_bounds__(256, (RT <= 2 ? 2 : 1)) void attn_e4m3_kernel(
                         uint32_t pair[4];                           // two tokens, two channels: (t0 c0, t1 c0, t0 c1, t1 c1)
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
-                            const uint32_t(&v)[4][kWords] = b.v[2 * hf + (j >> 1)];
+                            const uint32_t(&v)[4][kWords] = vreg[2 * hf + (j >> 1)];
                             pair[j] = __builtin_amdgcn_perm(v[2 * (j & 1) + 1][w], v[2 * (j & 1)][w], up ? 0x07030602u : 0x05010400u);
                         }
+                        if constexpr (RT > 2) __builtin_amdgcn_sched_barrier(0);
                         const uint4 even = make_uint4(e4m3_pair<BF16, false>(pair[0]), e4m3_pair<BF16, false>(pair[1]),
                                                       e4m3_pair<BF16, false>(pair[2]), e4m3_pair<BF16, false>(pair[3]));
                         const uint4 odd = make_uint4(e4m3_pair<BF16, true>(pair[0]), e4m3_pair<BF16, true>(pair[1]),
@@ -352,84 +364,77 @@ __global__ __launch_bounds__(256, (RT <= 2 ? 2 : 1)) void attn_e4m3_kernel(
                         }
                     }
             }
+            if (next) {
+                load_v(nb);
+                load_scales(nb);
+            }
         };
 
-        // Two buffers: the loads of the next block are issued before this one is worked on, without a branch around them, so
-        // that the compiler's waits count exactly.
         if (wv < u.nblk) {
+            const int full = max(min(first_masked, u.t1) - u.t0, 0) / kTokens;         // blocks that every row sees all of
             int bi = wv;
-            for (; bi + 2 * kWaves < u.nblk; bi += 2 * kWaves) {
-                load_block(u, bi + kWaves, b1);
-                block(bi, b0);
-                load_block(u, bi + 2 * kWaves, b0);
-                block(bi + kWaves, b1);
-            }
-            if (bi + kWaves < u.nblk) {
-                load_block(u, bi + kWaves, b1);
-                block(bi, b0);
-                block(bi + kWaves, b1);
-            } else {
-                block(bi, b0);
-            }
+            for (; bi + kWaves < u.nblk && bi < full; bi += kWaves) block(bi, std::true_type{});
+            for (; bi < u.nblk; bi += kWaves) block(bi, std::false_type{});
         }
 
         // ---- next unit: its first block and its Q rows travel while this unit's states are merged
         if (have_next) {
             load_q(nxt, qv);
             if constexpr (kTree) av = load_anc(nxt);
-            if (wv < nxt.nblk) load_block(nxt, wv, b0);
+            first_loads(nxt);
         }
-        // ---- merge the four wavefronts' states through LDS (as in attn_mfma.hip) ----------
+        // ---- merge the four wavefronts' states through LDS (as in attn_mfma.hip), one row tile after the other ----------
 #pragma unroll
         for (int nt = 0; nt < RT; ++nt) {
+            if (nt > 0) lds_barrier();                              // (the tile before has been read)
             lsum[nt] += __shfl_xor(lsum[nt], 16, kWave);
             lsum[nt] += __shfl_xor(lsum[nt], 32, kWave);
-            if (g == 0) { s_m[wv][16 * nt + n16] = m[nt]; s_l[wv][16 * nt + n16] = lsum[nt]; }
+            if (g == 0) { s_m[wv][n16] = m[nt]; s_l[wv][n16] = lsum[nt]; }
 #pragma unroll
             for (int r = 0; r < 4; ++r)
 #pragma unroll
                 for (int t = 0; t < kTiles; t += 4)
-                    *reinterpret_cast<f32x4 *>(my_state + (16 * nt + n16) * kORow + kTiles * (4 * g + r) + t) =
+                    *reinterpret_cast<f32x4 *>(my_state + n16 * kORow + kTiles * (4 * g + r) + t) =
                         f32x4{o[nt][t][r], o[nt][t + 1][r], o[nt][t + 2][r], o[nt][t + 3][r]};
-        }
-        lds_barrier();
-        // 256 threads: 16 RT rows x D / 4 float4 columns
-        constexpr int kCols = D / 4;
+            lds_barrier();
+            // 256 threads: 16 rows x D / 4 float4 columns
+            constexpr int kCols = D / 4;
 #pragma unroll
-        for (int it = 0; it < kRows * kCols / 256; ++it) {
-            const int idx = tid + 256 * it;
-            const int rl = idx / kCols, c4 = idx % kCols;
-            const int row = u.r0 + rl;
-            if (row >= u.rows) continue;
-            float ms = s_m[0][rl], ltot = 0.f;
+            for (int it = 0; it < 16 * kCols / 256; ++it) {
+                const int idx = tid + 256 * it;
+                const int rl = idx / kCols, c4 = idx % kCols;
+                const int row = u.r0 + 16 * nt + rl;
+                if (row >= u.rows) continue;
+                float ms = s_m[0][rl], ltot = 0.f;
 #pragma unroll
-            for (int w = 1; w < kWaves; ++w) ms = fmaxf(ms, s_m[w][rl]);
-            f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+                for (int w = 1; w < kWaves; ++w) ms = fmaxf(ms, s_m[w][rl]);
+                f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int w = 0; w < kWaves; ++w) {
-                const float sc = __builtin_amdgcn_exp2f(s_m[w][rl] - ms);
-                ltot += sc * s_l[w][rl];
-                acc += sc * *reinterpret_cast<const f32x4 *>(smem + w * kSlab + 4 * (rl * kORow + 4 * c4));
-            }
-            if (u.ns == 1) {
-                const float inv = 1.0f / ltot;
-                const int64_t obase = ((u.qrow0 + row / G) * Hq + u.gkv * G + row % G) * (int64_t)D + 4 * c4;
-                if (out_dtype == ADASPEC_F32) {
-                    *reinterpret_cast<f32x4 *>(reinterpret_cast<float *>(out) + obase) = acc * inv;
-                } else {
-                    uint2 pk = make_uint2(Mma<T>::pack2(acc[0] * inv, acc[1] * inv), Mma<T>::pack2(acc[2] * inv, acc[3] * inv));
-                    *reinterpret_cast<uint2 *>(reinterpret_cast<uint16_t *>(out) + obase) = pk;
+                for (int w = 0; w < kWaves; ++w) {
+                    const float sc = __builtin_amdgcn_exp2f(s_m[w][rl] - ms);
+                    ltot += sc * s_l[w][rl];
+                    acc += sc * *reinterpret_cast<const f32x4 *>(smem + w * kSlab + 4 * (rl * kORow + 4 * c4));
                 }
-            } else {
-                const int64_t idx_row = ((int64_t)u.item * Hkv + u.gkv) * max_rows + row;
-                if (kDirect && attn_merge_fits(D, RT) && direct.flags) {
-                    store_state(part_o + idx_row * D + 4 * c4, acc);
-                    if (c4 == 0) store_ml(part_ml + idx_row * 2, ms, ltot);
+                if (u.ns == 1) {
+                    const float inv = 1.0f / ltot;
+                    const int64_t obase = ((u.qrow0 + row / G) * Hq + u.gkv * G + row % G) * (int64_t)D + 4 * c4;
+                    if (out_dtype == ADASPEC_F32) {
+                        *reinterpret_cast<f32x4 *>(reinterpret_cast<float *>(out) + obase) = acc * inv;
+                    } else {
+                        uint2 pk = make_uint2(Mma<T>::pack2(acc[0] * inv, acc[1] * inv), Mma<T>::pack2(acc[2] * inv, acc[3] * inv));
+                        *reinterpret_cast<uint2 *>(reinterpret_cast<uint16_t *>(out) + obase) = pk;
+                    }
                 } else {
-                    *reinterpret_cast<f32x4 *>(part_o + idx_row * D + 4 * c4) = acc;
-                    if (c4 == 0) {
-                        part_ml[idx_row * 2] = ms;
-                        part_ml[idx_row * 2 + 1] = ltot;
+                    const int64_t idx_row = ((int64_t)u.item * Hkv + u.gkv) * max_rows + row;
+                    if (kDirect && attn_merge_fits(D, RT) && direct.flags) {
+                        store_state(part_o + idx_row * D + 4 * c4, acc);
+                        if (c4 == 0) store_ml(part_ml + idx_row * 2, ms, ltot);
+                    } else {
+                        *reinterpret_cast<f32x4 *>(part_o + idx_row * D + 4 * c4) = acc;
+                        if (c4 == 0) {
+                            part_ml[idx_row * 2] = ms;
+                            part_ml[idx_row * 2 + 1] = ltot;
+                        }
                     }
                 }
             }
