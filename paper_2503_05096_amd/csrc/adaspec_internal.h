@@ -16,6 +16,7 @@ namespace adaspec {
 // context lengths live there.
 struct AttnPlan {
     int   split_tokens;     // S: maximum tokens per split
+    int   split_most;       // S where the plan kernel keeps it; else it makes splits of up to this many tokens for a heavy batch
     int   block_tokens;     // split lengths are rounded up to a multiple of this
     int   max_items;        // host-side bound on the number of work items
     int   max_rows;         // (max_spec_len + 1) * G

@@ -105,6 +105,7 @@ constexpr int kDirectMaxUnits = 256, kDirectFewPairs = 128, kDirectMaxUnitsFew =
 constexpr int kDirectShortCtx = 512, kDirectLongestShort = 1024, kDirectShortBatch = 1024;
 constexpr int kDirectF32Tokens = 262144, kDirectRowsTokens = 262144, kDirectRingTokens = 1048576;   // possible tokens of all units
 constexpr int kWavesPerUnit = 4;
+constexpr int kE4m3MostSplit = 8192;
 
 AttnKind attn_kind(const adaspec_attn_dims &d)
 {
@@ -173,6 +174,17 @@ AttnPlan make_attn_plan(const adaspec_attn_dims &d, AttnKind kind, bool tree)
         p.block_tokens = 64;
         p.split_tokens = 256;
     }
+    p.split_most = p.split_tokens;
+    if (kind == AttnKind::kMfmaE4m3) {
+        // A unit of so many tokens is half the bytes that it is in 16 bits, and the states of its parts, in fp32, are not: longer
+        // splits.  How long follows from the lengths, which the plan kernel sees: tokens times kv heads over two units per compute
+        // unit, as the next power of two.  MI355X, us, 32/8 heads of 128, splits of 1024 / 2048 / 4096 / 8192 / 16384 (that figure):
+        // 8 requests of 5000-10000 34.5 / 41.4 / 52.2 / 90.0 / 92.9 (937), 32 of 500-6000 54.8 / 49.2 / 53.4 / 63.2 / 63.2 (1624), 64 of
+        // 500-4000 76.8 / 67.1 / 56.5 / 56.8 (2249), 32 of 4000-20000 186 / 168 / 159 / 138 / 197 (6000), 64 of 8192-32768 600 / 550 /
+        // 496 / 467 / 488 (20480).  Longer than 8192 gains nothing.
+        if (pairs >= 512) p.split_tokens = 2 * p.split_tokens;
+        p.split_most = kE4m3MostSplit;
+    }
     const int64_t max_ctx = (int64_t)d.max_pages_per_req * d.page_size;
     p.direct = false;
     const int n_groups = attn_row_groups(p.max_rows);
@@ -207,6 +219,17 @@ AttnPlan make_attn_plan(const adaspec_attn_dims &d, AttnKind kind, bool tree)
                 p.split_tokens = s;
             }
     }
+    // Caches of 8 bits, few (request, kv head) pairs: as many parts of equal length as make two units per compute unit, one for a single
+    // request, whatever the lengths are (parts of two blocks per wavefront at least).  MI355X, us, 32/8 heads of 128, metadata first / 256
+    // units / 512 / 768: 1 request of 60000 36.2 / 27.9 / 30.1 / 34.6, 4 of 10000-20000 35.7 / 32.0 / 30.9 / 35.7, 16 of 3000-8000
+    // 46.5 / 47.0 / 42.6 / 48.8, 16/2 heads, 16 of 1000-8000 37.9 / 28.0 / 26.4 / 30.7, 64/8 heads, 4 of 6000-20000 55.2 / 46.4 / 37.5 /
+    // 41.8; with more pairs lengths differ too much for it: 32 of 4000-20000 140 / 201 / 170 / 174.
+    int64_t equal_parts = 0;
+    if (kind == AttnKind::kMfmaE4m3 && !tree && !p.direct && d.batch <= kDirectMaxBatch && pairs * n_groups <= kDirectFewPairs) {
+        p.direct = true;
+        p.split_tokens = 2 * kWavesPerUnit * p.block_tokens;
+        equal_parts = (d.batch == 1 ? kDirectMaxUnits : kDirectMaxUnitsFew) / (pairs * n_groups);
+    }
     if (scheduled && !tree && !p.direct && max_ctx <= p.split_tokens && max_ctx <= kDirectLongestShort && d.batch <= kDirectShortBatch) {
         // Short contexts: every request is one unit per kv head (no combine), all of them about equally short.  Measured
         // with and without (MI355X, 32/8 heads of 128, bf16): 256 requests of 100-500 tokens 62.6 / 65.5 us, 126 of 119-185
@@ -219,7 +242,8 @@ AttnPlan make_attn_plan(const adaspec_attn_dims &d, AttnKind kind, bool tree)
         const int64_t deep = kind == AttnKind::kMfmaF32 ? kDirectF32Tokens : !many_rows ? 0 : row_split() ? kDirectRowsTokens : kDirectRingTokens;
         p.direct = deep ? units * max_ctx <= deep : units <= (max_ctx <= kDirectShortCtx ? 8192 : 512);
     }
-    const int64_t per_req = (max_ctx + p.split_tokens - 1) / p.split_tokens;
+    int64_t per_req = (max_ctx + p.split_tokens - 1) / p.split_tokens;
+    if (equal_parts > 0 && equal_parts < per_req) per_req = equal_parts;
     p.per_req = (int)per_req;
     p.row_split = row_split();
     // Splits merged in the kernel, not by a second one: up to 4 possible splits, of one row tile of 128 channels or two of 64.

@@ -194,6 +194,7 @@ __global__ __launch_bounds__(256, (RT == 1 ? 3 : 2)) void attn_e4m3_kernel(
             for (int t = 0; t < kTiles; ++t) o[nt][t] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
 
+        const int tiles = min((u.rows - u.r0 + 15) / 16, RT);       // row tiles of the unit that have rows (others cost nothing)
         // One block.  kInner: every row sees all of it, and another one follows, whose K and V are requested as soon as their
         // registers are free (without a branch around the loads, so that the compiler's waits count exactly).
         auto block = [&](int bi, auto inner_tag) {
@@ -219,6 +220,7 @@ __global__ __launch_bounds__(256, (RT == 1 ? 3 : 2)) void attn_e4m3_kernel(
                 if constexpr (RT > 2) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                 for (int nt = 0; nt < RT; ++nt) {
+                    if (nt > 0 && nt >= tiles) break;
                     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                     for (int s = 0; s < kSteps; ++s) acc = Mma<T>::run(kop[s], q_lds[(nt * kSteps + s) * 64 + lane], acc);
@@ -235,6 +237,7 @@ __global__ __launch_bounds__(256, (RT == 1 ? 3 : 2)) void attn_e4m3_kernel(
             uint32_t seen[RT];                                      // masked: bit e = the row sees token e
 #pragma unroll
             for (int nt = 0; nt < RT; ++nt) {
+                if (nt > 0 && nt >= tiles) break;
                 if (masked) {
                     seen[nt] = 0;
                     const unsigned long long am = kTree ? s_anc[16 * nt + n16] : 0ull;
@@ -303,6 +306,7 @@ __global__ __launch_bounds__(256, (RT == 1 ? 3 : 2)) void attn_e4m3_kernel(
                             const uint4 a = make_uint4(bad[0] | bad[1] << 16, bad[2] | bad[3] << 16, bad[4] | bad[5] << 16, bad[6] | bad[7] << 16);
 #pragma unroll
                             for (int nt = 0; nt < RT; ++nt) {
+                                if (nt > 0 && nt >= tiles) break;
                                 uint32_t see[8];
 #pragma unroll
                                 for (int e = 0; e < 8; ++e) see[e] = (seen[nt] >> (8 * hf + e)) & 1 ? 0x3f80u : 0u;
@@ -331,7 +335,8 @@ __global__ __launch_bounds__(256, (RT == 1 ? 3 : 2)) void attn_e4m3_kernel(
             for (int hf = 0; hf < kHalves; ++hf) {
                 uint4 hi[RT], lo[RT];
 #pragma unroll
-                for (int nt = 0; nt < RT; ++nt)
+                for (int nt = 0; nt < RT; ++nt) {
+                    if (nt > 0 && nt >= tiles) break;
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         const float x = p[nt][8 * hf + 2 * j], y = p[nt][8 * hf + 2 * j + 1];
@@ -339,6 +344,7 @@ __global__ __launch_bounds__(256, (RT == 1 ? 3 : 2)) void attn_e4m3_kernel(
                         (&hi[nt].x)[j] = w;
                         (&lo[nt].x)[j] = Mma<BF16>::pack2(x - __uint_as_float(w << 16), y - __uint_as_float(w & 0xffff0000u));
                     }
+                }
 #pragma unroll
                 for (int w = 0; w < kWords; ++w)
 #pragma unroll
@@ -357,6 +363,7 @@ __global__ __launch_bounds__(256, (RT == 1 ? 3 : 2)) void attn_e4m3_kernel(
                         const int t = 4 * w + 2 * up;
 #pragma unroll
                         for (int nt = 0; nt < RT; ++nt) {
+                            if (nt > 0 && nt >= tiles) break;
                             o[nt][t] = Mma<BF16>::run(even, hi[nt], o[nt][t]);
                             o[nt][t + 1] = Mma<BF16>::run(odd, hi[nt], o[nt][t + 1]);
                             o[nt][t] = Mma<BF16>::run(even, lo[nt], o[nt][t]);
@@ -386,6 +393,7 @@ __global__ __launch_bounds__(256, (RT == 1 ? 3 : 2)) void attn_e4m3_kernel(
         // ---- merge the four wavefronts' states through LDS (as in attn_mfma.hip), one row tile after the other ----------
 #pragma unroll
         for (int nt = 0; nt < RT; ++nt) {
+            if (nt > 0 && nt >= tiles) break;
             if (nt > 0) lds_barrier();                              // (the tile before has been read)
             lsum[nt] += __shfl_xor(lsum[nt], 16, kWave);
             lsum[nt] += __shfl_xor(lsum[nt], 32, kWave);

@@ -22,6 +22,16 @@ __host__ __device__ inline int log2_exact(int v)          // v is a power of two
 // a context length no split count of which overflows
 __device__ __forceinline__ int plan_ctx(int ctx_len) { return min(max(ctx_len, 1), 1 << 30); }
 
+// Splits as long as the batch is heavy (plan.split_most, for kernels that ask for it): the least power of two of tokens with which
+// the whole batch is about two units per compute unit; `heavy`: tokens of all requests times units per token.
+__device__ __forceinline__ int fitting_split_log2(int64_t heavy, int cus, int least_log2, int most_log2)
+{
+    const int64_t each = (heavy + 2 * cus - 1) / (2 * cus);
+    int l = least_log2;
+    while (l < most_log2 && ((int64_t)1 << l) < each) ++l;
+    return l;
+}
+
 // Tree calls (batches up to kFusedMaskMaxBatch): the plan kernels' workgroups 1.. build the ancestor masks beside the
 // plan, one wavefront per request.  They share nothing with workgroup 0: each wavefront adds up the rows of the requests
 // before its own.
@@ -70,7 +80,7 @@ __device__ __forceinline__ int order_of(int total, int W, int cus, int even_roun
 // requests, more than kSchedItems items) read their own global stores back, behind a full barrier.
 __global__ __launch_bounds__(kPlanThreads) void attn_plan_kernel(
     const int32_t *__restrict__ ctx_lens, const int32_t *__restrict__ spec_lens, int B, int total_q,
-    int max_spec_len, int split_log2, int block_log2, int max_items, int G, int32_t *__restrict__ header,
+    int max_spec_len, int split_log2, int most_log2, int block_log2, int max_items, int G, int32_t *__restrict__ header,
     int32_t *__restrict__ cu_q, int32_t *__restrict__ split_base, int32_t *__restrict__ item_req,
     int32_t *__restrict__ item_order, int32_t *__restrict__ unit_meta, int32_t *__restrict__ row_rec,
     int W, int Hkv, int n_row_groups, int rows_per_group, int32_t *__restrict__ sched, int cus, int even_rounds,
@@ -88,6 +98,18 @@ __global__ __launch_bounds__(kPlanThreads) void attn_plan_kernel(
     __shared__ uint8_t item_blocks[kSchedItems], item_groups[kSchedItems];   // per SORTED item: token blocks, row groups
     __shared__ int bins[kPlanThreads], wg_work[kPlanThreads], wave_tot[kPlanThreads / kWave];
     const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
+    if (most_log2 > split_log2) {
+        __shared__ int64_t tokens[kPlanThreads / kWave];
+        int64_t sum = 0;
+        for (int i = tid; i < B; i += kPlanThreads) sum += plan_ctx(ctx_lens[i]);
+        sum = last_lane(wave_scan(sum, (int64_t)0, [](int64_t a, int64_t b) { return a + b; }));
+        if (lane == 0) tokens[wv] = sum;
+        lds_barrier();
+        sum = 0;
+#pragma unroll
+        for (int w = 0; w < kPlanThreads / kWave; ++w) sum += tokens[w];
+        split_log2 = fitting_split_log2(sum * Hkv * n_row_groups, cus, split_log2, most_log2);
+    }
     const int split_tokens = 1 << split_log2, block_tokens = 1 << block_log2;
     const bool fast = W > 0;
     const bool items_on_chip = max_items <= kSchedItems && B <= 65535;  // host-side bounds: uniform
@@ -281,7 +303,7 @@ constexpr int kWorkBins = 1024;          // of the counting sort by accumulated 
 
 __global__ __launch_bounds__(kSmallThreads) void attn_plan_small_kernel(
     const int32_t *__restrict__ ctx_lens, const int32_t *__restrict__ spec_lens, int B, int total_q,
-    int max_spec_len, int split_log2, int block_log2, int max_items, int G, int32_t *__restrict__ header,
+    int max_spec_len, int split_log2, int most_log2, int block_log2, int max_items, int G, int32_t *__restrict__ header,
     int32_t *__restrict__ unit_meta, int32_t *__restrict__ row_rec, int W, int Hkv, int n_row_groups, int rows_per_group,
     int32_t *__restrict__ sched, int cus, int even_rounds, const int32_t *__restrict__ parents, unsigned long long *__restrict__ anc)
 {
@@ -296,13 +318,23 @@ __global__ __launch_bounds__(kSmallThreads) void attn_plan_small_kernel(
     __shared__ __attribute__((aligned(16))) int bins[kWorkBins], place[kWorkBins];
     __shared__ uint16_t item_size[kSchedItems];                 // per SORTED item: token blocks, row groups << 8
     const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, i = tid;
-    const int split_tokens = 1 << split_log2, block_tokens = 1 << block_log2;
     int n = 0, ns = 0, L = 1;
     if (i < B) {
         n = min(max(spec_lens[i], 0), max_spec_len) + 1;
         L = plan_ctx(ctx_lens[i]);
-        ns = (L + split_tokens - 1) >> split_log2;
     }
+    if (most_log2 > split_log2) {
+        __shared__ int64_t tokens[kPlanWaves];
+        const int64_t mine = last_lane(wave_scan((int64_t)(i < B ? L : 0), (int64_t)0, [](int64_t a, int64_t b) { return a + b; }));
+        if (lane == 0) tokens[wv] = mine;
+        lds_barrier();
+        int64_t sum = 0;
+#pragma unroll
+        for (int w = 0; w < kPlanWaves; ++w) sum += tokens[w];
+        split_log2 = fitting_split_log2(sum * Hkv * n_row_groups, cus, split_log2, most_log2);
+    }
+    const int split_tokens = 1 << split_log2, block_tokens = 1 << block_log2;
+    if (i < B) ns = (L + split_tokens - 1) >> split_log2;
     if (tid < kWave) { hist[tid] = 0; taken[tid] = 0; }
     *reinterpret_cast<int4 *>(bins + 4 * tid) = make_int4(0, 0, 0, 0);
 
@@ -426,7 +458,7 @@ hipError_t launch_attn_plan(const AttnArgs &a)
     if (a.sched_w > 0 && a.dims.batch <= kSmallThreads && p.max_items <= kSchedItems && a.sched_cus <= kSmallThreads) {
         hipLaunchKernelGGL(attn_plan_small_kernel, workgroups(kSmallThreads), dim3(kSmallThreads), 0, a.stream, a.ctx_lens,
                            a.spec_lens, a.dims.batch, a.dims.total_q, a.dims.max_spec_len,
-                           log2_exact(p.split_tokens), log2_exact(p.block_tokens), p.max_items,
+                           log2_exact(p.split_tokens), log2_exact(p.split_most), log2_exact(p.block_tokens), p.max_items,
                            a.dims.n_q_heads / a.dims.n_kv_heads, (int32_t *)(a.ws + p.off_header),
                            (int32_t *)(a.ws + p.off_unit_meta), (int32_t *)(a.ws + p.off_row_rec), a.sched_w,
                            a.dims.n_kv_heads, a.n_row_groups, a.rows_per_group, (int32_t *)(a.ws + p.off_sched),
@@ -435,7 +467,7 @@ hipError_t launch_attn_plan(const AttnArgs &a)
     }
     hipLaunchKernelGGL(attn_plan_kernel, workgroups(kPlanThreads), dim3(kPlanThreads), 0, a.stream, a.ctx_lens,
                        a.spec_lens, a.dims.batch, a.dims.total_q, a.dims.max_spec_len,
-                       log2_exact(p.split_tokens), log2_exact(p.block_tokens), p.max_items,
+                       log2_exact(p.split_tokens), log2_exact(p.split_most), log2_exact(p.block_tokens), p.max_items,
                        a.dims.n_q_heads / a.dims.n_kv_heads, (int32_t *)(a.ws + p.off_header),
                        (int32_t *)(a.ws + p.off_cu_q), (int32_t *)(a.ws + p.off_split_base),
                        (int32_t *)(a.ws + p.off_item_req), (int32_t *)(a.ws + p.off_item_order),
