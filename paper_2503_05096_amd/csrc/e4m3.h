@@ -34,17 +34,22 @@ __device__ __forceinline__ uint32_t float2_to_e4m3(float a, float b)
     return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(e4m3_input(a), e4m3_input(b), 0, false) & 0xffffu;
 }
 
-// eight elements times `ratio` (at most 1: nothing overflows), rounded again; aligned to 8 bytes
+// elements times `ratio` (at most 1: nothing overflows), rounded again
+__device__ __forceinline__ uint32_t e4m3_rescale4(uint32_t w, float ratio)
+{
+    float f[4];
+    e4m3_to_float2<false>(w, f[0], f[1]);
+    e4m3_to_float2<true>(w, f[2], f[3]);
+    return float4_to_e4m3(f[0] * ratio, f[1] * ratio, f[2] * ratio, f[3] * ratio);
+}
 __device__ __forceinline__ void e4m3_rescale8(const uint8_t *from, uint8_t *to, float ratio)
 {
     const uint2 w = *reinterpret_cast<const uint2 *>(from);
-    float f[8];
-    e4m3_to_float2<false>(w.x, f[0], f[1]);
-    e4m3_to_float2<true>(w.x, f[2], f[3]);
-    e4m3_to_float2<false>(w.y, f[4], f[5]);
-    e4m3_to_float2<true>(w.y, f[6], f[7]);
-    *reinterpret_cast<uint2 *>(to) = make_uint2(float4_to_e4m3(f[0] * ratio, f[1] * ratio, f[2] * ratio, f[3] * ratio),
-                                                float4_to_e4m3(f[4] * ratio, f[5] * ratio, f[6] * ratio, f[7] * ratio));
+    *reinterpret_cast<uint2 *>(to) = make_uint2(e4m3_rescale4(w.x, ratio), e4m3_rescale4(w.y, ratio));
+}
+__device__ __forceinline__ uint4 e4m3_rescale16(uint4 w, float ratio)
+{
+    return make_uint4(e4m3_rescale4(w.x, ratio), e4m3_rescale4(w.y, ratio), e4m3_rescale4(w.z, ratio), e4m3_rescale4(w.w, ratio));
 }
 
 // log2 of the least power of two s with most <= (448 s)^2: 448^2 = 1.53125 * 2^17.  In squares of 64 bits, so that it does not

@@ -8,9 +8,13 @@
 //
 // A workgroup takes up to 16 consecutive rows of a request (for a cache of 8 bits: those of one page, whose scale they
 // decide together) and some of the kv heads with their query heads; cosines and sines of its rows are worked out once.
+//
+// Small calls are bound by latency: two memory round trips (lengths, rows), three into a cache of 8 bits (the page's scale), with
+// the angles worked out while the rows travel.  Large ones by HBM.
 #include <type_traits>
 
 #include "adaspec_internal.h"
+#include "attn_mfma_common.h"
 #include "device_utils.h"
 #include "e4m3.h"
 
@@ -31,45 +35,86 @@ struct RopeArgs {
     int heads;                  // heads (kv heads with their query heads; query heads where nothing is appended) per workgroup
 };
 
-// W consecutive elements
-template <class T, int W>
-__device__ __forceinline__ void load_unit(const void *base, int64_t at, float (&x)[W])
+// x / n for 0 <= x < 2^21 and 1 <= n, by the rounded reciprocal: (x + 1/2) / n is at least 1 / (2 n) away from an integer, and off by
+// less than x / n * 2^-22
+struct Divider {
+    int n;
+    float inv;
+    __device__ __forceinline__ explicit Divider(int n_) : n(n_), inv(1.0f / (float)n_) {}
+    __device__ __forceinline__ int operator()(int x, int &rest) const
+    {
+        const int q = (int)(((float)x + 0.5f) * inv);
+        rest = x - q * n;
+        return q;
+    }
+};
+
+// kBytes at an address aligned to them (to 16 bytes, if there are more), in words
+template <int kBytes> struct Words { uint32_t w[kBytes / 4]; };
+template <int kBytes>
+__device__ __forceinline__ Words<kBytes> load_words(const void *at)
 {
-    using S = typename T::storage;
-    const S *p = static_cast<const S *>(base) + at;
-    if constexpr (W == 8) {
-        S raw[8];
-        if constexpr (sizeof(S) == 2) {
-            *reinterpret_cast<uint4 *>(raw) = *reinterpret_cast<const uint4 *>(p);
-        } else {
-            reinterpret_cast<uint4 *>(raw)[0] = reinterpret_cast<const uint4 *>(p)[0];
-            reinterpret_cast<uint4 *>(raw)[1] = reinterpret_cast<const uint4 *>(p)[1];
-        }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = load_as_float<T>(raw, e);
+    Words<kBytes> r;
+    if constexpr (kBytes == 4) {
+        r.w[0] = *static_cast<const uint32_t *>(at);
+    } else if constexpr (kBytes == 8) {
+        const uint2 v = *static_cast<const uint2 *>(at);
+        r.w[0] = v.x, r.w[1] = v.y;
     } else {
 #pragma unroll
-        for (int e = 0; e < W; ++e) x[e] = load_as_float<T>(p, e);
+        for (int e = 0; e < kBytes / 16; ++e) {
+            const uint4 v = static_cast<const uint4 *>(at)[e];
+            r.w[4 * e] = v.x, r.w[4 * e + 1] = v.y, r.w[4 * e + 2] = v.z, r.w[4 * e + 3] = v.w;
+        }
+    }
+    return r;
+}
+template <int kBytes>
+__device__ __forceinline__ void store_words(void *at, const Words<kBytes> &r)
+{
+    if constexpr (kBytes == 4) {
+        *static_cast<uint32_t *>(at) = r.w[0];
+    } else if constexpr (kBytes == 8) {
+        *static_cast<uint2 *>(at) = make_uint2(r.w[0], r.w[1]);
+    } else {
+#pragma unroll
+        for (int e = 0; e < kBytes / 16; ++e) static_cast<uint4 *>(at)[e] = make_uint4(r.w[4 * e], r.w[4 * e + 1], r.w[4 * e + 2], r.w[4 * e + 3]);
     }
 }
+// W consecutive elements as they are stored, in words (an array of 16-bit elements would take a register each), or a single one
+template <class T, int W> struct Raw {
+    static constexpr int kBytes = W * sizeof(typename T::storage);
+    std::conditional_t<kBytes >= 4, Words<kBytes < 4 ? 4 : kBytes>, uint16_t> x;
+    __device__ __forceinline__ void load(const void *base, int64_t at)
+    {
+        const typename T::storage *p = static_cast<const typename T::storage *>(base) + at;
+        if constexpr (kBytes >= 4) x = load_words<kBytes>(p);
+        else x = *p;
+    }
+    __device__ __forceinline__ float operator[](int e) const
+    {
+        if constexpr (kBytes < 4) return load_as_float<T>(&x, 0);
+        else if constexpr (T::id == ADASPEC_F32) return __uint_as_float(x.w[e]);
+        else if constexpr (T::id == ADASPEC_BF16) return __uint_as_float(e & 1 ? x.w[e / 2] & 0xffff0000u : x.w[e / 2] << 16);
+        else return f16_bits_to_float((uint16_t)(x.w[e / 2] >> (16 * (e & 1))));
+    }
+};
 template <class T, int W>
 __device__ __forceinline__ void store_unit(void *base, int64_t at, const float (&x)[W])
 {
-    using S = typename T::storage;
-    S *p = static_cast<S *>(base) + at;
-    if constexpr (W == 8) {
-        S raw[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) store_out(raw, e, x[e], T::id);
-        if constexpr (sizeof(S) == 2) {
-            *reinterpret_cast<uint4 *>(p) = *reinterpret_cast<const uint4 *>(raw);
-        } else {
-            reinterpret_cast<uint4 *>(p)[0] = reinterpret_cast<const uint4 *>(raw)[0];
-            reinterpret_cast<uint4 *>(p)[1] = reinterpret_cast<const uint4 *>(raw)[1];
-        }
+    typename T::storage *p = static_cast<typename T::storage *>(base) + at;
+    if constexpr (W == 1) {
+        store_out(p, 0, x[0], T::id);
     } else {
+        Words<W * sizeof(*p)> r;
+        if constexpr (T::id == ADASPEC_F32) {
 #pragma unroll
-        for (int e = 0; e < W; ++e) store_out(p, e, x[e], T::id);
+            for (int e = 0; e < W; ++e) r.w[e] = __float_as_uint(x[e]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < W / 2; ++e) r.w[e] = Mma<T>::pack2(x[2 * e], x[2 * e + 1]);
+        }
+        store_words(p, r);
     }
 }
 template <int W>
@@ -79,10 +124,10 @@ __device__ __forceinline__ void store_unit8(void *base, int64_t at, const float 
     if constexpr (W == 8) {
         *reinterpret_cast<uint2 *>(p) = make_uint2(float4_to_e4m3(x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv),
                                                    float4_to_e4m3(x[4] * inv, x[5] * inv, x[6] * inv, x[7] * inv));
+    } else if constexpr (W == 4) {
+        *reinterpret_cast<uint32_t *>(p) = float4_to_e4m3(x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv);
     } else if constexpr (W == 2) {
-        const uint32_t w = float2_to_e4m3(x[0] * inv, x[1] * inv);
-        p[0] = (uint8_t)w;
-        p[1] = (uint8_t)(w >> 8);
+        *reinterpret_cast<uint16_t *>(p) = (uint16_t)float2_to_e4m3(x[0] * inv, x[1] * inv);
     } else {
         *p = (uint8_t)float2_to_e4m3(x[0] * inv, 0.f);
     }
@@ -92,206 +137,311 @@ __device__ __forceinline__ void store_unit8(void *base, int64_t at, const float 
 // entries; behind them, W at a time, those that are not turned.
 template <class T, int W, bool kInter>
 struct Units {
-    static __device__ __forceinline__ int turned(int rot) { return kInter ? rot / W : rot / (2 * W); }
-    static __device__ __forceinline__ int count(int rot, int d) { return turned(rot) + (d - rot) / W; }
+    struct Item { Raw<T, W> a, b; };    // (b: the partners)
+    int rot, turned, count;
+    __device__ __forceinline__ Units(int rot_, int d) : rot(rot_), turned(kInter ? rot / W : rot / (2 * W)), count(turned + (d - rot) / W) {}
 
-    // unit u of the row that starts at `src`, turned (cs: the row's cosines and sines): put(place in the row, values)
+    __device__ __forceinline__ int place(int u) const { return u < turned ? u * W : rot + (u - turned) * W; }
+    // unit u of the row at `src`
+    __device__ __forceinline__ void fetch(Item &it, const void *base, int64_t src, int u) const
+    {
+        it.a.load(base, src + place(u));
+        if constexpr (!kInter)
+            if (u < turned) it.b.load(base, src + u * W + rot / 2);
+    }
+    // turned (cs: the row's cosines and sines): put(place in the row, values)
     template <class Put>
-    static __device__ __forceinline__ void turn(const void *base, int64_t src, int u, int rot, const float2 *cs, Put &&put)
+    __device__ __forceinline__ void turn(const Item &it, int u, const float2 *cs, Put &&put) const
     {
-        const int n = turned(rot);
         float a[W];
-        if (u >= n) {
-            const int c = rot + (u - n) * W;
-            load_unit<T, W>(base, src + c, a);
-            put(c, a);
-        } else if constexpr (kInter) {
-            load_unit<T, W>(base, src + u * W, a);
 #pragma unroll
-            for (int e = 0; e < W; e += 2) {
-                const float2 r = cs[(u * W + e) / 2];
-                const float x = a[e], y = a[e + 1];
-                a[e] = x * r.x - y * r.y;
-                a[e + 1] = y * r.x + x * r.y;
-            }
-            put(u * W, a);
-        } else {
-            float b[W];
-            load_unit<T, W>(base, src + u * W, a);
-            load_unit<T, W>(base, src + u * W + rot / 2, b);
+        for (int e = 0; e < W; ++e) a[e] = it.a[e];
+        if (u < turned) {
+            if constexpr (kInter) {
 #pragma unroll
-            for (int e = 0; e < W; ++e) {
-                const float2 r = cs[u * W + e];
-                const float x = a[e], y = b[e];
-                a[e] = x * r.x - y * r.y;
-                b[e] = y * r.x + x * r.y;
+                for (int e = 0; e + 1 < W; e += 2) {
+                    const float2 r = cs[(u * W + e) / 2];
+                    const float x = a[e], y = a[e + 1];
+                    a[e] = x * r.x - y * r.y;
+                    a[e + 1] = y * r.x + x * r.y;
+                }
+            } else {
+                float b[W];
+#pragma unroll
+                for (int e = 0; e < W; ++e) {
+                    const float2 r = cs[u * W + e];
+                    const float x = a[e], y = it.b[e];
+                    a[e] = x * r.x - y * r.y;
+                    b[e] = y * r.x + x * r.y;
+                }
+                put(u * W + rot / 2, b);
             }
-            put(u * W, a);
-            put(u * W + rot / 2, b);
+        }
+        put(place(u), a);
+    }
+    // the largest squared length of the unit's pairs and of its other entries, in F; what is not a number does not count
+    template <class F>
+    __device__ __forceinline__ void longest(const Item &it, int u, F &pairs, F &rest) const
+    {
+#pragma unroll
+        for (int e = 0; e < W; ++e) {
+            const F x = it.a[e];
+            if (u >= turned) {
+                rest = larger(rest, x * x);
+            } else if constexpr (!kInter) {
+                const F y = it.b[e];
+                pairs = larger(pairs, x * x + y * y);
+            } else if (e % 2 == 0 && e + 1 < W) {
+                const F y = it.a[e + 1];
+                pairs = larger(pairs, x * x + y * y);
+            }
         }
     }
-    // the largest squared length of the unit's pairs, in 64 bits; pairs with something that is not finite do not count
-    static __device__ __forceinline__ void longest(const void *base, int64_t src, int u, int rot, double &pairs, double &rest)
-    {
-        const auto count = [](double s, double &most) { if (s < 1e200) most = fmax(most, s); };
-        const int n = turned(rot);
-        float a[W];
-        if (u >= n) {
-            load_unit<T, W>(base, src + rot + (u - n) * W, a);
-#pragma unroll
-            for (int e = 0; e < W; ++e) count((double)a[e] * a[e], rest);
-        } else if constexpr (kInter) {
-            load_unit<T, W>(base, src + u * W, a);
-#pragma unroll
-            for (int e = 0; e < W; e += 2) count((double)a[e] * a[e] + (double)a[e + 1] * a[e + 1], pairs);
-        } else {
-            float b[W];
-            load_unit<T, W>(base, src + u * W, a);
-            load_unit<T, W>(base, src + u * W + rot / 2, b);
-#pragma unroll
-            for (int e = 0; e < W; ++e) count((double)a[e] * a[e] + (double)b[e] * b[e], pairs);
-        }
-    }
+    static __device__ __forceinline__ float larger(float most, float s) { return fmaxf(most, s); }
+    // (in 64 bits squares of floats are finite, infinities do not count)
+    static __device__ __forceinline__ double larger(double most, double s) { return fmax(most, s < 1e200 ? s : 0.0); }
 };
 
 // The new tokens of one (page, kv head) of K or of V, by one wavefront: rows src, src + stride, ... go to slots [lo, hi).
+// begin() requests what it can (the rows stay in registers up to kHeld units per lane, more are read twice); finish() finds the
+// scale, rounds the page's earlier tokens to it where it has grown, and writes the new ones.
 template <class T, int W, bool kInter>
-__device__ __forceinline__ void append_page8(const void *x, int64_t src, int64_t stride, int d, int rot, double gain2, const float2 *cs,
-                                             int cs_stride, uint8_t *block, float *scale_at, int lo, int hi, int lane)
-{
+struct PageAppend {
     using U = Units<T, W, kInter>;
-    const int units = U::count(rot, d), n = hi - lo;
-    double pairs = 0.0, rest = 0.0;
-    for (int idx = lane; idx < n * units; idx += kWave) U::longest(x, src + (idx / units) * stride, idx % units, rot, pairs, rest);
-    const double most = last_lane(wave_scan(fmax(pairs * gain2, rest), 0.0, [](double a, double b) { return fmax(a, b); }));
-    float scale = power_of_two(scale_log2_for(most));
-    if (lo > 0) {                                       // the page keeps earlier tokens: their scale never falls
-        const float old = *scale_at;
-        scale = fmaxf(old, scale);
-        if (scale != old) {
-            const float ratio = old / scale;
-            for (int idx = lane; idx < lo * d / 8; idx += kWave) e4m3_rescale8(block + 8 * idx, block + 8 * idx, ratio);
+    static constexpr int kHeld = kInter ? 4 : 2;        // 16 rows of 128 channels
+    U units;
+    const void *x;
+    int64_t src, stride;
+    uint8_t *block;
+    float *scale_at;
+    int d, lo, work, lane;
+    bool held_all;
+    float old;
+    typename U::Item held[kHeld];
+
+    __device__ __forceinline__ PageAppend(const U &units_) : units(units_) {}
+    __device__ __forceinline__ void begin(const void *x_, int64_t src_, int64_t stride_, int d_, uint8_t *block_, float *scale_at_, int lo_, int n, int lane_)
+    {
+        x = x_, src = src_, stride = stride_, d = d_, block = block_, scale_at = scale_at_, lo = lo_, lane = lane_;
+        work = n * units.count;
+        held_all = work <= kHeld * kWave;
+        old = lo > 0 ? *scale_at : 0.f;
+        if (held_all) {
+#pragma unroll
+            for (int e = 0; e < kHeld; ++e)
+                if (lane + e * kWave < work) fetch(held[e], lane + e * kWave);
         }
     }
-    const float inv = 1.0f / scale;
-    for (int idx = lane; idx < n * units; idx += kWave) {
-        const int j = idx / units;
-        U::turn(x, src + j * stride, idx % units, rot, cs + j * cs_stride, [&](int c, const float (&y)[W]) {
-            store_unit8<W>(block, (int64_t)(lo + j) * d + c, y, inv);
-        });
+    __device__ __forceinline__ int of(int idx, int &u) const { return Divider(units.count)(idx, u); }
+    __device__ __forceinline__ void fetch(typename U::Item &it, int idx) const
+    {
+        int u;
+        const int j = of(idx, u);
+        units.fetch(it, x, src + j * stride, u);
     }
-    if (lane == 0) *scale_at = scale;
-}
+    // f(unit of the page in registers, its number)
+    template <class Fn>
+    __device__ __forceinline__ void each(Fn &&f)
+    {
+        if (held_all) {
+#pragma unroll
+            for (int e = 0; e < kHeld; ++e)
+                if (lane + e * kWave < work) f(held[e], lane + e * kWave);
+        } else {
+            for (int idx = lane; idx < work; idx += kWave) {
+                fetch(held[0], idx);
+                f(held[0], idx);
+            }
+        }
+    }
+    // log2 of the scale that the new tokens need.  Squares and their sums in 32 bits are off by a few units in the last place; where
+    // that leaves the scale in doubt (near a border, 1.53125 * 2^odd, or where they overflow or underflow) it is worked out in 64,
+    // where the products are exact, so that it never depends on a rounding.
+    __device__ __forceinline__ int scale_log2(float gain)
+    {
+        float pairs = 0.f, rest = 0.f;
+        each([&](const typename U::Item &it, int idx) {
+            int u;
+            of(idx, u);
+            units.longest(it, u, pairs, rest);
+        });
+        const float most = wave_max(fmaxf(pairs * (gain * gain), rest));
+        const uint32_t fraction = (__float_as_uint(most) & 0x7fffffu) - 0x440000u;              // of 1.53125
+        if (most > 1e-30f && most < 1e37f && (fraction + 32u) > 64u) return scale_log2_for(most);
+        double pairs64 = 0.0, rest64 = 0.0;
+        each([&](const typename U::Item &it, int idx) {
+            int u;
+            of(idx, u);
+            units.longest(it, u, pairs64, rest64);
+        });
+        const double gain64 = gain, most64 = fmax(pairs64 * (gain64 * gain64), rest64);
+        return scale_log2_for(last_lane(wave_scan(most64, 0.0, [](double a, double b) { return fmax(a, b); })));
+    }
+    __device__ __forceinline__ void finish(float gain, const float2 *cs, int cs_stride)
+    {
+        float scale = power_of_two(scale_log2(gain));
+        if (lo > 0) {                                   // the page keeps earlier tokens: their scale never falls
+            scale = fmaxf(old, scale);
+            if (scale != old) {
+                const float ratio = old / scale;
+                for (int c = lane; c < lo * d / 8; c += kWave) e4m3_rescale8(block + 8 * c, block + 8 * c, ratio);
+            }
+        }
+        const float inv = 1.0f / scale;
+        each([&](const typename U::Item &it, int idx) {
+            int u;
+            const int j = of(idx, u);
+            units.turn(it, u, cs + j * cs_stride, [&](int c, const float (&y)[W]) { store_unit8<W>(block, (int64_t)(lo + j) * d + c, y, inv); });
+        });
+        if (lane == 0) *scale_at = scale;
+    }
+};
 
 template <class T, int W, bool kInter, bool k8>
 __global__ __launch_bounds__(kRopeThreads) void rope_append_kernel(RopeArgs a)
 {
-    __shared__ float2 cs[kRopeRows * kRopeMaxHalf];
+    extern __shared__ float2 cs[];                      // [rows][pairs]
+    __shared__ float freq[kRopeMaxHalf];
     __shared__ int wsum[kRopeThreads / kWave];
     __shared__ int depth[kWave];
     __shared__ int pages[2];
     using U = Units<T, W, kInter>;
     const adaspec_rope_dims &D = a.d;
-    const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
+    const int tid = threadIdx.x, lane = tid & 63, wv = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int i = blockIdx.x / a.chunks, chunk = blockIdx.x % a.chunks;
-    const int d = D.head_dim, rot = D.rot_dim, half = rot / 2, Hkv = D.n_kv_heads;
+    const int d = D.head_dim, half = D.rot_dim / 2, Hkv = D.n_kv_heads;
 
-    int part = 0;
-    for (int j = tid; j < i; j += kRopeThreads) part += min(max(a.spec_lens[j], 0), D.max_spec_len) + 1;
-    part = wave_sum(part);
-    if (lane == 0) wsum[wv] = part;
     const int n = min(max(a.spec_lens[i], 0), D.max_spec_len) + 1;
     const int L = a.ctx_lens[i], first = L - n;
     // tokens [t0, t1) of the request
     const int t0 = k8 ? max(first, (first / kPageTokens + chunk) * kPageTokens) : first + chunk * kRopeRows;
     const int t1 = k8 ? min(L, (first / kPageTokens + chunk + 1) * kPageTokens) : min(L, t0 + kRopeRows);
+    int part = 0;
+    for (int j = tid; j < i; j += kRopeThreads) part += min(max(a.spec_lens[j], 0), D.max_spec_len) + 1;
+    if (tid < half) freq[tid] = a.inv_freq[tid];
     if (first < 0 || t0 >= t1) return;
-    const int nt = t1 - t0, j0 = t0 - first;
     if (a.k && tid < 2) {
         const int at = t0 / kPageTokens + tid;
         int page = -1;
         if (at <= (t1 - 1) / kPageTokens && at < D.max_pages_per_req) page = a.block_table[(int64_t)i * D.max_pages_per_req + at];
         pages[tid] = page >= 0 && page < D.num_pages ? page : -1;
     }
-    __syncthreads();
+    part = wave_sum(part);
+    if (lane == 0) wsum[wv] = part;
+    lds_barrier();
     int row0 = 0;
 #pragma unroll
     for (int w = 0; w < kRopeThreads / kWave; ++w) row0 += wsum[w];
     if (row0 + n > D.total_q) return;                   // inconsistent metadata: touch nothing
-    if (a.parents && half > 0) {
-        // depths by doubling: every node looks at the node that its jumps so far have led to (the root at itself)
-        if (wv == 0) {
-            int up = lane > 0 && lane < n ? min(max(a.parents[row0 + lane], 0), lane - 1) : 0, dep = lane > 0 && lane < n ? 1 : 0;
-#pragma unroll
-            for (int s = 0; s < 6; ++s) {
-                dep += __shfl(dep, up, kWave);
-                up = __shfl(up, up, kWave);
-            }
-            depth[lane] = dep;
-        }
-        __syncthreads();
-    }
-    for (int idx = tid; idx < nt * half; idx += kRopeThreads) {
-        const int j = idx / half, f = idx - j * half;
-        const int pos = first + (a.parents ? depth[j0 + j] : j0 + j);
-        const double turns = (double)pos * (double)a.inv_freq[f] * 0.15915494309189533577;      // 1 / (2 pi)
-        const float r = (float)(2.0 * (turns - rint(turns)));
-        float s, c;
-        sincospif(r, &s, &c);
-        cs[j * half + f] = make_float2(c * D.attn_factor, s * D.attn_factor);
-    }
-    __syncthreads();
-
-    const int units = U::count(rot, d);
+    const int nt = t1 - t0, j0 = t0 - first;
     const int64_t row = (int64_t)row0 + j0;
-    if (a.q) {
-        const int per = a.k ? D.n_q_heads / Hkv : 1;    // query heads per head of the grid
-        const int h0 = blockIdx.y * a.heads * per, h1 = min(h0 + a.heads * per, D.n_q_heads);
-        const int work = (h1 - h0) * nt * units;
-        for (int idx = tid; idx < work; idx += kRopeThreads) {
-            const int u = idx % units, hj = idx / units, h = h0 + hj % (h1 - h0), j = hj / (h1 - h0);
-            U::turn(a.q, (row + j) * D.q_row_stride + (int64_t)h * d, u, rot, cs + j * half, [&](int c, const float (&y)[W]) {
-                store_unit<T, W>(a.q_out, (row + j) * D.q_out_row_stride + (int64_t)h * d + c, y);
-            });
+
+    // Rows of heads in the order of memory, unit by unit: the query heads of this workgroup and, 16-bit and fp32 caches, its kv heads.
+    const U units(D.rot_dim, d);
+    const int per = a.k ? (a.q ? D.n_q_heads / Hkv : 0) : 1;        // query heads per head of the grid
+    const int h0 = blockIdx.y * a.heads, nh = min(a.heads, (a.k ? Hkv : D.n_q_heads) - h0);
+    const int nq = nh * per, nk = a.k && !k8 ? nh : 0, both = nq + nk;
+    const int work = both * nt * units.count;
+    // Cosines and sines of the rows' pairs, by all wavefronts (each of which comes here once, with its own rows on their way).
+    const auto angles = [&] {
+        if (half == 0) return;
+        if (a.parents) {
+            // depths by doubling: every node looks at the node that its jumps so far have led to (the root at itself)
+            if (wv == 0) {
+                int up = lane > 0 && lane < n ? min(max(a.parents[row0 + lane], 0), lane - 1) : 0, dep = lane > 0 && lane < n ? 1 : 0;
+#pragma unroll
+                for (int s = 0; s < 6; ++s) {
+                    dep += __shfl(dep, up, kWave);
+                    up = __shfl(up, up, kWave);
+                }
+                depth[lane] = dep;
+            }
+            lds_barrier();
+        }
+        const Divider by_half(half);
+        for (int idx = tid; idx < nt * half; idx += kRopeThreads) {
+            int f;
+            const int j = by_half(idx, f);
+            const int pos = first + (a.parents ? depth[j0 + j] : j0 + j);
+            const double turns = (double)pos * (double)freq[f] * 0.15915494309189533577;        // 1 / (2 pi)
+            const float r = (float)(2.0 * (turns - rint(turns)));
+            float s, c;
+            sincospif(r, &s, &c);
+            cs[idx] = make_float2(c * D.attn_factor, s * D.attn_factor);
+        }
+        lds_barrier();
+    };
+    // (into a cache of 8 bits two wavefronts take the keys and values, where there are queries: one the keys, one the values)
+    const int kv_waves = k8 ? (a.q ? 2 : 4) : 0, threads = kRopeThreads - kv_waves * kWave, me = tid - kv_waves * kWave;
+    if constexpr (k8) {
+        if (wv < kv_waves) {
+            const int page = pages[0], lo = t0 % kPageTokens, last = page < 0 ? 0 : h0 + nh;
+            const auto append = [&](auto part, const void *x, int64_t stride, void *pages_of, float *scales, float gain, int cs_stride) {
+                const auto begin = [&](int h) {
+                    const int64_t at = (int64_t)page * Hkv + h;
+                    part.begin(x, row * stride + (int64_t)h * d, stride, d, static_cast<uint8_t *>(pages_of) + at * kPageTokens * d, scales + at, lo, nt, lane);
+                };
+                int h = h0 + wv / 2;
+                if (h < last) begin(h);
+                angles();
+                while (h < last) {
+                    part.finish(gain, cs, cs_stride);
+                    h += kv_waves / 2;
+                    if (h < last) begin(h);
+                }
+            };
+            if (wv & 1) append(PageAppend<T, 8, true>(Units<T, 8, true>(0, d)), a.v, D.v_row_stride, a.v_pages, a.v_scales, 1.f, 0);
+            else append(PageAppend<T, W, kInter>(units), a.k, D.k_row_stride, a.k_pages, a.k_scales, D.attn_factor, half);
+            return;
         }
     }
-    if (!a.k) return;
-    const int h0 = blockIdx.y * a.heads, h1 = min(h0 + a.heads, Hkv);
-    if constexpr (k8) {
-        const int page = pages[0], lo = t0 % kPageTokens;
-        if (page < 0) return;
-        const double gain2 = (double)D.attn_factor * (double)D.attn_factor;
-        for (int task = wv; task < 2 * (h1 - h0); task += kRopeThreads / kWave) {
-            const int h = h0 + task / 2;
-            const int64_t at = (int64_t)page * Hkv + h, off = at * kPageTokens * d;
-            if (task & 1)
-                append_page8<T, 8, true>(a.v, row * D.v_row_stride + (int64_t)h * d, D.v_row_stride, d, 0, 1.0, cs, 0,
-                                         static_cast<uint8_t *>(a.v_pages) + off, a.v_scales + at, lo, lo + nt, lane);
-            else
-                append_page8<T, W, kInter>(a.k, row * D.k_row_stride + (int64_t)h * d, D.k_row_stride, d, rot, gain2, cs, half,
-                                           static_cast<uint8_t *>(a.k_pages) + off, a.k_scales + at, lo, lo + nt, lane);
+    const Divider by_units(units.count), by_heads(both);
+    constexpr int kAhead = 2;
+    typename U::Item item[kAhead];
+    const auto where = [&](int idx, int &j, int &h, int &u) { j = by_heads(by_units(idx, u), h); };
+    const auto fetch = [&](typename U::Item &it, int idx) {
+        int j, h, u;
+        where(idx, j, h, u);
+        if (k8 || h < nq) units.fetch(it, a.q, (row + j) * D.q_row_stride + (int64_t)(h0 * per + h) * d, u);
+        else units.fetch(it, a.k, (row + j) * D.k_row_stride + (int64_t)(h0 + h - nq) * d, u);
+    };
+#pragma unroll
+    for (int e = 0; e < kAhead; ++e)
+        if (me + e * threads < work) fetch(item[e], me + e * threads);
+    angles();
+    for (int idx = me; idx < work; idx += kAhead * threads) {
+#pragma unroll
+        for (int e = 0; e < kAhead; ++e) {
+            if (idx + e * threads >= work) continue;
+            int j, h, u;
+            where(idx + e * threads, j, h, u);
+            void *out = a.q_out;
+            int64_t dst = (row + j) * D.q_out_row_stride + (int64_t)(h0 * per + h) * d;
+            if (!k8 && h >= nq) {
+                const int t = t0 + j, page = pages[t / kPageTokens - t0 / kPageTokens];
+                if (page < 0) continue;
+                out = a.k_pages;
+                dst = (((int64_t)page * Hkv + h0 + h - nq) * kPageTokens + t % kPageTokens) * d;
+            }
+            units.turn(item[e], u, cs + j * half, [&](int c, const float (&y)[W]) { store_unit<T, W>(out, dst + c, y); });
         }
-    } else {
-        const int nh = h1 - h0, work = nh * nt * units;
-        for (int idx = tid; idx < work; idx += kRopeThreads) {
-            const int u = idx % units, hj = idx / units, h = h0 + hj % nh, j = hj / nh, t = t0 + j;
-            const int page = pages[t / kPageTokens - t0 / kPageTokens];
-            if (page < 0) continue;
-            const int64_t dst = (((int64_t)page * Hkv + h) * kPageTokens + t % kPageTokens) * d;
-            U::turn(a.k, (row + j) * D.k_row_stride + (int64_t)h * d, u, rot, cs + j * half, [&](int c, const float (&y)[W]) {
-                store_unit<T, W>(a.k_pages, dst + c, y);
-            });
-        }
+#pragma unroll
+        for (int e = 0; e < kAhead; ++e)
+            if (idx + (kAhead + e) * threads < work) fetch(item[e], idx + (kAhead + e) * threads);
+    }
+    if constexpr (!k8) {
         // values as they are, 16 bytes at a time
         constexpr int kSize = sizeof(typename T::storage);
-        const int vecs = d * kSize / 16, copies = nh * nt * vecs;
+        const int vecs = d * kSize / 16, copies = nk * nt * vecs;
+        const Divider by_vecs(vecs), by_kv(max(nk, 1));
         for (int idx = tid; idx < copies; idx += kRopeThreads) {
-            const int u = idx % vecs, hj = idx / vecs, h = h0 + hj % nh, j = hj / nh, t = t0 + j;
+            int u, h;
+            const int j = by_kv(by_vecs(idx, u), h), t = t0 + j;
             const int page = pages[t / kPageTokens - t0 / kPageTokens];
             if (page < 0) continue;
-            const int64_t dst = (((int64_t)page * Hkv + h) * kPageTokens + t % kPageTokens) * d;
+            const int64_t dst = (((int64_t)page * Hkv + h0 + h) * kPageTokens + t % kPageTokens) * d;
             reinterpret_cast<uint4 *>(static_cast<char *>(a.v_pages) + dst * kSize)[u] =
-                reinterpret_cast<const uint4 *>(static_cast<const char *>(a.v) + ((row + j) * D.v_row_stride + (int64_t)h * d) * kSize)[u];
+                reinterpret_cast<const uint4 *>(static_cast<const char *>(a.v) + ((row + j) * D.v_row_stride + (int64_t)(h0 + h) * d) * kSize)[u];
         }
     }
 }
@@ -311,21 +461,33 @@ hipError_t launch_rope_append(const void *q, const void *k, const void *v, const
     RopeArgs a{q, k, v, inv_freq, q_out, k_pages, v_pages, k_scales, v_scales, block_table, ctx_lens, spec_lens, parents, d, rope_chunks(d, fp8), 1};
     if (!inv_freq) a.d.rot_dim = 0;
     const int heads = k ? d.n_kv_heads : d.n_q_heads;
-    a.heads = heads;
+    // Heads per workgroup: enough for its angles to be shared (20 rows of heads per row; into 8 bits, where a wavefront takes a head's keys
+    // or values, 2 kv heads, or 4 without shared ones), fewer where that leaves less than two workgroups per compute unit.
+    // MI355X, us, 1 / 2 / 4 / 8 kv heads of 32/8: 128 requests of up to 7 rows 6.9 / 6.3 / 7.3 / 9.8, into 8 bits 12.5 / 10.3 / 12.1 /
+    // 16.7; prompts of 32000 rows 189 / 195 / 168 / 177, into 8 bits (64/8) 306 / 258 / 264 / 275; 16 trees of up to 61 rows into 8
+    // bits 12.5 / 13.7 / 16.6 / 23.7; query heads alone (1 / 2 / 4 / 8), 17400 rows of 32 86 / 56 / 50 / 51.
+    const int shared = k && q ? d.n_q_heads / d.n_kv_heads : 1;
+    a.heads = !k ? 4 : !fp8 ? 20 / (shared + 1) : shared > 1 ? 2 : 4;
+    a.heads = a.heads < 1 ? 1 : a.heads > heads ? heads : a.heads;
+    while (a.heads > 1 && (int64_t)d.batch * a.chunks * ceil_div(heads, a.heads) < 512) a.heads = (a.heads + 1) / 2;
+    const size_t lds = (size_t)kRopeRows * (a.d.rot_dim / 2) * sizeof(float2);
     const dim3 grid((unsigned)((int64_t)d.batch * a.chunks), ceil_div(heads, a.heads));
     auto launch = [&](auto tag) {
         using T = decltype(tag);
         auto with = [&](auto w, auto inter) {
             constexpr int W = decltype(w)::value;
             constexpr bool kInter = decltype(inter)::value;
-            if (fp8) hipLaunchKernelGGL((rope_append_kernel<T, W, kInter, true>), grid, dim3(kRopeThreads), 0, stream, a);
-            else hipLaunchKernelGGL((rope_append_kernel<T, W, kInter, false>), grid, dim3(kRopeThreads), 0, stream, a);
+            if (fp8) hipLaunchKernelGGL((rope_append_kernel<T, W, kInter, true>), grid, dim3(kRopeThreads), lds, stream, a);
+            else hipLaunchKernelGGL((rope_append_kernel<T, W, kInter, false>), grid, dim3(kRopeThreads), lds, stream, a);
         };
         if (d.interleaved || a.d.rot_dim == 0) {
             if (a.d.rot_dim % 8 == 0) with(std::integral_constant<int, 8>{}, std::true_type{});
+            else if (a.d.rot_dim % 4 == 0) with(std::integral_constant<int, 4>{}, std::true_type{});
             else with(std::integral_constant<int, 2>{}, std::true_type{});
         } else {
             if (a.d.rot_dim % 16 == 0) with(std::integral_constant<int, 8>{}, std::false_type{});
+            else if (a.d.rot_dim % 8 == 0) with(std::integral_constant<int, 4>{}, std::false_type{});
+            else if (a.d.rot_dim % 4 == 0) with(std::integral_constant<int, 2>{}, std::false_type{});
             else with(std::integral_constant<int, 1>{}, std::false_type{});
         }
     };
