@@ -403,7 +403,7 @@ int adaspec_kv_append_rope(const void *q, const void *k_new, const void *v_new, 
 /* ------------------------------------------------------------------------
  * adaspec_verify_attn_scaled - verification attention over a cache of 8 bits, as
  * adaspec_kv_append_rope leaves it: k_pages, v_pages of e4m3 (dims->dtype is the
- * type of q), k_scales, v_scales [num_pages][Hkv] fp32 of any finite value.
+ * type of q), k_scales, v_scales [num_pages][Hkv] fp32, finite and not negative.
  * parents NULL: a chain, as adaspec_verify_attn; else a tree, as
  * adaspec_verify_attn_tree.  Same dims, plan modes and error rules; a workspace
  * of its own size.  A token influences only rows that see it, whatever it holds.

@@ -5,8 +5,8 @@
 //   S^T = K Q^T,  O^T += V^T P^T,  in accumulator layouts that need no shuffle.
 // What 8 bits change:
 //   * An e4m3 value is exact in bf16 and in f16.  K becomes Q's type in registers, two elements an instruction; its scale is
-//     one factor per page, applied to the scores.  V becomes bf16; its scale is applied to the softmax weights, which are
-//     split into two bf16 pieces (16 bits): one piece, off by up to 2^-9, would be the largest error there is.
+//     one factor per page, applied to the scores.  V becomes f16; its scale is applied to the softmax weights, relative to the
+//     largest so far, which the accumulators are kept in units of.
 //   * Both products contract in any order of their k-slots, as long as their two operands agree.  So a lane takes 16
 //     consecutive bytes of a key at a time, and Q is laid out to match.
 //   * No LDS tile for V^T: a lane loads D / 16 neighbouring channels of the four tokens 4g .. 4g + 3 of a page, and byte
@@ -37,6 +37,10 @@ template <class T> __device__ __forceinline__ uint4 e4m3_operand(uint32_t lo, ui
 // the bytes of w that are NaN, as 0x80
 __device__ __forceinline__ uint32_t e4m3_nans(uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
 
+// Softmax weights reach the matrix core as f16, 11 bits, 2^kWeightShift larger: at most 2^15, as they trail 1 by 2^kLazyLog2 at most, and
+// down to 2^-21 of the largest before bits are lost to subnormals.  Off by 2^-11 at most, where what they weigh has 4 bits.
+constexpr int kWeightShift = 7;
+
 template <class T, int D, int RT, bool kTree, bool kDirect>
 __global__ __launch_bounds__(256, (RT == 1 ? 3 : 2)) void attn_e4m3_kernel(
     const char *__restrict__ q, const char *__restrict__ k_pages, const char *__restrict__ v_pages,
@@ -47,6 +51,7 @@ __global__ __launch_bounds__(256, (RT == 1 ? 3 : 2)) void attn_e4m3_kernel(
     int Hq, int Hkv, int max_pages_per_req, int max_rows, int n_row_groups, float scale_log2, int out_dtype, int cus, DirectArgs direct)
 {
     constexpr int kRows = 16 * RT;
+    constexpr bool kCount = RT > 3;                                 // tiles without rows are skipped at run time in the inner loop, too
     constexpr int kTokens = attn_e4m3_block(D), kPages = kTokens / 16;
     constexpr int kKLoads = D / 64;                                 // 16-byte pieces of a key per lane
     constexpr int kSteps = D / 32;                                  // products per 16 x 16 tile of scores
@@ -68,12 +73,13 @@ __global__ __launch_bounds__(256, (RT == 1 ? 3 : 2)) void attn_e4m3_kernel(
     const int total_units = kDirect ? 0 : header[0] * Hkv * n_row_groups;
     float *my_state = reinterpret_cast<float *>(smem + wv * kSlab);
 
-    // K: lane (g, m) <- token 16 mt + m, channels 64 c + 16 g .. + 15.  V: lane (g, m) <- token 16 p + 4 g + i, channels (D / 16) m ..
+    // Row m of a tile of K is token (m >> 2) + 4 (m & 3) of its page: lane (g, n) then holds scores of tokens g, g + 4, g + 8, g + 12, and of V
+    // it takes the same, D / 16 channels from (D / 16) n on.  (Four neighbouring rows of V per load.)
     uint4 kreg[kPages][kKLoads];
     uint32_t vreg[kPages][4][kWords];
     float ks[kPages], vs[kPages];                                   // scales of the block in registers
-    const uint32_t k_lane_off = n16 * D + 16 * g;
-    const uint32_t v_lane_off = (4 * g) * D + kTiles * n16;
+    const uint32_t k_lane_off = ((n16 >> 2) + 4 * (n16 & 3)) * D + 16 * g;
+    const uint32_t v_lane_off = g * D + kTiles * n16;
 
     const int W = gridDim.x, wg = blockIdx.x;
     const int n_rounds = kDirect ? 0 : header[2];
@@ -121,7 +127,7 @@ __global__ __launch_bounds__(256, (RT == 1 ? 3 : 2)) void attn_e4m3_kernel(
         for (int p = 0; p < kPages; ++p)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const char *at = v_pages + b[p] * (16 * D) + v_lane_off + i * D;
+                const char *at = v_pages + b[p] * (16 * D) + v_lane_off + 4 * i * D;
                 if constexpr (kWords == 2) {
                     const u32x2v w = __builtin_nontemporal_load(reinterpret_cast<const u32x2v *>(at));
                     vreg[p][i][0] = w.x;
@@ -185,7 +191,7 @@ __global__ __launch_bounds__(256, (RT == 1 ? 3 : 2)) void attn_e4m3_kernel(
         if constexpr (kTree) { if (tid < kRows) s_anc[tid] = av; }
         lds_barrier();
 
-        float m[RT], lsum[RT];
+        float m[RT], lsum[RT], vref = 0.f, vref_inv = 0.f;         // O is kept in units of vref 2^-kWeightShift
         f32x4 o[RT][kTiles];
 #pragma unroll
         for (int nt = 0; nt < RT; ++nt) {
@@ -197,8 +203,10 @@ __global__ __launch_bounds__(256, (RT == 1 ? 3 : 2)) void attn_e4m3_kernel(
         const int tiles = min((u.rows - u.r0 + 15) / 16, RT);       // row tiles of the unit that have rows (others cost nothing)
         // One block.  kInner: every row sees all of it, and another one follows, whose K and V are requested as soon as their
         // registers are free (without a branch around the loads, so that the compiler's waits count exactly).
-        auto block = [&](int bi, auto inner_tag) {
+        // kNT: its row tiles that have rows, where that is known, else RT.
+        auto block = [&](int bi, auto inner_tag, auto tiles_tag) {
             constexpr bool kInner = decltype(inner_tag)::value;
+            constexpr int kNT = decltype(tiles_tag)::value;
             constexpr int kE = 4 * kPages;                          // scores per lane and row tile
             const int tb = u.t0 + bi * kTokens;
             int64_t nb[kPages];
@@ -207,7 +215,7 @@ __global__ __launch_bounds__(256, (RT == 1 ? 3 : 2)) void attn_e4m3_kernel(
             if (next) page_blocks(u, bi + kWaves, nb);
 
             // ---- S^T = K Q^T ------------------------------------------------------------
-            float p[RT][kE];
+            float p[kNT][kE];
 #pragma unroll
             for (int mt = 0; mt < kPages; ++mt) {
                 uint4 kop[kSteps];
@@ -219,8 +227,8 @@ __global__ __launch_bounds__(256, (RT == 1 ? 3 : 2)) void attn_e4m3_kernel(
                 const float factor = ks[mt] * scale_log2;
                 if constexpr (RT > 2) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int nt = 0; nt < RT; ++nt) {
-                    if (nt > 0 && nt >= tiles) break;
+                for (int nt = 0; nt < kNT; ++nt) {
+                    if ((!kInner || kCount) && nt > 0 && nt >= tiles) break;
                     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                     for (int s = 0; s < kSteps; ++s) acc = Mma<T>::run(kop[s], q_lds[(nt * kSteps + s) * 64 + lane], acc);
@@ -234,10 +242,25 @@ __global__ __launch_bounds__(256, (RT == 1 ? 3 : 2)) void attn_e4m3_kernel(
             __builtin_amdgcn_sched_barrier(0);
 
             // ---- online softmax (per lane: row n16 of each row tile, kE of the tokens), in log2 units ----
-            uint32_t seen[RT];                                      // masked: bit e = the row sees token e
+            uint32_t seen[kNT];                                      // masked: bit e = the row sees token e
+            // (the values' scales relative to the largest so far, which O is kept in units of)
+            float most_vs = vs[0], weight[kPages];
 #pragma unroll
-            for (int nt = 0; nt < RT; ++nt) {
-                if (nt > 0 && nt >= tiles) break;
+            for (int mt = 1; mt < kPages; ++mt) most_vs = fmaxf(most_vs, vs[mt]);
+            if (__builtin_expect(most_vs > vref, 0)) {
+                const float down = vref / most_vs;
+                vref = most_vs;
+                vref_inv = (1 << kWeightShift) / most_vs;
+#pragma unroll
+                for (int nt = 0; nt < kNT; ++nt)
+#pragma unroll
+                    for (int t = 0; t < kTiles; ++t) o[nt][t] *= down;
+            }
+#pragma unroll
+            for (int mt = 0; mt < kPages; ++mt) weight[mt] = vs[mt] * vref_inv;
+#pragma unroll
+            for (int nt = 0; nt < kNT; ++nt) {
+                if ((!kInner || kCount) && nt > 0 && nt >= tiles) break;
                 if (masked) {
                     seen[nt] = 0;
                     const unsigned long long am = kTree ? s_anc[16 * nt + n16] : 0ull;
@@ -245,7 +268,7 @@ __global__ __launch_bounds__(256, (RT == 1 ? 3 : 2)) void attn_e4m3_kernel(
                     const int pos = row < u.rows ? base + row / G : -1, lim = min(pos, u.t1 - 1);
 #pragma unroll
                     for (int e = 0; e < kE; ++e) {
-                        const int t = tb + 16 * (e >> 2) + 4 * g + (e & 3), rel = t - base;
+                        const int t = tb + 16 * (e >> 2) + g + 4 * (e & 3), rel = t - base;
                         bool vis;
                         if constexpr (kTree) vis = t < u.t1 && (rel < 0 ? pos >= 0 : ((am >> (rel & 63)) & 1ull) != 0);
                         else vis = t <= lim;
@@ -273,7 +296,7 @@ __global__ __launch_bounds__(256, (RT == 1 ? 3 : 2)) void attn_e4m3_kernel(
                 for (int e = 0; e < kE; ++e) {
                     p[nt][e] = __builtin_amdgcn_exp2f(p[nt][e] - m[nt]);
                     psum += p[nt][e];
-                    p[nt][e] *= vs[e >> 2];
+                    p[nt][e] *= weight[e >> 2];
                     // what hidden tokens hold stays out: no weight, whatever their scale
                     if (masked) p[nt][e] = (seen[nt] >> e) & 1 ? p[nt][e] : 0.f;
                 }
@@ -289,7 +312,7 @@ __global__ __launch_bounds__(256, (RT == 1 ? 3 : 2)) void attn_e4m3_kernel(
                     for (int i = 0; i < 4; ++i)
 #pragma unroll
                         for (int w = 0; w < kWords; ++w) {
-                            if (tb + 16 * pg + 4 * g + i >= u.t1) vreg[pg][i][w] = 0;
+                            if (tb + 16 * pg + g + 4 * i >= u.t1) vreg[pg][i][w] = 0;
                             nans |= e4m3_nans(vreg[pg][i][w]);
                         }
                 if (__builtin_expect(__builtin_amdgcn_ballot_w64(nans != 0) != 0, 0)) {
@@ -305,8 +328,8 @@ __global__ __launch_bounds__(256, (RT == 1 ? 3 : 2)) void attn_e4m3_kernel(
                                 bad[e] = (e4m3_nans(vreg[2 * hf + (e >> 2)][e & 3][t >> 2]) >> (8 * (t & 3))) & 0x80u ? 0x3f80u : 0u;
                             const uint4 a = make_uint4(bad[0] | bad[1] << 16, bad[2] | bad[3] << 16, bad[4] | bad[5] << 16, bad[6] | bad[7] << 16);
 #pragma unroll
-                            for (int nt = 0; nt < RT; ++nt) {
-                                if (nt > 0 && nt >= tiles) break;
+                            for (int nt = 0; nt < kNT; ++nt) {
+                                if ((!kInner || kCount) && nt > 0 && nt >= tiles) break;
                                 uint32_t see[8];
 #pragma unroll
                                 for (int e = 0; e < 8; ++e) see[e] = (seen[nt] >> (8 * hf + e)) & 1 ? 0x3f80u : 0u;
@@ -333,17 +356,12 @@ __global__ __launch_bounds__(256, (RT == 1 ? 3 : 2)) void attn_e4m3_kernel(
             // ---- O^T += V^T P^T, 32 tokens at a time ------------------------------
 #pragma unroll
             for (int hf = 0; hf < kHalves; ++hf) {
-                uint4 hi[RT], lo[RT];
+                uint4 pop[kNT];
 #pragma unroll
-                for (int nt = 0; nt < RT; ++nt) {
-                    if (nt > 0 && nt >= tiles) break;
+                for (int nt = 0; nt < kNT; ++nt) {
+                    if ((!kInner || kCount) && nt > 0 && nt >= tiles) break;
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const float x = p[nt][8 * hf + 2 * j], y = p[nt][8 * hf + 2 * j + 1];
-                        const uint32_t w = Mma<BF16>::pack2(x, y);
-                        (&hi[nt].x)[j] = w;
-                        (&lo[nt].x)[j] = Mma<BF16>::pack2(x - __uint_as_float(w << 16), y - __uint_as_float(w & 0xffff0000u));
-                    }
+                    for (int j = 0; j < 4; ++j) (&pop[nt].x)[j] = Mma<F16>::pack2(p[nt][8 * hf + 2 * j], p[nt][8 * hf + 2 * j + 1]);
                 }
 #pragma unroll
                 for (int w = 0; w < kWords; ++w)
@@ -356,18 +374,16 @@ __global__ __launch_bounds__(256, (RT == 1 ? 3 : 2)) void attn_e4m3_kernel(
                             pair[j] = __builtin_amdgcn_perm(v[2 * (j & 1) + 1][w], v[2 * (j & 1)][w], up ? 0x07030602u : 0x05010400u);
                         }
                         if constexpr (RT > 2) __builtin_amdgcn_sched_barrier(0);
-                        const uint4 even = make_uint4(e4m3_pair<BF16, false>(pair[0]), e4m3_pair<BF16, false>(pair[1]),
-                                                      e4m3_pair<BF16, false>(pair[2]), e4m3_pair<BF16, false>(pair[3]));
-                        const uint4 odd = make_uint4(e4m3_pair<BF16, true>(pair[0]), e4m3_pair<BF16, true>(pair[1]),
-                                                     e4m3_pair<BF16, true>(pair[2]), e4m3_pair<BF16, true>(pair[3]));
+                        const uint4 even = make_uint4(e4m3_pair<F16, false>(pair[0]), e4m3_pair<F16, false>(pair[1]),
+                                                      e4m3_pair<F16, false>(pair[2]), e4m3_pair<F16, false>(pair[3]));
+                        const uint4 odd = make_uint4(e4m3_pair<F16, true>(pair[0]), e4m3_pair<F16, true>(pair[1]),
+                                                     e4m3_pair<F16, true>(pair[2]), e4m3_pair<F16, true>(pair[3]));
                         const int t = 4 * w + 2 * up;
 #pragma unroll
-                        for (int nt = 0; nt < RT; ++nt) {
-                            if (nt > 0 && nt >= tiles) break;
-                            o[nt][t] = Mma<BF16>::run(even, hi[nt], o[nt][t]);
-                            o[nt][t + 1] = Mma<BF16>::run(odd, hi[nt], o[nt][t + 1]);
-                            o[nt][t] = Mma<BF16>::run(even, lo[nt], o[nt][t]);
-                            o[nt][t + 1] = Mma<BF16>::run(odd, lo[nt], o[nt][t + 1]);
+                        for (int nt = 0; nt < kNT; ++nt) {
+                            if ((!kInner || kCount) && nt > 0 && nt >= tiles) break;
+                            o[nt][t] = Mma<F16>::run(even, pop[nt], o[nt][t]);
+                            o[nt][t + 1] = Mma<F16>::run(odd, pop[nt], o[nt][t + 1]);
                         }
                     }
             }
@@ -380,8 +396,17 @@ __global__ __launch_bounds__(256, (RT == 1 ? 3 : 2)) void attn_e4m3_kernel(
         if (wv < u.nblk) {
             const int full = max(min(first_masked, u.t1) - u.t0, 0) / kTokens;         // blocks that every row sees all of
             int bi = wv;
-            for (; bi + kWaves < u.nblk && bi < full; bi += kWaves) block(bi, std::true_type{});
-            for (; bi < u.nblk; bi += kWaves) block(bi, std::false_type{});
+            auto inner = [&](auto tiles_tag) {
+                for (; bi + kWaves < u.nblk && bi < full; bi += kWaves) block(bi, std::true_type{}, tiles_tag);
+            };
+            // (A copy of the loop for every number of tiles; with four of them they crowd the instruction cache: 128 requests of 128-4096
+            // tokens, trees of up to 13 nodes, 32/8 heads: 152 us with one copy, whose tiles are counted at run time, 168 with four.
+            // Up to three: 100.4 us against 101.7 for the headline batch, 497 against 505 for 64 of 8192-32768, 64/8 heads)
+            if (kCount) inner(std::integral_constant<int, RT>{});
+            else if (RT == 1 || tiles <= 1) inner(std::integral_constant<int, 1>{});
+            else if (RT == 2 || tiles == 2) inner(std::integral_constant<int, RT < 2 ? 1 : 2>{});
+            else inner(std::integral_constant<int, RT < 3 ? 1 : 3>{});
+            for (; bi < u.nblk; bi += kWaves) block(bi, std::false_type{}, std::integral_constant<int, RT>{});
         }
 
         // ---- next unit: its first block and its Q rows travel while this unit's states are merged
@@ -391,6 +416,7 @@ __global__ __launch_bounds__(256, (RT == 1 ? 3 : 2)) void attn_e4m3_kernel(
             first_loads(nxt);
         }
         // ---- merge the four wavefronts' states through LDS (as in attn_mfma.hip), one row tile after the other ----------
+        const float o_unit = vref * (1.f / (1 << kWeightShift));
 #pragma unroll
         for (int nt = 0; nt < RT; ++nt) {
             if (nt > 0 && nt >= tiles) break;
@@ -403,7 +429,7 @@ __global__ __launch_bounds__(256, (RT == 1 ? 3 : 2)) void attn_e4m3_kernel(
 #pragma unroll
                 for (int t = 0; t < kTiles; t += 4)
                     *reinterpret_cast<f32x4 *>(my_state + n16 * kORow + kTiles * (4 * g + r) + t) =
-                        f32x4{o[nt][t][r], o[nt][t + 1][r], o[nt][t + 2][r], o[nt][t + 3][r]};
+                        f32x4{o[nt][t][r], o[nt][t + 1][r], o[nt][t + 2][r], o[nt][t + 3][r]} * o_unit;
             lds_barrier();
             // 256 threads: 16 rows x D / 4 float4 columns
             constexpr int kCols = D / 4;

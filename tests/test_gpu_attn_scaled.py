@@ -1,8 +1,9 @@
 """Verification attention over the cache in 8 bits (csrc/attn_e4m3.hip, attn_vector.hip) against the oracle in 64 bits.
 
-Tolerance on the fp32 accumulator: 2e-5 for values of unit size, that of the other attention tests.  Keys and values are exact in the
-products; the softmax weights are two bf16 pieces, which leave at most 2^-18 of a weight out: of a mean of values below 5, 1.9e-5 if every
-weight were off by that much to the same side.  Outputs of 16 bits: half a step on top."""
+Tolerance on the fp32 accumulator: 2e-5 for values of unit size, that of the other attention tests, where weights are fp32 (the
+portable form).  On the matrix cores keys and values are exact in the products, the softmax weights are f16: each is off by up to half
+a step of 11 bits, torch.finfo(torch.float16).eps / 2 = 2^-11 of it, and a mean of values by up to 2^-11 times the mean of their magnitudes, which the oracle's weights give row by
+row and channel by channel.  Outputs of 16 bits: half a step on top."""
 import numpy as np
 import pytest
 
@@ -43,21 +44,28 @@ def call(pkg, c, **kw):  # noqa: F811
 
 
 def oracle(c):
+    """(outputs, the mean of the values' magnitudes with the same weights)"""
+    magnitudes = dict(c, v8=np.where(c["v8"] & 0x7f == 0x7f, c["v8"], c["v8"] & 0x7f))
+    return _oracle(c), _oracle(magnitudes)
+
+
+def _oracle(c):
     return P.verify_attn_scaled(c["q"], c["k8"], c["v8"], c["ks"], c["vs"], c["bt"], c["ctx"], c["spec"], dtype=c["dtype"], parents=c["parents"])
 
 
 def check(pkg, c, paths=("auto", "vector"), ref=None, **kw):  # noqa: F811
-    ref = oracle(c) if ref is None else ref
+    ref, size = oracle(c) if ref is None else ref
+    fast = c["q"].shape[2] in (64, 128) and c["dtype"] != "f32"
     for path in paths:
+        tol = TOL + (2.0 ** -11 * size if fast and path == "auto" else 0.0) + np.zeros(ref.shape)
         print(f"[case] attn8 {c['dtype']} {c['q'].shape} Hkv={c['k8'].shape[1]} B={len(c['ctx'])} tree={c['parents'] is not None} {path}", flush=True)
         out = host(call(pkg, c, out_dtype=0, path=path, **kw)).astype(np.float64)
         assert np.array_equal(np.isnan(out), np.isnan(ref)), path
         fine = ~np.isnan(ref)
-        assert np.abs(out - ref)[fine].max() <= TOL, (path, np.abs(out - ref)[fine].max())
+        assert (np.abs(out - ref) <= tol)[fine].all(), (path, np.abs(out - ref)[fine].max())
         own = widen(host(call(pkg, c, path=path, **kw), c["dtype"]), c["dtype"])
-        tol = TOL + HALF_STEP[c["dtype"]] * (np.abs(ref) + TOL) + LEAST[c["dtype"]]
+        tol = tol + HALF_STEP[c["dtype"]] * (np.abs(ref) + tol) + LEAST[c["dtype"]]
         assert (np.abs(own - ref) <= tol)[fine].all(), path
-    return ref
 
 
 SHAPES = [
@@ -115,7 +123,7 @@ def test_a_token_counts_only_where_it_is_seen(is_tree, d, pkg):  # noqa: F811
                 c["vs"][page, 0] = np.nan                   # a page of drafts alone
         ref = oracle(c)
         if what != "scales":
-            assert np.isnan(ref).any() and not np.isnan(ref).all()
+            assert np.isnan(ref[0]).any() and not np.isnan(ref[0]).all()
         check(pkg, c, ref=ref)
 
 
@@ -133,7 +141,7 @@ def test_large_scores_and_scales(dtype, pkg):  # noqa: F811
     c = make(12, [300, 33], [5, 0], 8, 2, 128, dtype)
     c["ks"] *= np.float32(400.0)
     c["vs"] *= np.float32(2.0 ** 40)
-    ref = oracle(c)
+    ref, _ = oracle(c)
     for path in ("auto", "vector"):
         out = host(call(pkg, c, out_dtype=0, path=path)).astype(np.float64)
         assert np.abs(out - ref).max() <= 4e-3 * 2.0 ** 40 * 5
@@ -150,8 +158,9 @@ def test_plans_graphs_streams_and_threads(pkg):  # noqa: F811
         t = [dev(c["q"], "bf16"), dev(c["k8"], "e4m3"), dev(c["v8"], "e4m3"), dev(c["bt"]), ints(*c["ctx"]), ints(*c["spec"])]
         kw = dict(max_spec_len=6, k_scales=dev(c["ks"]), v_scales=dev(c["vs"]), parents=None if c["parents"] is None else dev(c["parents"]))
         want = pkg.verify_attn(*t, **kw)
-        ref = oracle(c)
-        assert (np.abs(widen(host(want, "bf16"), "bf16") - ref) <= TOL + HALF_STEP["bf16"] * (np.abs(ref) + TOL)).all()
+        ref, size = oracle(c)
+        tol = TOL + 2.0 ** -11 * size
+        assert (np.abs(widen(host(want, "bf16"), "bf16") - ref) <= tol + HALF_STEP["bf16"] * (np.abs(ref) + tol)).all()
         jobs.append((t, kw, want))
         # metadata once, then used
         ws = torch.empty(1 << 24, dtype=torch.uint8, device="cuda")
@@ -204,11 +213,11 @@ def test_a_pool_beyond_32_bits(pkg):  # noqa: F811
     for t, x in ((ks, c["ks"]), (vs, c["vs"])):
         t[num - len(x):] = torch.from_numpy(x).cuda()
     bt = np.where(c["bt"] >= 0, far[np.maximum(c["bt"], 0)], -1).astype(np.int32)
-    ref, e8 = oracle(c), torch.float8_e4m3fn
+    (ref, size), e8 = oracle(c), torch.float8_e4m3fn
     for path in ("auto", "vector"):
         out = pkg.verify_attn(dev(c["q"], "bf16"), k8.view(e8), v8.view(e8), dev(bt), ints(100, 50), ints(3, 1), max_spec_len=3, k_scales=ks, v_scales=vs,
                               out_dtype=0, path=path)
-        assert np.abs(host(out) - ref).max() <= TOL
+        assert (np.abs(host(out) - ref) <= TOL + 2.0 ** -11 * size).all()
     # an append there
     kn, vn = (torch.randn((6, hkv, d), device="cuda").bfloat16() for _ in range(2))
     pkg.kv_append(kn, vn, k8.view(e8), v8.view(e8), dev(bt), ints(100, 50), ints(3, 1), max_spec_len=3, k_scales=ks, v_scales=vs)
