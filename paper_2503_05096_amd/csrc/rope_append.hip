@@ -367,10 +367,12 @@ __global__ __launch_bounds__(kRopeThreads) void rope_append_kernel(RopeArgs a)
             const int j = by_half(idx, f);
             const int pos = first + (a.parents ? depth[j0 + j] : j0 + j);
             const double turns = (double)pos * (double)freq[f] * 0.15915494309189533577;        // 1 / (2 pi)
-            const float r = (float)(2.0 * (turns - rint(turns)));
+            // (half turns, in two floats: what the first leaves turns the result by that little further)
+            const double halves = 2.0 * (turns - rint(turns));
+            const float r = (float)halves, more = (float)(halves - r) * 3.14159265f;
             float s, c;
             sincospif(r, &s, &c);
-            cs[idx] = make_float2(c * D.attn_factor, s * D.attn_factor);
+            cs[idx] = make_float2(fmaf(-s, more, c) * D.attn_factor, fmaf(c, more, s) * D.attn_factor);
         }
         lds_barrier();
     };
