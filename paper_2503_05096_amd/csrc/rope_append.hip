@@ -22,6 +22,7 @@ namespace adaspec {
 
 constexpr int kRopeThreads = 256;
 constexpr int kRopeRows = 16;
+static_assert(kRopeRows == kPageTokens, "a workgroup's rows are those of a page");
 constexpr int kRopeMaxHalf = 128;       // pairs of a head
 constexpr int kFewChunks = 8;           // MI355X, us: headline step into 8 bits, 2 chunks a request, 10.2 -> 9.4, but prompts of up to 250 257 -> 324
 
@@ -316,13 +317,14 @@ __global__ __launch_bounds__(kRopeThreads) void rope_append_kernel(RopeArgs a)
 
     const int n = min(max(a.spec_lens[i], 0), D.max_spec_len) + 1;
     const int L = a.ctx_lens[i], first = L - n;
-    // tokens [t0, t1) of the request
-    const int t0 = k8 ? max(first, (first / kPageTokens + chunk) * kPageTokens) : first + chunk * kRopeRows;
-    const int t1 = k8 ? min(L, (first / kPageTokens + chunk + 1) * kPageTokens) : min(L, t0 + kRopeRows);
+    // its rows [j0, j1) here: tokens [t0, t1) of the request (counted from the first row: a length may be anything)
+    const int in_page = k8 ? first % kPageTokens : 0;
+    const int j0 = max(0, chunk * kRopeRows - in_page), j1 = min(n, (chunk + 1) * kRopeRows - in_page);
+    const int t0 = first + j0, t1 = first + j1;
     int part = 0;
     for (int j = tid; j < i; j += kRopeThreads) part += min(max(a.spec_lens[j], 0), D.max_spec_len) + 1;
     if (tid < half) freq[tid] = a.inv_freq[tid];
-    if (first < 0 || t0 >= t1) return;
+    if (L < n || j0 >= j1) return;
     if (a.k && tid < 2) {
         const int at = t0 / kPageTokens + tid;
         int page = -1;
@@ -336,7 +338,7 @@ __global__ __launch_bounds__(kRopeThreads) void rope_append_kernel(RopeArgs a)
 #pragma unroll
     for (int w = 0; w < kRopeThreads / kWave; ++w) row0 += wsum[w];
     if (row0 + n > D.total_q) return;                   // inconsistent metadata: touch nothing
-    const int nt = t1 - t0, j0 = t0 - first;
+    const int nt = j1 - j0;
     const int64_t row = (int64_t)row0 + j0;
 
     // Rows of heads in the order of memory, unit by unit: the query heads of this workgroup and, 16-bit and fp32 caches, its kv heads.

@@ -446,7 +446,7 @@ __global__ __launch_bounds__(64) void kv_compact_path_scaled_kernel(
     const int k = min(max(spec_lens[i], 0), min(max_spec_len, 63));
     const int a = min(max(out_accept_len[i], 0), k);
     const int base = ctx_lens[i] - (k + 1);
-    if (base < 0 || a == 0) return;
+    if (ctx_lens[i] < k + 1 || a == 0) return;
     // lane j: accepted node j (they rise; what does not ends the path)
     const int node = lane < a ? out_path[(int64_t)i * path_stride + lane] : 0;
     int before = __shfl_up(node, 1, kWave);

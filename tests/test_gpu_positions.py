@@ -161,6 +161,33 @@ def test_lengths_that_make_no_sense_are_left_alone(pkg):  # noqa: F811
     assert bool((out[6:] == 7).all()) and not bool((out[:6] == 7).any())
 
 
+@pytest.mark.parametrize("bits", [16, 8])
+def test_lengths_at_the_ends_of_32_bits(bits, pkg):  # noqa: F811
+    """Several chunks of rows behind a position whose next ones do not fit in 32 bits: turned, and no page is written to."""
+    import torch
+    d, most, low = 64, 2 ** 31 - 1, -2 ** 31
+    f = frequencies(d, 10.0) / np.float32(64)           # (2^31 steps of 1 are more turns than 64 bits hold to 2^-21)
+    ctx, spec = [most, low, most - 20, 40, low + 30, most], [40, 40, 5, 40, 60, 0]
+    TQ = sum(spec) + len(spec)
+    q, k, v = (torch.randn((TQ, 2, d), device="cuda").half() for _ in range(3))
+    kind = torch.float8_e4m3fn if bits == 8 else torch.half
+    pools = [torch.zeros((4, 2, 16, d), device="cuda").to(kind) for _ in range(2)]
+    scales = [torch.ones((4, 2), device="cuda") for _ in range(2)] if bits == 8 else [None] * 2
+    out, table_ = torch.full_like(q, 7.0), torch.full((6, 3), 2, dtype=torch.int32, device="cuda")
+    pkg.kv_append_rope(q, k, v, dev(f), *pools, table_, ints(*ctx), ints(*spec), max_spec_len=62, k_scales=scales[0], v_scales=scales[1], q_out=out)
+    torch.cuda.synchronize()
+    assert all(bool((x.float() == 0).all()) for x in pools) and all(bool((x == 1).all()) for x in scales if x is not None)
+    row = 0
+    for L, s in zip(ctx, spec):
+        part = slice(row, row + s + 1)
+        if L < s + 1:                                       # no such request
+            assert bool((out[part] == 7).all())
+        else:
+            close(widen(host(out[part]), "f16"), P.rope(host(q[part]), f, [L], [s], dtype="f16"), widen(host(q[part]), "f16"), d, "f16", False, 1.0)
+        row += s + 1
+    assert torch.equal(pkg.rope(q, dev(f), ints(*ctx), ints(*spec), max_spec_len=62, out=torch.full_like(q, 7.0)), out)
+
+
 def test_many_requests_on_streams_and_in_graphs(pkg):  # noqa: F811
     import torch
     rng = np.random.default_rng(8)
