@@ -369,7 +369,8 @@ int adaspec_kv_append(const void *k_new, const void *v_new, void *k_pages, void 
  * Rows of q, k_new, v_new, q_out may be apart (strides in elements, multiples of 8,
  * at least heads * head_dim): slices of one projection's output.  All tensors 16-byte
  * aligned.  head_dim is a multiple of 8 up to 256, rot_dim even, in [2, head_dim];
- * page_size 16; at most 2^23 (request, 16 rows) pairs at max_spec_len.  Needs no
+ * page_size 16; at most 2^23 (request, 16 rows) pairs at max_spec_len, 65535 heads of
+ * either kind, 2^23 entries of them, 255 query heads per kv head.  Needs no
  * workspace.  A request whose lengths make no sense is left alone, an entry of
  * block_table outside the pool is not written to.
  * ---------------------------------------------------------------------- */

@@ -910,9 +910,11 @@ static int rope_impl(const void *q, const void *k_new, const void *v_new, const 
     if (append && d.page_size != 16) return ADASPEC_ERR_UNSUPPORTED;
     if (parents && d.max_spec_len > 63) return ADASPEC_ERR_UNSUPPORTED;
     const int64_t q_width = (int64_t)d.n_q_heads * d.head_dim, kv_width = (int64_t)d.n_kv_heads * d.head_dim;
-    // (rows of a workgroup are counted in 32 bits, a page's bytes too)
-    if (q && q_width > 1 << 23) return ADASPEC_ERR_UNSUPPORTED;
-    if (append && kv_width > 1 << 23) return ADASPEC_ERR_UNSUPPORTED;
+    // (rows of a workgroup are counted in 32 bits, a page's bytes too; heads are a dimension of the grid; a workgroup's units, 16 rows of
+    // up to 2 kv heads' query heads, are fewer than 2^21: Divider in rope_append.hip)
+    if (q && (q_width > 1 << 23 || d.n_q_heads > 65535)) return ADASPEC_ERR_UNSUPPORTED;
+    if (append && (kv_width > 1 << 23 || d.n_kv_heads > 65535)) return ADASPEC_ERR_UNSUPPORTED;
+    if (q && append && d.n_q_heads / d.n_kv_heads > 255) return ADASPEC_ERR_UNSUPPORTED;
     if (d.max_spec_len > (1 << 30) || !rope_grid_fits(d, e4m3)) return ADASPEC_ERR_UNSUPPORTED;
     if (q && (d.q_row_stride < q_width || d.q_out_row_stride < q_width)) return ADASPEC_ERR_DIM;
     if (append && (d.k_row_stride < kv_width || d.v_row_stride < kv_width)) return ADASPEC_ERR_DIM;

@@ -123,6 +123,23 @@ def test_append(shape, heads, dtype, pkg):  # noqa: F811
     assert torch.equal(kp, kp2) and torch.equal(vp, vp2)
 
 
+@pytest.mark.parametrize("bits", [16, 8])
+def test_the_most_query_heads_per_kv_head(bits, pkg):  # noqa: F811
+    """As many units per workgroup as there may be: 255 query heads of 256 channels, two kv heads, one pair turned."""
+    import torch
+    ctx, spec, hkv, d = [40, 16], [31, 15], 2, 256
+    q = torch.randn((48, 255 * hkv, d), device="cuda").half()
+    k, v = (torch.randn((48, hkv, d), device="cuda").half() for _ in range(2))
+    kind = torch.float8_e4m3fn if bits == 8 else torch.half
+    pools = [torch.zeros((4, hkv, 16, d), device="cuda").to(kind) for _ in range(2)]
+    scales = [torch.ones((4, hkv), device="cuda") for _ in range(2)] if bits == 8 else [None] * 2
+    f, bt = frequencies(2), dev(np.array([[2, 0, 1], [3, -1, -1]], np.int32))
+    out = pkg.kv_append_rope(q, k, v, dev(f), *pools, bt, ints(*ctx), ints(*spec), max_spec_len=31, k_scales=scales[0], v_scales=scales[1])
+    close(widen(host(out), "f16"), P.rope(host(q), f, ctx, spec, dtype="f16"), widen(host(q), "f16"), 2, "f16", False, 1.0)
+    if bits == 16:
+        assert torch.equal(pools[1][3].transpose(0, 1), v[32:])
+
+
 def test_far_positions_and_fast_pairs(pkg):  # noqa: F811
     """Angles of 10^9 radians: what 32 bits would make of them is noise."""
     L = (1 << 30) - 1

@@ -55,6 +55,15 @@ def test_bad_dims(kw, code):
         assert _append(_dims(**{**dict(k_row_stride=1 << 20, v_row_stride=1 << 20), **kw})) == code
 
 
+def test_too_many_heads():
+    wide = dict(head_dim=8, rot_dim=8, q_row_stride=1 << 20, q_out_row_stride=1 << 20, k_row_stride=1 << 20, v_row_stride=1 << 20)
+    assert _rope(_dims(n_q_heads=65536, **wide)) == -6
+    for scales in (False, True):
+        assert _append(_dims(n_q_heads=65536, n_kv_heads=65536, **wide), scales=scales) == -6
+        assert _append(_dims(n_q_heads=0, n_kv_heads=65536, **wide), scales=scales, q=None, q_out=None) == -6
+        assert _append(_dims(n_q_heads=512, n_kv_heads=2, **wide), scales=scales) == -6
+
+
 @pytest.mark.parametrize("kw,code", [
     (dict(n_kv_heads=3), -2), (dict(n_kv_heads=0), -2), (dict(page_size=32), -6), (dict(page_size=0), -2), (dict(num_pages=0), -2),
     (dict(max_pages_per_req=0), -2), (dict(k_row_stride=248), -2), (dict(v_row_stride=128), -2), (dict(v_row_stride=260), -4),
