@@ -39,7 +39,21 @@ __device__ __forceinline__ uint32_t e4m3_nans(uint32_t w) { return ((w & 0x7f7f7
 
 // Softmax weights reach the matrix core as f16, 11 bits, 2^kWeightShift larger: at most 2^15, as they trail 1 by 2^kLazyLog2 at most, and
 // down to 2^-21 of the largest before bits are lost to subnormals.  Off by 2^-11 at most, where what they weigh has 4 bits.
+// They are multiplied by their value's scale before that, relative to the largest scale so far, which O is kept in units of: a factor
+// per page.  That is sound where all scales are within kScalesApart of each other: 2^-25 of a unit, what a subnormal may be off by, is
+// then at most 2^-26 of the row's largest weighted scale.  A wavefront that has met scales further apart, which it knows at the end of its
+// blocks, takes them once more with a unit for every row, the largest weight times scale that this row has seen, so that neither a page
+// that is far louder (and perhaps hidden from the row) nor one that is far quieter costs the others their bits.  (To leave the inner
+// loop at the first such page instead, its keys kept or requested again, cost the usual case 3 % and 8 %.  128 requests of 128-4096 tokens,
+// 32/8 heads: 105 us, 167 with a page a thousand times as loud in each.)
 constexpr int kWeightShift = 7;
+constexpr float kScalesApart = 64.f;
+// (Units are powers of two: what is kept in them changes exactly.)  Units of rows times this: the product of a scale and a weight up to 2^kLazyLog2 stays finite
+constexpr float kUnitShift = 0x1p-16f, kLeastUnit = 0x1p-110f, kMostUnit = 0x1p126f;
+
+__device__ __forceinline__ float power_of_two_below(float x) { return __uint_as_float(__float_as_uint(x) & 0x7f800000u); }
+// 2^kShift over a power of two
+template <int kShift> __device__ __forceinline__ float one_over(float x) { return __uint_as_float(((254u + kShift) << 23) - __float_as_uint(x)); }
 
 template <class T, int D, int RT, bool kTree, bool kDirect>
 __global__ __launch_bounds__(256, (RT == 1 ? 3 : 2)) void attn_e4m3_kernel(
@@ -64,6 +78,7 @@ __global__ __launch_bounds__(256, (RT == 1 ? 3 : 2)) void attn_e4m3_kernel(
     __shared__ __attribute__((aligned(16))) char smem[kWaves * kSlab];
     __shared__ __attribute__((aligned(16))) uint4 q_lds[kQEntries];   // Q^T operands, MFMA lane order
     __shared__ float s_m[kWaves][16], s_l[kWaves][16];
+    __shared__ float s_unit[kWaves][kRows];                         // (rows' units, where one does not do for all)
     __shared__ unsigned long long s_anc[kTree ? kRows : 1];         // ancestor mask of each row of the unit
 
     const int tid = threadIdx.x, lane = tid & 63;
@@ -71,7 +86,7 @@ __global__ __launch_bounds__(256, (RT == 1 ? 3 : 2)) void attn_e4m3_kernel(
     const int g = lane >> 4, n16 = lane & 15;
     const int G = Hq / Hkv;
     const int total_units = kDirect ? 0 : header[0] * Hkv * n_row_groups;
-    float *my_state = reinterpret_cast<float *>(smem + wv * kSlab);
+    float *my_state = reinterpret_cast<float *>(smem + wv * kSlab), *my_units = &s_unit[wv][n16];
 
     // Row m of a tile of K is token (m >> 2) + 4 (m & 3) of its page: lane (g, n) then holds scores of tokens g, g + 4, g + 8, g + 12, and of V
     // it takes the same, D / 16 channels from (D / 16) n on.  (Four neighbouring rows of V per load.)
@@ -191,7 +206,10 @@ __global__ __launch_bounds__(256, (RT == 1 ? 3 : 2)) void attn_e4m3_kernel(
         if constexpr (kTree) { if (tid < kRows) s_anc[tid] = av; }
         lds_barrier();
 
-        float m[RT], lsum[RT], vref = 0.f, vref_inv = 0.f;         // O is kept in units of vref 2^-kWeightShift
+        float m[RT], lsum[RT];
+        float vref = kLeastUnit / kUnitShift, vref_inv = one_over<kWeightShift>(vref);    // O is kept in units of vref 2^-kWeightShift
+        float least_scale = kMostUnit;                              // of all so far
+        bool wide = false;                                          // again, with a unit for every row
         f32x4 o[RT][kTiles];
 #pragma unroll
         for (int nt = 0; nt < RT; ++nt) {
@@ -204,9 +222,11 @@ __global__ __launch_bounds__(256, (RT == 1 ? 3 : 2)) void attn_e4m3_kernel(
         // One block.  kInner: every row sees all of it, and another one follows, whose K and V are requested as soon as their
         // registers are free (without a branch around the loads, so that the compiler's waits count exactly).
         // kNT: its row tiles that have rows, where that is known, else RT.
-        auto block = [&](int bi, auto inner_tag, auto tiles_tag) {
+        // kWide: O in units of every row's own, 2^-kWeightShift / kUnitShift of it.
+        auto block = [&](int bi, auto inner_tag, auto tiles_tag, auto wide_tag) {
             constexpr bool kInner = decltype(inner_tag)::value;
             constexpr int kNT = decltype(tiles_tag)::value;
+            constexpr bool kWide = decltype(wide_tag)::value;
             constexpr int kE = 4 * kPages;                          // scores per lane and row tile
             const int tb = u.t0 + bi * kTokens;
             int64_t nb[kPages];
@@ -243,21 +263,28 @@ __global__ __launch_bounds__(256, (RT == 1 ? 3 : 2)) void attn_e4m3_kernel(
 
             // ---- online softmax (per lane: row n16 of each row tile, kE of the tokens), in log2 units ----
             uint32_t seen[kNT];                                      // masked: bit e = the row sees token e
-            // (the values' scales relative to the largest so far, which O is kept in units of)
-            float most_vs = vs[0], weight[kPages];
+            float weight[kPages];
+            if constexpr (!kWide) {
+                // the values' scales relative to the largest so far, which O is kept in units of
+                float most_vs = vs[0];
+                least_scale = fminf(least_scale, vs[0]);
 #pragma unroll
-            for (int mt = 1; mt < kPages; ++mt) most_vs = fmaxf(most_vs, vs[mt]);
-            if (__builtin_expect(most_vs > vref, 0)) {
-                const float down = vref / most_vs;
-                vref = most_vs;
-                vref_inv = (1 << kWeightShift) / most_vs;
+                for (int mt = 1; mt < kPages; ++mt) {
+                    most_vs = fmaxf(most_vs, vs[mt]);
+                    least_scale = fminf(least_scale, vs[mt]);
+                }
+                if (__builtin_expect(most_vs > vref, 0)) {
+                    const float up = __uint_as_float((__float_as_uint(most_vs) + 0x7fffffu) & 0x7f800000u), down = vref * one_over<0>(up);
+                    vref = up;
+                    vref_inv = one_over<kWeightShift>(up);
 #pragma unroll
-                for (int nt = 0; nt < kNT; ++nt)
+                    for (int nt = 0; nt < kNT; ++nt)
 #pragma unroll
-                    for (int t = 0; t < kTiles; ++t) o[nt][t] *= down;
+                        for (int t = 0; t < kTiles; ++t) o[nt][t] *= down;
+                }
             }
 #pragma unroll
-            for (int mt = 0; mt < kPages; ++mt) weight[mt] = vs[mt] * vref_inv;
+            for (int mt = 0; mt < kPages; ++mt) weight[mt] = vs[mt] * (kWide ? kUnitShift : vref_inv);
 #pragma unroll
             for (int nt = 0; nt < kNT; ++nt) {
                 if ((!kInner || kCount) && nt > 0 && nt >= tiles) break;
@@ -288,8 +315,12 @@ __global__ __launch_bounds__(256, (RT == 1 ? 3 : 2)) void attn_e4m3_kernel(
                     const float alpha = __builtin_amdgcn_exp2f(m[nt] - m_new);
                     m[nt] = m_new;
                     lsum[nt] *= alpha;
+                    if constexpr (kWide) {
+                        my_units[16 * nt] *= alpha;
+                    } else {
 #pragma unroll
-                    for (int t = 0; t < kTiles; ++t) o[nt][t] *= alpha;
+                        for (int t = 0; t < kTiles; ++t) o[nt][t] *= alpha;
+                    }
                 }
                 float psum = 0.f;
 #pragma unroll
@@ -301,6 +332,30 @@ __global__ __launch_bounds__(256, (RT == 1 ? 3 : 2)) void attn_e4m3_kernel(
                     if (masked) p[nt][e] = (seen[nt] >> e) & 1 ? p[nt][e] : 0.f;
                 }
                 lsum[nt] += psum;
+            }
+            if constexpr (kWide) {
+                // every row's unit follows the largest weight times scale that it has seen, as m the largest score
+#pragma unroll
+                for (int nt = 0; nt < kNT; ++nt) {
+                    if (nt > 0 && nt >= tiles) break;
+                    if constexpr (RT > 2) __builtin_amdgcn_sched_barrier(0);
+                    float most = p[nt][0];
+#pragma unroll
+                    for (int e = 1; e < kE; ++e) most = fmaxf(most, p[nt][e]);
+                    most = max_over_row_groups(most);
+                    const float was = my_units[16 * nt];
+                    const bool move = was != power_of_two_below(was) || was < kLeastUnit || most > was * (float)(1 << (int)kLazyLog2);
+                    const float to = move ? power_of_two_below(fmaxf(fmaxf(most, was), kLeastUnit)) : was;
+                    if (__builtin_amdgcn_ballot_w64(move) != 0) {
+                        const float ratio = was * one_over<0>(to);
+#pragma unroll
+                        for (int t = 0; t < kTiles; ++t) o[nt][t] *= ratio;
+                        my_units[16 * nt] = to;
+                    }
+                    const float inv = one_over<kWeightShift>(to);
+#pragma unroll
+                    for (int e = 0; e < kE; ++e) p[nt][e] *= inv;
+                }
             }
 
             // ---- no value behind the request's end, and NaN values only in rows that see them ----
@@ -397,7 +452,7 @@ __global__ __launch_bounds__(256, (RT == 1 ? 3 : 2)) void attn_e4m3_kernel(
             const int full = max(min(first_masked, u.t1) - u.t0, 0) / kTokens;         // blocks that every row sees all of
             int bi = wv;
             auto inner = [&](auto tiles_tag) {
-                for (; bi + kWaves < u.nblk && bi < full; bi += kWaves) block(bi, std::true_type{}, tiles_tag);
+                for (; bi + kWaves < u.nblk && bi < full; bi += kWaves) block(bi, std::true_type{}, tiles_tag, std::false_type{});
             };
             // (A copy of the loop for every number of tiles; with four of them they crowd the instruction cache: 128 requests of 128-4096
             // tokens, trees of up to 13 nodes, 32/8 heads: 152 us with one copy, whose tiles are counted at run time, 168 with four.
@@ -406,7 +461,19 @@ __global__ __launch_bounds__(256, (RT == 1 ? 3 : 2)) void attn_e4m3_kernel(
             else if (RT == 1 || tiles <= 1) inner(std::integral_constant<int, 1>{});
             else if (RT == 2 || tiles == 2) inner(std::integral_constant<int, RT < 2 ? 1 : 2>{});
             else inner(std::integral_constant<int, RT < 3 ? 1 : 3>{});
-            for (; bi < u.nblk; bi += kWaves) block(bi, std::false_type{}, std::integral_constant<int, RT>{});
+            for (; bi < u.nblk; bi += kWaves) block(bi, std::false_type{}, std::integral_constant<int, RT>{}, std::false_type{});
+            wide = !(least_scale * kScalesApart >= vref && vref < kMostUnit);
+            if (__builtin_expect(wide, 0)) {
+                first_loads(u);
+#pragma unroll
+                for (int nt = 0; nt < RT; ++nt) {
+                    m[nt] = kLowestRef; lsum[nt] = 0.f;
+                    my_units[16 * nt] = kLeastUnit;
+#pragma unroll
+                    for (int t = 0; t < kTiles; ++t) o[nt][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+                }
+                for (bi = wv; bi < u.nblk; bi += kWaves) block(bi, std::false_type{}, std::integral_constant<int, RT>{}, std::true_type{});
+            }
         }
 
         // ---- next unit: its first block and its Q rows travel while this unit's states are merged
@@ -416,11 +483,11 @@ __global__ __launch_bounds__(256, (RT == 1 ? 3 : 2)) void attn_e4m3_kernel(
             first_loads(nxt);
         }
         // ---- merge the four wavefronts' states through LDS (as in attn_mfma.hip), one row tile after the other ----------
-        const float o_unit = vref * (1.f / (1 << kWeightShift));
 #pragma unroll
         for (int nt = 0; nt < RT; ++nt) {
             if (nt > 0 && nt >= tiles) break;
             if (nt > 0) lds_barrier();                              // (the tile before has been read)
+            const float o_unit = (wide ? my_units[16 * nt] * (1.f / kUnitShift) : vref) * (1.f / (1 << kWeightShift));
             lsum[nt] += __shfl_xor(lsum[nt], 16, kWave);
             lsum[nt] += __shfl_xor(lsum[nt], 32, kWave);
             if (g == 0) { s_m[wv][n16] = m[nt]; s_l[wv][n16] = lsum[nt]; }

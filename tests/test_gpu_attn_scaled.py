@@ -147,6 +147,36 @@ def test_large_scores_and_scales(dtype, pkg):  # noqa: F811
         assert np.abs(out - ref).max() <= 4e-3 * 2.0 ** 40 * 5
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("is_tree", [False, True], ids=["chain", "tree"])
+@pytest.mark.parametrize("apart", [4, 9, 20, 60, -30])
+def test_pages_of_very_different_scales(apart, is_tree, d, pkg):  # noqa: F811
+    """Single pages 2^apart as loud as the others, whose weights are as much smaller, or the square of that, or hidden from most rows.
+
+    Tolerance, relative to the mean of the values' magnitudes under the exact weights: 2^-11 for the f16 weights (as above); fp32 scores of up to
+    `most` in magnitude are sums of d products and two factors, off by (d + 2) 2^-24 of it, weights and their sum by that much each; TOL for
+    the rest.  What is lost to f16 subnormals: 2^-26 of the row's largest weighted scale per token."""
+    ctx, spec = [593, 900, 2100, 33], [6, 5, 3, 1]          # (593, 33: the last token is alone in its page, and hidden from the other rows)
+    for square in (1, 2):
+        c = make(40 + square, ctx, spec, 8, 2, d, "bf16", is_tree)
+        c["q"] = store(np.abs(widen(c["q"], "bf16")), "bf16")
+        for i, L in enumerate(ctx):
+            loud = {L // 64, (L - 1) // 16 - 9, (L - 1) // 16} if L > 200 else {(L - 1) // 16}
+            for p in loud:
+                page = c["bt"][i, p]
+                c["vs"][page] *= np.float32(2.0 ** apart)
+                if p < (L - 1) // 16:                       # scores of about -apart * square, in log2, everywhere in it
+                    c["k8"][page] = P.to_e4m3(np.array([-256.0]))[0]
+                    c["ks"][page] = max(apart, 0) * square * np.log(2.0) / (0.8 * np.sqrt(d)) / 256.0
+        ref, size = oracle(c)
+        k = P.E4M3[c["k8"]] * c["ks"][..., None, None].astype(np.float64)
+        longest = np.sqrt(np.nanmax((np.nan_to_num(k) ** 2).sum(-1)) * (widen(c["q"], "bf16") ** 2).sum(-1).max()) / np.sqrt(d)
+        tol = (TOL + 2.0 ** -11 + 2 * (d + 2) * 2.0 ** -24 * longest) * size + 2.0 ** -26 * max(ctx) * size.max(axis=-1, keepdims=True)
+        for path in ("auto", "vector"):
+            off = np.abs(host(call(pkg, c, out_dtype=0, path=path)).astype(np.float64) - ref)
+            assert (off <= tol).all(), (square, path, (off / size).max())
+
+
 def test_plans_graphs_streams_and_threads(pkg):  # noqa: F811
     import threading
     import torch
