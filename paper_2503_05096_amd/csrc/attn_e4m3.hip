@@ -14,7 +14,9 @@
 //     out).  The lane then holds D / 16 whole operand columns: tile t of O^T has channel (D / 16) m + t in row m.
 // A block is 32 tokens of 128 channels or 64 of 64: 8 KB of K and V per wavefront, 32 registers.
 //
-// Bound: HBM.
+// Bound: HBM where requests are many and rows few: 128 requests of 128-4096 tokens, 32/8 heads of 128, 562 MB in 95-98 us of the kernel, 5.8
+// TB/s; 64 of 8192-32768, 64/8 heads, 2.7 GB in 474-489 us, 5.6 TB/s (one row tile 435: up to 6.3).  The vector ALU where they are many: a score costs
+// about 10 instructions whatever it weighs, and with four row tiles (trees of 13 nodes, G = 4) there are 64 of them per token.
 #include <type_traits>
 
 #include "adaspec_internal.h"
@@ -48,7 +50,8 @@ __device__ __forceinline__ uint32_t e4m3_nans(uint32_t w) { return ((w & 0x7f7f7
 // 32/8 heads: 105 us, 167 with a page a thousand times as loud in each.)
 constexpr int kWeightShift = 7;
 constexpr float kScalesApart = 64.f;
-// (Units are powers of two: what is kept in them changes exactly.)  Units of rows times this: the product of a scale and a weight up to 2^kLazyLog2 stays finite
+// (Units are powers of two: what is kept in them changes exactly.)  Units of rows times kUnitShift: the product of a scale and a weight up to
+// 2^kLazyLog2 stays finite.
 constexpr float kUnitShift = 0x1p-16f, kLeastUnit = 0x1p-110f, kMostUnit = 0x1p126f;
 
 __device__ __forceinline__ float power_of_two_below(float x) { return __uint_as_float(__float_as_uint(x) & 0x7f800000u); }
@@ -228,133 +231,263 @@ __global__ __launch_bounds__(256, (RT == 1 ? 3 : 2)) void attn_e4m3_kernel(
             constexpr int kNT = decltype(tiles_tag)::value;
             constexpr bool kWide = decltype(wide_tag)::value;
             constexpr int kE = 4 * kPages;                          // scores per lane and row tile
+            constexpr bool kByTile = D == 64;
             const int tb = u.t0 + bi * kTokens;
             int64_t nb[kPages];
             const bool next = kInner || bi + kWaves < u.nblk;
             const bool masked = !kInner && (tb + kTokens > first_masked || tb + kTokens > u.t1);
             if (next) page_blocks(u, bi + kWaves, nb);
 
-            // ---- S^T = K Q^T ------------------------------------------------------------
-            float p[kNT][kE];
+            // Two orders of the same work.  head_dim 64: row tile by row tile, with all keys in Q's type (32 registers) and P packed at once, so
+            // that Q is read once per block, not once per page, and the scores of one tile are live, not of all: 64 requests of 256-4096
+            // tokens, trees of up to 13 nodes, 32/8 heads: 52.6 us against 60.9.  head_dim 128, whose O leaves no registers for that: page by
+            // page (the other way costs 64 requests of 8192-32768 tokens, 64/8 heads, 520 us against 495, trees of up to 13 nodes 168 against 155).
+            float p[kByTile ? 1 : kNT][kE];
+            uint4 packed[kByTile ? kNT : 1][kHalves];               // P as an operand
+            uint32_t seen[kNT];                                     // masked: bit e = the row sees token e
+            if constexpr (kByTile) {
+                // ---- S^T = K Q^T, row tile by row tile: the keys once in Q's type, P packed as soon as it is known -------
+                uint4 kop[kPages][kSteps];
 #pragma unroll
-            for (int mt = 0; mt < kPages; ++mt) {
-                uint4 kop[kSteps];
+                for (int mt = 0; mt < kPages; ++mt)
 #pragma unroll
-                for (int s = 0; s < kSteps; ++s) {
-                    const uint4 raw = kreg[mt][s >> 1];
-                    kop[s] = (s & 1) ? e4m3_operand<T>(raw.z, raw.w) : e4m3_operand<T>(raw.x, raw.y);
+                    for (int s = 0; s < kSteps; ++s) {
+                        const uint4 raw = kreg[mt][s >> 1];
+                        kop[mt][s] = (s & 1) ? e4m3_operand<T>(raw.z, raw.w) : e4m3_operand<T>(raw.x, raw.y);
+                    }
+                float factor[kPages];
+#pragma unroll
+                for (int mt = 0; mt < kPages; ++mt) factor[mt] = ks[mt] * scale_log2;
+                __builtin_amdgcn_sched_barrier(0);
+                if (next) load_k(nb);
+                __builtin_amdgcn_sched_barrier(0);
+                float weight[kPages];
+                if constexpr (!kWide) {
+                    // the values' scales relative to the largest so far, which O is kept in units of
+                    float most_vs = vs[0];
+                    least_scale = fminf(least_scale, vs[0]);
+#pragma unroll
+                    for (int mt = 1; mt < kPages; ++mt) {
+                        most_vs = fmaxf(most_vs, vs[mt]);
+                        least_scale = fminf(least_scale, vs[mt]);
+                    }
+                    if (__builtin_expect(most_vs > vref, 0)) {
+                        const float up = __uint_as_float((__float_as_uint(most_vs) + 0x7fffffu) & 0x7f800000u), down = vref * one_over<0>(up);
+                        vref = up;
+                        vref_inv = one_over<kWeightShift>(up);
+#pragma unroll
+                        for (int nt = 0; nt < kNT; ++nt)
+#pragma unroll
+                            for (int t = 0; t < kTiles; ++t) o[nt][t] *= down;
+                    }
                 }
-                const float factor = ks[mt] * scale_log2;
-                if constexpr (RT > 2) __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int mt = 0; mt < kPages; ++mt) weight[mt] = vs[mt] * (kWide ? kUnitShift : vref_inv);
+
+                auto weigh = [&](int nt, float (&x)[kE]) {
+                    // ---- online softmax (per lane: row n16 of the tile, kE of the tokens), in log2 units
+                    if (masked) {
+                        seen[nt] = 0;
+                        const unsigned long long am = kTree ? s_anc[16 * nt + n16] : 0ull;
+                        const int row = u.r0 + 16 * nt + n16, base = u.L - u.n;
+                        const int pos = row < u.rows ? base + row / G : -1, lim = min(pos, u.t1 - 1);
+#pragma unroll
+                        for (int e = 0; e < kE; ++e) {
+                            const int t = tb + 16 * (e >> 2) + g + 4 * (e & 3), rel = t - base;
+                            bool vis;
+                            if constexpr (kTree) vis = t < u.t1 && (rel < 0 ? pos >= 0 : ((am >> (rel & 63)) & 1ull) != 0);
+                            else vis = t <= lim;
+                            x[e] = vis ? x[e] : -INFINITY;
+                            seen[nt] |= vis ? 1u << e : 0u;
+                        }
+                    }
+                    float mx = x[0];
+#pragma unroll
+                    for (int e = 1; e < kE; ++e) mx = fmaxf(mx, x[e]);
+                    mx = max_over_row_groups(mx);
+                    // lazy reference: moves only when the block's maximum exceeds it by more than kLazyLog2
+                    const bool grow = mx > m[nt] + kLazyLog2;
+                    if (__builtin_expect(__builtin_amdgcn_ballot_w64(grow) != 0, 0)) {
+                        const float m_new = grow ? mx : m[nt];
+                        const float alpha = __builtin_amdgcn_exp2f(m[nt] - m_new);
+                        m[nt] = m_new;
+                        lsum[nt] *= alpha;
+                        if constexpr (kWide) {
+                            my_units[16 * nt] *= alpha;
+                        } else {
+#pragma unroll
+                            for (int t = 0; t < kTiles; ++t) o[nt][t] *= alpha;
+                        }
+                    }
+                    float psum = 0.f;
+#pragma unroll
+                    for (int e = 0; e < kE; ++e) {
+                        x[e] = __builtin_amdgcn_exp2f(x[e] - m[nt]);
+                        psum += x[e];
+                        x[e] *= weight[e >> 2];
+                        // what hidden tokens hold stays out: no weight, whatever their scale
+                        if (masked) x[e] = (seen[nt] >> e) & 1 ? x[e] : 0.f;
+                    }
+                    lsum[nt] += psum;
+                    if constexpr (kWide) {
+                        // the row's unit follows the largest weight times scale that it has seen, as m the largest score
+                        float most = x[0];
+#pragma unroll
+                        for (int e = 1; e < kE; ++e) most = fmaxf(most, x[e]);
+                        most = max_over_row_groups(most);
+                        const float was = my_units[16 * nt];
+                        const bool move = was != power_of_two_below(was) || was < kLeastUnit || most > was * (float)(1 << (int)kLazyLog2);
+                        const float to = move ? power_of_two_below(fmaxf(fmaxf(most, was), kLeastUnit)) : was;
+                        if (__builtin_amdgcn_ballot_w64(move) != 0) {
+                            const float ratio = was * one_over<0>(to);
+#pragma unroll
+                            for (int t = 0; t < kTiles; ++t) o[nt][t] *= ratio;
+                            my_units[16 * nt] = to;
+                        }
+                        const float inv = one_over<kWeightShift>(to);
+#pragma unroll
+                        for (int e = 0; e < kE; ++e) x[e] *= inv;
+                    }
+#pragma unroll
+                    for (int hf = 0; hf < kHalves; ++hf)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) (&packed[nt][hf].x)[j] = Mma<F16>::pack2(x[8 * hf + 2 * j], x[8 * hf + 2 * j + 1]);
+                };
 #pragma unroll
                 for (int nt = 0; nt < kNT; ++nt) {
                     if ((!kInner || kCount) && nt > 0 && nt >= tiles) break;
-                    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+                    f32x4 acc[kPages];
 #pragma unroll
-                    for (int s = 0; s < kSteps; ++s) acc = Mma<T>::run(kop[s], q_lds[(nt * kSteps + s) * 64 + lane], acc);
+                    for (int s = 0; s < kSteps; ++s) {
+                        const uint4 qop = q_lds[(nt * kSteps + s) * 64 + lane];
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) p[nt][4 * mt + r] = acc[r] * factor;
-                    if constexpr (RT > 3) __builtin_amdgcn_sched_barrier(0);
+                        for (int mt = 0; mt < kPages; ++mt) acc[mt] = Mma<T>::run(kop[mt][s], qop, s == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : acc[mt]);
+                    }
+#pragma unroll
+                    for (int e = 0; e < kE; ++e) p[0][e] = acc[e >> 2][e & 3] * factor[e >> 2];
+                    weigh(nt, p[0]);
                 }
-            }
-            __builtin_amdgcn_sched_barrier(0);
-            if (next) load_k(nb);
-            __builtin_amdgcn_sched_barrier(0);
+            } else {
+                // ---- S^T = K Q^T ------------------------------------------------------------
+#pragma unroll
+                for (int mt = 0; mt < kPages; ++mt) {
+                    uint4 kop[kSteps];
+#pragma unroll
+                    for (int s = 0; s < kSteps; ++s) {
+                        const uint4 raw = kreg[mt][s >> 1];
+                        kop[s] = (s & 1) ? e4m3_operand<T>(raw.z, raw.w) : e4m3_operand<T>(raw.x, raw.y);
+                    }
+                    const float factor = ks[mt] * scale_log2;
+                    if constexpr (RT > 2) __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int nt = 0; nt < kNT; ++nt) {
+                        if ((!kInner || kCount) && nt > 0 && nt >= tiles) break;
+                        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                        for (int s = 0; s < kSteps; ++s) acc = Mma<T>::run(kop[s], q_lds[(nt * kSteps + s) * 64 + lane], acc);
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) p[nt][4 * mt + r] = acc[r] * factor;
+                        if constexpr (RT > 3) __builtin_amdgcn_sched_barrier(0);
+                    }
+                }
+                __builtin_amdgcn_sched_barrier(0);
+                if (next) load_k(nb);
+                __builtin_amdgcn_sched_barrier(0);
 
-            // ---- online softmax (per lane: row n16 of each row tile, kE of the tokens), in log2 units ----
-            uint32_t seen[kNT];                                      // masked: bit e = the row sees token e
-            float weight[kPages];
-            if constexpr (!kWide) {
-                // the values' scales relative to the largest so far, which O is kept in units of
-                float most_vs = vs[0];
-                least_scale = fminf(least_scale, vs[0]);
+                // ---- online softmax (per lane: row n16 of each row tile, kE of the tokens), in log2 units ----
+                float weight[kPages];
+                if constexpr (!kWide) {
+                    // the values' scales relative to the largest so far, which O is kept in units of
+                    float most_vs = vs[0];
+                    least_scale = fminf(least_scale, vs[0]);
 #pragma unroll
-                for (int mt = 1; mt < kPages; ++mt) {
-                    most_vs = fmaxf(most_vs, vs[mt]);
-                    least_scale = fminf(least_scale, vs[mt]);
-                }
-                if (__builtin_expect(most_vs > vref, 0)) {
-                    const float up = __uint_as_float((__float_as_uint(most_vs) + 0x7fffffu) & 0x7f800000u), down = vref * one_over<0>(up);
-                    vref = up;
-                    vref_inv = one_over<kWeightShift>(up);
+                    for (int mt = 1; mt < kPages; ++mt) {
+                        most_vs = fmaxf(most_vs, vs[mt]);
+                        least_scale = fminf(least_scale, vs[mt]);
+                    }
+                    if (__builtin_expect(most_vs > vref, 0)) {
+                        const float up = __uint_as_float((__float_as_uint(most_vs) + 0x7fffffu) & 0x7f800000u), down = vref * one_over<0>(up);
+                        vref = up;
+                        vref_inv = one_over<kWeightShift>(up);
 #pragma unroll
-                    for (int nt = 0; nt < kNT; ++nt)
+                        for (int nt = 0; nt < kNT; ++nt)
 #pragma unroll
-                        for (int t = 0; t < kTiles; ++t) o[nt][t] *= down;
-                }
-            }
-#pragma unroll
-            for (int mt = 0; mt < kPages; ++mt) weight[mt] = vs[mt] * (kWide ? kUnitShift : vref_inv);
-#pragma unroll
-            for (int nt = 0; nt < kNT; ++nt) {
-                if ((!kInner || kCount) && nt > 0 && nt >= tiles) break;
-                if (masked) {
-                    seen[nt] = 0;
-                    const unsigned long long am = kTree ? s_anc[16 * nt + n16] : 0ull;
-                    const int row = u.r0 + 16 * nt + n16, base = u.L - u.n;
-                    const int pos = row < u.rows ? base + row / G : -1, lim = min(pos, u.t1 - 1);
-#pragma unroll
-                    for (int e = 0; e < kE; ++e) {
-                        const int t = tb + 16 * (e >> 2) + g + 4 * (e & 3), rel = t - base;
-                        bool vis;
-                        if constexpr (kTree) vis = t < u.t1 && (rel < 0 ? pos >= 0 : ((am >> (rel & 63)) & 1ull) != 0);
-                        else vis = t <= lim;
-                        p[nt][e] = vis ? p[nt][e] : -INFINITY;
-                        seen[nt] |= vis ? 1u << e : 0u;
+                            for (int t = 0; t < kTiles; ++t) o[nt][t] *= down;
                     }
                 }
-                if constexpr (RT > 2) __builtin_amdgcn_sched_barrier(0);
-                float mx = p[nt][0];
 #pragma unroll
-                for (int e = 1; e < kE; ++e) mx = fmaxf(mx, p[nt][e]);
-                mx = max_over_row_groups(mx);
-                // lazy reference: moves only when the block's maximum exceeds it by more than kLazyLog2
-                const bool grow = mx > m[nt] + kLazyLog2;
-                if (__builtin_expect(__builtin_amdgcn_ballot_w64(grow) != 0, 0)) {
-                    const float m_new = grow ? mx : m[nt];
-                    const float alpha = __builtin_amdgcn_exp2f(m[nt] - m_new);
-                    m[nt] = m_new;
-                    lsum[nt] *= alpha;
-                    if constexpr (kWide) {
-                        my_units[16 * nt] *= alpha;
-                    } else {
-#pragma unroll
-                        for (int t = 0; t < kTiles; ++t) o[nt][t] *= alpha;
-                    }
-                }
-                float psum = 0.f;
-#pragma unroll
-                for (int e = 0; e < kE; ++e) {
-                    p[nt][e] = __builtin_amdgcn_exp2f(p[nt][e] - m[nt]);
-                    psum += p[nt][e];
-                    p[nt][e] *= weight[e >> 2];
-                    // what hidden tokens hold stays out: no weight, whatever their scale
-                    if (masked) p[nt][e] = (seen[nt] >> e) & 1 ? p[nt][e] : 0.f;
-                }
-                lsum[nt] += psum;
-            }
-            if constexpr (kWide) {
-                // every row's unit follows the largest weight times scale that it has seen, as m the largest score
+                for (int mt = 0; mt < kPages; ++mt) weight[mt] = vs[mt] * (kWide ? kUnitShift : vref_inv);
 #pragma unroll
                 for (int nt = 0; nt < kNT; ++nt) {
-                    if (nt > 0 && nt >= tiles) break;
-                    if constexpr (RT > 2) __builtin_amdgcn_sched_barrier(0);
-                    float most = p[nt][0];
+                    if ((!kInner || kCount) && nt > 0 && nt >= tiles) break;
+                    if (masked) {
+                        seen[nt] = 0;
+                        const unsigned long long am = kTree ? s_anc[16 * nt + n16] : 0ull;
+                        const int row = u.r0 + 16 * nt + n16, base = u.L - u.n;
+                        const int pos = row < u.rows ? base + row / G : -1, lim = min(pos, u.t1 - 1);
 #pragma unroll
-                    for (int e = 1; e < kE; ++e) most = fmaxf(most, p[nt][e]);
-                    most = max_over_row_groups(most);
-                    const float was = my_units[16 * nt];
-                    const bool move = was != power_of_two_below(was) || was < kLeastUnit || most > was * (float)(1 << (int)kLazyLog2);
-                    const float to = move ? power_of_two_below(fmaxf(fmaxf(most, was), kLeastUnit)) : was;
-                    if (__builtin_amdgcn_ballot_w64(move) != 0) {
-                        const float ratio = was * one_over<0>(to);
-#pragma unroll
-                        for (int t = 0; t < kTiles; ++t) o[nt][t] *= ratio;
-                        my_units[16 * nt] = to;
+                        for (int e = 0; e < kE; ++e) {
+                            const int t = tb + 16 * (e >> 2) + g + 4 * (e & 3), rel = t - base;
+                            bool vis;
+                            if constexpr (kTree) vis = t < u.t1 && (rel < 0 ? pos >= 0 : ((am >> (rel & 63)) & 1ull) != 0);
+                            else vis = t <= lim;
+                            p[nt][e] = vis ? p[nt][e] : -INFINITY;
+                            seen[nt] |= vis ? 1u << e : 0u;
+                        }
                     }
-                    const float inv = one_over<kWeightShift>(to);
+                    if constexpr (RT > 2) __builtin_amdgcn_sched_barrier(0);
+                    float mx = p[nt][0];
 #pragma unroll
-                    for (int e = 0; e < kE; ++e) p[nt][e] *= inv;
+                    for (int e = 1; e < kE; ++e) mx = fmaxf(mx, p[nt][e]);
+                    mx = max_over_row_groups(mx);
+                    // lazy reference: moves only when the block's maximum exceeds it by more than kLazyLog2
+                    const bool grow = mx > m[nt] + kLazyLog2;
+                    if (__builtin_expect(__builtin_amdgcn_ballot_w64(grow) != 0, 0)) {
+                        const float m_new = grow ? mx : m[nt];
+                        const float alpha = __builtin_amdgcn_exp2f(m[nt] - m_new);
+                        m[nt] = m_new;
+                        lsum[nt] *= alpha;
+                        if constexpr (kWide) {
+                            my_units[16 * nt] *= alpha;
+                        } else {
+#pragma unroll
+                            for (int t = 0; t < kTiles; ++t) o[nt][t] *= alpha;
+                        }
+                    }
+                    float psum = 0.f;
+#pragma unroll
+                    for (int e = 0; e < kE; ++e) {
+                        p[nt][e] = __builtin_amdgcn_exp2f(p[nt][e] - m[nt]);
+                        psum += p[nt][e];
+                        p[nt][e] *= weight[e >> 2];
+                        // what hidden tokens hold stays out: no weight, whatever their scale
+                        if (masked) p[nt][e] = (seen[nt] >> e) & 1 ? p[nt][e] : 0.f;
+                    }
+                    lsum[nt] += psum;
+                }
+                if constexpr (kWide) {
+                    // every row's unit follows the largest weight times scale that it has seen, as m the largest score
+#pragma unroll
+                    for (int nt = 0; nt < kNT; ++nt) {
+                        if (nt > 0 && nt >= tiles) break;
+                        if constexpr (RT > 2) __builtin_amdgcn_sched_barrier(0);
+                        float most = p[nt][0];
+#pragma unroll
+                        for (int e = 1; e < kE; ++e) most = fmaxf(most, p[nt][e]);
+                        most = max_over_row_groups(most);
+                        const float was = my_units[16 * nt];
+                        const bool move = was != power_of_two_below(was) || was < kLeastUnit || most > was * (float)(1 << (int)kLazyLog2);
+                        const float to = move ? power_of_two_below(fmaxf(fmaxf(most, was), kLeastUnit)) : was;
+                        if (__builtin_amdgcn_ballot_w64(move) != 0) {
+                            const float ratio = was * one_over<0>(to);
+#pragma unroll
+                            for (int t = 0; t < kTiles; ++t) o[nt][t] *= ratio;
+                            my_units[16 * nt] = to;
+                        }
+                        const float inv = one_over<kWeightShift>(to);
+#pragma unroll
+                        for (int e = 0; e < kE; ++e) p[nt][e] *= inv;
+                    }
                 }
             }
 
@@ -416,7 +549,10 @@ __global__ __launch_bounds__(256, (RT == 1 ? 3 : 2)) void attn_e4m3_kernel(
                 for (int nt = 0; nt < kNT; ++nt) {
                     if ((!kInner || kCount) && nt > 0 && nt >= tiles) break;
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) (&pop[nt].x)[j] = Mma<F16>::pack2(p[nt][8 * hf + 2 * j], p[nt][8 * hf + 2 * j + 1]);
+                    for (int j = 0; j < 4; ++j) {
+                        if constexpr (kByTile) (&pop[nt].x)[j] = (&packed[nt][hf].x)[j];
+                        else (&pop[nt].x)[j] = Mma<F16>::pack2(p[nt][8 * hf + 2 * j], p[nt][8 * hf + 2 * j + 1]);
+                    }
                 }
 #pragma unroll
                 for (int w = 0; w < kWords; ++w)
