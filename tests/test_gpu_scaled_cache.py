@@ -122,6 +122,34 @@ def test_scales_at_their_borders(dtype, pkg):  # noqa: F811
             assert np.array_equal(P.E4M3[got], P.E4M3[want], equal_nan=True)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("bad", [np.inf, -np.inf, np.nan])
+def test_the_largest_entry_beside_one_that_is_not_finite(bad, dtype, pkg):  # noqa: F811
+    """It counts, wherever the two are: a value's neighbours, a key's entries that are not turned."""
+    import torch
+    d = 64
+    rows = []
+    for at in range(24):
+        row = np.full(d, 0.5)
+        row[16 + at], row[16 + at + (1 if at % 2 else -1)] = bad, 96.0
+        rows.append(row)
+    with np.errstate(over="ignore"):
+        x = store(np.array(rows)[:, None, :], dtype)
+    n = len(rows)
+    ctx, spec, bt = [1] * n, [0] * n, np.arange(n, dtype=np.int32)[:, None]
+    k8, ks = np.zeros((n, 1, 16, d), np.uint8), np.ones((n, 1), np.float32)
+    for f, inter in ((None, False), (frequencies(16), False), (frequencies(16), True)):
+        dk, dv, dks, dvs = dev(k8, "e4m3"), dev(k8, "e4m3"), dev(ks), dev(ks)
+        pkg.kv_append_rope(None, dev(x, dtype), dev(x, dtype), None if f is None else dev(f), dk, dv, dev(bt), ints(*ctx), ints(*spec), max_spec_len=0,
+                           k_scales=dks, v_scales=dvs, interleaved=inter)
+        torch.cuda.synchronize()
+        with np.errstate(invalid="ignore"):
+            wk, wv, wks, wvs = P.append_scaled(x, x, f, k8, k8, ks, ks, bt, ctx, spec, dtype=dtype, interleaved=inter)
+        assert (wvs == 0.25).all() and np.array_equal(host(dks), wks.astype(np.float32)) and np.array_equal(host(dvs), wvs.astype(np.float32))
+        for got, want in ((host(dk, "e4m3"), wk), (host(dv, "e4m3"), wv)):
+            assert np.array_equal(P.E4M3[got], P.E4M3[want], equal_nan=True)
+
+
 @pytest.mark.parametrize("layers", [None, 3])
 def test_copies_of_pages(layers, pkg):  # noqa: F811
     import torch
