@@ -10,7 +10,8 @@
 // decide together) and some of the kv heads with their query heads; cosines and sines of its rows are worked out once.
 //
 // Small calls are bound by latency: two memory round trips (lengths, rows), three into a cache of 8 bits (the page's scale), with
-// the angles worked out while the rows travel.  Large ones by HBM.
+// the angles worked out while the rows travel: 128 requests of up to 7 rows, 32/8 heads of 128, 6.7 us, into 8 bits 8.9.  Large ones by
+// HBM: 16 prompts of 100-4000 rows 168 us for 806 MB, 4.8 TB/s; into 8 bits, 64/8 heads, 256 for 1276 MB, 5.0 TB/s (a large copy: 5.07).
 #include <type_traits>
 
 #include "adaspec_internal.h"
