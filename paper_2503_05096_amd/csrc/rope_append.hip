@@ -470,7 +470,8 @@ hipError_t launch_rope_append(const void *q, const void *k, const void *v, const
     // or values, 2 kv heads, or 4 without shared ones), fewer where that leaves less than two workgroups per compute unit.
     // MI355X, us, 1 / 2 / 4 / 8 kv heads of 32/8: 128 requests of up to 7 rows 6.9 / 6.3 / 7.3 / 9.8, into 8 bits 12.5 / 10.3 / 12.1 /
     // 16.7; prompts of 32000 rows 189 / 195 / 168 / 177, into 8 bits (64/8) 306 / 258 / 264 / 275; 16 trees of up to 61 rows into 8
-    // bits 12.5 / 13.7 / 16.6 / 23.7; query heads alone (1 / 2 / 4 / 8), 17400 rows of 32 86 / 56 / 50 / 51.
+    // bits 12.5 / 13.7 / 16.6 / 23.7 (8 bits: all of them when scratch memory still cost the small ones 1-4 us); query heads alone, 17400 rows
+    // of 32 86 / 56 / 50 / 51.
     const int shared = k && q ? d.n_q_heads / d.n_kv_heads : 1;
     a.heads = !k ? 4 : !fp8 ? 20 / (shared + 1) : shared > 1 ? 2 : 4;
     a.heads = a.heads < 1 ? 1 : a.heads > heads ? heads : a.heads;
