@@ -36,11 +36,22 @@ template <class T> __device__ __forceinline__ uint4 e4m3_operand(uint32_t lo, ui
 {
     return make_uint4(e4m3_pair<T, false>(lo), e4m3_pair<T, true>(lo), e4m3_pair<T, false>(hi), e4m3_pair<T, true>(hi));
 }
+// What hi, the two f16 next to a and b, leaves of them, as two f16 more: 22 bits together.
+__device__ __forceinline__ uint32_t f16_rest2(uint32_t hi, float a, float b)
+{
+    float one = 1.0f;
+    asm("" : "+s"(one));                    // (a multiply-add takes f16 as they are, the subtraction that the compiler would make of it does not)
+    const f16x2 h = __builtin_bit_cast(f16x2, hi);
+    return Mma<F16>::pack2(fmaf(a, one, -(float)h.x), fmaf(b, one, -(float)h.y));
+}
 // the bytes of w that are NaN, as 0x80
 __device__ __forceinline__ uint32_t e4m3_nans(uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
 
-// Softmax weights reach the matrix core as f16, 11 bits, 2^kWeightShift larger: at most 2^15, as they trail 1 by 2^kLazyLog2 at most, and
-// down to 2^-21 of the largest before bits are lost to subnormals.  Off by 2^-11 at most, where what they weigh has 4 bits.
+// Softmax weights reach the matrix core as two f16, the nearest one and what it leaves: 22 bits, 2^kWeightShift larger: at most 2^15, as
+// they trail 1 by 2^kLazyLog2 at most.  Off by 2^-22 of themselves, or by 2^-25 (half a subnormal) where that is more, as little as the
+// fp32 sums they go into.  The first piece alone is off by up to 2^-12 and leaves that in the output wherever weights round alike.  MI355X, output in
+// fp32 against 64 bits, relative, one piece / two: 128 requests of 128-4096 tokens, 32/8 heads of 128, 1.8e-4 / 2.7e-7 (100.9 / 101.7
+// us), 64 trees of up to 13 nodes, 256-4096, 32/8 of 64, 1.8e-4 / 3.4e-7 (52.5 / 56.8); 64 of 8192-32768, 64/8 of 128, 495 / 509 us.
 // They are multiplied by their value's scale before that, relative to the largest scale so far, which O is kept in units of: a factor
 // per page.  That is sound where all scales are within kScalesApart of each other: 2^-25 of a unit, what a subnormal may be off by, is
 // then at most 2^-26 of the row's largest weighted scale.  A wavefront that has met scales further apart, which it knows at the end of its
@@ -243,7 +254,7 @@ __global__ __launch_bounds__(256, (RT == 1 ? 3 : 2)) void attn_e4m3_kernel(
             // tokens, trees of up to 13 nodes, 32/8 heads: 52.6 us against 60.9.  head_dim 128, whose O leaves no registers for that: page by
             // page (the other way costs 64 requests of 8192-32768 tokens, 64/8 heads, 520 us against 495, trees of up to 13 nodes 168 against 155).
             float p[kByTile ? 1 : kNT][kE];
-            uint4 packed[kByTile ? kNT : 1][kHalves];               // P as an operand
+            uint4 packed[kByTile ? kNT : 1][kHalves][2];            // P as an operand, in two pieces
             uint32_t seen[kNT];                                     // masked: bit e = the row sees token e
             if constexpr (kByTile) {
                 // ---- S^T = K Q^T, row tile by row tile: the keys once in Q's type, P packed as soon as it is known -------
@@ -351,7 +362,12 @@ __global__ __launch_bounds__(256, (RT == 1 ? 3 : 2)) void attn_e4m3_kernel(
 #pragma unroll
                     for (int hf = 0; hf < kHalves; ++hf)
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) (&packed[nt][hf].x)[j] = Mma<F16>::pack2(x[8 * hf + 2 * j], x[8 * hf + 2 * j + 1]);
+                        for (int j = 0; j < 4; ++j) {
+                            const float a = x[8 * hf + 2 * j], b = x[8 * hf + 2 * j + 1];
+                            const uint32_t hi = Mma<F16>::pack2(a, b);
+                            (&packed[nt][hf][0].x)[j] = hi;
+                            (&packed[nt][hf][1].x)[j] = f16_rest2(hi, a, b);
+                        }
                 };
 #pragma unroll
                 for (int nt = 0; nt < kNT; ++nt) {
@@ -544,14 +560,21 @@ __global__ __launch_bounds__(256, (RT == 1 ? 3 : 2)) void attn_e4m3_kernel(
             // ---- O^T += V^T P^T, 32 tokens at a time ------------------------------
 #pragma unroll
             for (int hf = 0; hf < kHalves; ++hf) {
-                uint4 pop[kNT];
+                uint4 pop[kNT][2];
 #pragma unroll
                 for (int nt = 0; nt < kNT; ++nt) {
                     if ((!kInner || kCount) && nt > 0 && nt >= tiles) break;
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        if constexpr (kByTile) (&pop[nt].x)[j] = (&packed[nt][hf].x)[j];
-                        else (&pop[nt].x)[j] = Mma<F16>::pack2(p[nt][8 * hf + 2 * j], p[nt][8 * hf + 2 * j + 1]);
+                        if constexpr (kByTile) {
+                            (&pop[nt][0].x)[j] = (&packed[nt][hf][0].x)[j];
+                            (&pop[nt][1].x)[j] = (&packed[nt][hf][1].x)[j];
+                        } else {
+                            const float a = p[nt][8 * hf + 2 * j], b = p[nt][8 * hf + 2 * j + 1];
+                            const uint32_t hi = Mma<F16>::pack2(a, b);
+                            (&pop[nt][0].x)[j] = hi;
+                            (&pop[nt][1].x)[j] = f16_rest2(hi, a, b);
+                        }
                     }
                 }
 #pragma unroll
@@ -573,8 +596,11 @@ __global__ __launch_bounds__(256, (RT == 1 ? 3 : 2)) void attn_e4m3_kernel(
 #pragma unroll
                         for (int nt = 0; nt < kNT; ++nt) {
                             if ((!kInner || kCount) && nt > 0 && nt >= tiles) break;
-                            o[nt][t] = Mma<F16>::run(even, pop[nt], o[nt][t]);
-                            o[nt][t + 1] = Mma<F16>::run(odd, pop[nt], o[nt][t + 1]);
+#pragma unroll
+                            for (int piece = 1; piece >= 0; --piece) {
+                                o[nt][t] = Mma<F16>::run(even, pop[nt][piece], o[nt][t]);
+                                o[nt][t + 1] = Mma<F16>::run(odd, pop[nt][piece], o[nt][t + 1]);
+                            }
                         }
                     }
             }
