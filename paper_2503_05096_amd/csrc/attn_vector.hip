@@ -18,6 +18,9 @@ namespace adaspec {
 constexpr int kRC = 8;      // query rows per unit
 constexpr int kMaxD = 256;
 constexpr uint32_t kHidden = 0x7fcabcdeu;       // weight of a token that a row does not see
+// Reference of a row that has seen no score yet, or only -inf and NaN: finite, so that a NaN score keeps its NaN weight, and so that the state of
+// a split of which the row sees nothing is joined with weight 0 (differences of two -inf would be NaN).
+constexpr float kLowestRef = -3.4028235e38f;
 
 template <class T, bool kScaled>
 __device__ __forceinline__ float load_cached(const void *pages, int64_t at)
@@ -85,7 +88,7 @@ __global__ __launch_bounds__(64) void attn_vector_kernel(
         float m[kRC], l[kRC], acc[kRC][4];
 #pragma unroll
         for (int r = 0; r < kRC; ++r) {
-            m[r] = -INFINITY; l[r] = 0.f;
+            m[r] = kLowestRef; l[r] = 0.f;
 #pragma unroll
             for (int e = 0; e < 4; ++e) acc[r][e] = 0.f;
         }
@@ -125,11 +128,7 @@ __global__ __launch_bounds__(64) void attn_vector_kernel(
                 const float sv = vis ? sc[r] * scale_log2 : -INFINITY;
                 const float bm = wave_max(sv);
                 const float mn = fmaxf(m[r], bm);
-                float p = 0.f, alpha = 1.f;
-                if (mn > -INFINITY) {
-                    alpha = __builtin_amdgcn_exp2f(m[r] - mn);   // m = -inf -> 0
-                    p = vis ? __builtin_amdgcn_exp2f(sv - mn) : 0.f;
-                }
+                const float alpha = __builtin_amdgcn_exp2f(m[r] - mn), p = vis ? __builtin_amdgcn_exp2f(sv - mn) : 0.f;
                 l[r] = l[r] * alpha + wave_sum(p);
                 m[r] = mn;
 #pragma unroll
