@@ -220,15 +220,26 @@ AttnPlan make_attn_plan(const adaspec_attn_dims &d, AttnKind kind, bool tree)
             }
     }
     // Caches of 8 bits, few (request, kv head) pairs: as many parts of equal length as make two units per compute unit, one for a single
-    // request, whatever the lengths are (parts of two blocks per wavefront at least).  MI355X, us, 32/8 heads of 128, metadata first / 256
-    // units / 512 / 768: 1 request of 60000 36.2 / 27.9 / 30.1 / 34.6, 4 of 10000-20000 35.7 / 32.0 / 30.9 / 35.7, 16 of 3000-8000
-    // 46.5 / 47.0 / 42.6 / 48.8, 16/2 heads, 16 of 1000-8000 37.9 / 28.0 / 26.4 / 30.7, 64/8 heads, 4 of 6000-20000 55.2 / 46.4 / 37.5 /
-    // 41.8; with more pairs lengths differ too much for it: 32 of 4000-20000 140 / 201 / 170 / 174.
+    // request (parts of two blocks per wavefront at least).  MI355X, us, 32/8 heads of 128, metadata first / 256 units / 512 / 768: 1 request of
+    // 60000 36.2 / 27.9 / 30.1 / 34.6, 4 of 10000-20000 35.7 / 32.0 / 30.9 / 35.7, 16 of 3000-8000 46.5 / 47.0 / 42.6 / 48.8, 16/2 heads, 16
+    // of 1000-8000 37.9 / 28.0 / 26.4 / 30.7, 64/8 heads, 4 of 6000-20000 55.2 / 46.4 / 37.5 / 41.8; with more pairs lengths differ too
+    // much for it: 32 of 4000-20000 140 / 201 / 170 / 174.
+    // The longest request of a batch may be alone with its length: its units, fewer the more requests there are, then keep everybody
+    // waiting.  So more than two requests (whose longest has a unit for every compute unit) are cut like this only where a part of the
+    // longest possible one is short, 32 tokens of 128 channels for each of its units, 2048 at least.  Equal parts / metadata first, 32/8 of 128: one
+    // request of 60000 tokens and 15 of 500 123 / 42.3, of 20000 49.1 / 26.8, of 8000 26.4 / 23.6, of 4000 19.2 / 22.3 (16 of 3000-8000
+    // 42.5 / 45.7); one of 30000 and 7 of 500 39.9 / 31.4, of 16000 26.5 / 28.8 (8 of 20000-40000 97.4 / 92.0); one of 120000 and 3 of 1000
+    // 72.8 / 58.1, of 60000 42.1 / 39.0 (4 of 40000-60000 76.0 / 87.2); one of 120000 and one of 1000 50.5 / 58.7; 64 channels, one
+    // of 60000 and 7 of 500 47.5 / 35.8, of 20000 21.9 / 26.0.
     int64_t equal_parts = 0;
     if (kind == AttnKind::kMfmaE4m3 && !tree && !p.direct && d.batch <= kDirectMaxBatch && pairs * n_groups <= kDirectFewPairs) {
-        p.direct = true;
-        p.split_tokens = 2 * kWavesPerUnit * p.block_tokens;
-        equal_parts = (d.batch == 1 ? kDirectMaxUnits : kDirectMaxUnitsFew) / (pairs * n_groups);
+        const int64_t parts = (d.batch == 1 ? kDirectMaxUnits : kDirectMaxUnitsFew) / (pairs * n_groups), units = parts * d.n_kv_heads * n_groups;
+        const int64_t longest = (units > 64 ? 32 * units : 2048) * 128 / d.head_dim;
+        if (d.batch <= 2 || max_ctx <= parts * longest) {
+            p.direct = true;
+            p.split_tokens = 2 * kWavesPerUnit * p.block_tokens;
+            equal_parts = parts;
+        }
     }
     if (scheduled && !tree && !p.direct && max_ctx <= p.split_tokens && max_ctx <= kDirectLongestShort && d.batch <= kDirectShortBatch) {
         // Short contexts: every request is one unit per kv head (no combine), all of them about equally short.  Measured
