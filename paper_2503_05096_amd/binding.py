@@ -719,8 +719,8 @@ def _rope_dims(rows, heads, kv_heads, d, table_shape, num_pages, max_spec_len, d
     if inv_freq is not None:
         assert inv_freq.is_cuda and inv_freq.is_contiguous() and inv_freq.dtype == torch.float32 and inv_freq.dim() == 1
         rot = 2 * inv_freq.shape[0]
-    if not attn_factor > 0:
-        raise ValueError("attn_factor= is more than 0")
+    if not C.c_float(float(attn_factor)).value > 0:                # (0 in fp32 would mean 1 to the library)
+        raise ValueError("attn_factor= is more than 0, in fp32")
     B, max_pages = table_shape
     return RopeDims(B, rows, int(max_spec_len), heads, kv_heads, d, 16, num_pages, max_pages, dtype, rot, int(bool(interleaved)),
                     float(attn_factor), 0, 0, 0, 0, 0)
