@@ -57,4 +57,4 @@ def rope_frequencies(rot_dim: int, *, base: float = 10000.0, scaling: Optional[d
         raise ValueError(f"rope_frequencies: no scaling {kind!r}")
     if s:
         raise ValueError(f"rope_frequencies: what is {sorted(s)}?")
-    return torch.tensor(freq, dtype=torch.float64).float().to(device or "cpu"), gain
+    return torch.tensor(freq, dtype=torch.float64).float().to("cpu" if device is None else device), gain

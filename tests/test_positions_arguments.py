@@ -20,3 +20,10 @@ def test_a_factor_that_is_nothing_in_fp32_is_refused(gain, monkeypatch):
             pkg.rope(x, f, lens, lens, max_spec_len=1, attn_factor=gain)
         with pytest.raises(ValueError):
             pkg.kv_append_rope(x, kv, kv, f, pages, pages, table, lens, lens, max_spec_len=1, attn_factor=gain)
+
+
+def test_frequencies_on_a_device_by_its_number():
+    with FakeTensorMode():
+        freq, _ = pkg.rope_frequencies(16, device=0)
+    assert freq.device == torch.device("cuda", 0)
+    assert pkg.rope_frequencies(16)[0].device.type == "cpu" and pkg.rope_frequencies(16, device="meta")[0].device.type == "meta"
