@@ -47,10 +47,6 @@ __device__ __forceinline__ void e4m3_rescale8(const uint8_t *from, uint8_t *to, 
     const uint2 w = *reinterpret_cast<const uint2 *>(from);
     *reinterpret_cast<uint2 *>(to) = make_uint2(e4m3_rescale4(w.x, ratio), e4m3_rescale4(w.y, ratio));
 }
-__device__ __forceinline__ uint4 e4m3_rescale16(uint4 w, float ratio)
-{
-    return make_uint4(e4m3_rescale4(w.x, ratio), e4m3_rescale4(w.y, ratio), e4m3_rescale4(w.z, ratio), e4m3_rescale4(w.w, ratio));
-}
 
 // log2 of the least power of two s with most <= (448 s)^2: 448^2 = 1.53125 * 2^17.  In squares of 64 bits, so that it does not
 // depend on any rounding (products of two floats are exact there).
