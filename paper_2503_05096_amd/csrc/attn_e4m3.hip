@@ -256,23 +256,8 @@ __global__ __launch_bounds__(256, (RT == 1 ? 3 : 2)) void attn_e4m3_kernel(
             float p[kByTile ? 1 : kNT][kE];
             uint4 packed[kByTile ? kNT : 1][kHalves][2];            // P as an operand, in two pieces
             uint32_t seen[kNT];                                     // masked: bit e = the row sees token e
-            if constexpr (kByTile) {
-                // ---- S^T = K Q^T, row tile by row tile: the keys once in Q's type, P packed as soon as it is known -------
-                uint4 kop[kPages][kSteps];
-#pragma unroll
-                for (int mt = 0; mt < kPages; ++mt)
-#pragma unroll
-                    for (int s = 0; s < kSteps; ++s) {
-                        const uint4 raw = kreg[mt][s >> 1];
-                        kop[mt][s] = (s & 1) ? e4m3_operand<T>(raw.z, raw.w) : e4m3_operand<T>(raw.x, raw.y);
-                    }
-                float factor[kPages];
-#pragma unroll
-                for (int mt = 0; mt < kPages; ++mt) factor[mt] = ks[mt] * scale_log2;
-                __builtin_amdgcn_sched_barrier(0);
-                if (next) load_k(nb);
-                __builtin_amdgcn_sched_barrier(0);
-                float weight[kPages];
+            float weight[kPages];                                   // of a value: its scale in units of O
+            auto find_weights = [&] {
                 if constexpr (!kWide) {
                     // the values' scales relative to the largest so far, which O is kept in units of
                     float most_vs = vs[0];
@@ -294,81 +279,90 @@ __global__ __launch_bounds__(256, (RT == 1 ? 3 : 2)) void attn_e4m3_kernel(
                 }
 #pragma unroll
                 for (int mt = 0; mt < kPages; ++mt) weight[mt] = vs[mt] * (kWide ? kUnitShift : vref_inv);
-
-                auto weigh = [&](int nt, float (&x)[kE]) {
-                    // ---- online softmax (per lane: row n16 of the tile, kE of the tokens), in log2 units
-                    if (masked) {
-                        seen[nt] = 0;
-                        const unsigned long long am = kTree ? s_anc[16 * nt + n16] : 0ull;
-                        const int row = u.r0 + 16 * nt + n16, base = u.L - u.n;
-                        const int pos = row < u.rows ? base + row / G : -1, lim = min(pos, u.t1 - 1);
-#pragma unroll
-                        for (int e = 0; e < kE; ++e) {
-                            const int t = tb + 16 * (e >> 2) + g + 4 * (e & 3), rel = t - base;
-                            bool vis;
-                            if constexpr (kTree) vis = t < u.t1 && (rel < 0 ? pos >= 0 : ((am >> (rel & 63)) & 1ull) != 0);
-                            else vis = t <= lim;
-                            x[e] = vis ? x[e] : -INFINITY;
-                            seen[nt] |= vis ? 1u << e : 0u;
-                        }
-                    }
-                    float mx = x[0];
-#pragma unroll
-                    for (int e = 1; e < kE; ++e) mx = fmaxf(mx, x[e]);
-                    mx = max_over_row_groups(mx);
-                    // lazy reference: moves only when the block's maximum exceeds it by more than kLazyLog2
-                    const bool grow = mx > m[nt] + kLazyLog2;
-                    if (__builtin_expect(__builtin_amdgcn_ballot_w64(grow) != 0, 0)) {
-                        const float m_new = grow ? mx : m[nt];
-                        const float alpha = __builtin_amdgcn_exp2f(m[nt] - m_new);
-                        m[nt] = m_new;
-                        lsum[nt] *= alpha;
-                        if constexpr (kWide) {
-                            my_units[16 * nt] *= alpha;
-                        } else {
-#pragma unroll
-                            for (int t = 0; t < kTiles; ++t) o[nt][t] *= alpha;
-                        }
-                    }
-                    float psum = 0.f;
+            };
+            // Online softmax of row tile nt (per lane: row n16 of the tile, kE of the tokens), in log2 units: scores to weights.
+            auto weigh = [&](int nt, float (&x)[kE]) {
+                if (masked) {
+                    seen[nt] = 0;
+                    const unsigned long long am = kTree ? s_anc[16 * nt + n16] : 0ull;
+                    const int row = u.r0 + 16 * nt + n16, base = u.L - u.n;
+                    const int pos = row < u.rows ? base + row / G : -1, lim = min(pos, u.t1 - 1);
 #pragma unroll
                     for (int e = 0; e < kE; ++e) {
-                        x[e] = __builtin_amdgcn_exp2f(x[e] - m[nt]);
-                        psum += x[e];
-                        x[e] *= weight[e >> 2];
-                        // what hidden tokens hold stays out: no weight, whatever their scale
-                        if (masked) x[e] = (seen[nt] >> e) & 1 ? x[e] : 0.f;
+                        const int t = tb + 16 * (e >> 2) + g + 4 * (e & 3), rel = t - base;
+                        bool vis;
+                        if constexpr (kTree) vis = t < u.t1 && (rel < 0 ? pos >= 0 : ((am >> (rel & 63)) & 1ull) != 0);
+                        else vis = t <= lim;
+                        x[e] = vis ? x[e] : -INFINITY;
+                        seen[nt] |= vis ? 1u << e : 0u;
                     }
-                    lsum[nt] += psum;
+                }
+                if constexpr (!kByTile && RT > 2) __builtin_amdgcn_sched_barrier(0);
+                float mx = x[0];
+#pragma unroll
+                for (int e = 1; e < kE; ++e) mx = fmaxf(mx, x[e]);
+                mx = max_over_row_groups(mx);
+                // lazy reference: moves only when the block's maximum exceeds it by more than kLazyLog2
+                const bool grow = mx > m[nt] + kLazyLog2;
+                if (__builtin_expect(__builtin_amdgcn_ballot_w64(grow) != 0, 0)) {
+                    const float m_new = grow ? mx : m[nt];
+                    const float alpha = __builtin_amdgcn_exp2f(m[nt] - m_new);
+                    m[nt] = m_new;
+                    lsum[nt] *= alpha;
                     if constexpr (kWide) {
-                        // the row's unit follows the largest weight times scale that it has seen, as m the largest score
-                        float most = x[0];
+                        my_units[16 * nt] *= alpha;
+                    } else {
 #pragma unroll
-                        for (int e = 1; e < kE; ++e) most = fmaxf(most, x[e]);
-                        most = max_over_row_groups(most);
-                        const float was = my_units[16 * nt];
-                        const bool move = was != power_of_two_below(was) || was < kLeastUnit || most > was * (float)(1 << (int)kLazyLog2);
-                        const float to = move ? power_of_two_below(fmaxf(fmaxf(most, was), kLeastUnit)) : was;
-                        if (__builtin_amdgcn_ballot_w64(move) != 0) {
-                            const float ratio = was * one_over<0>(to);
-#pragma unroll
-                            for (int t = 0; t < kTiles; ++t) o[nt][t] *= ratio;
-                            my_units[16 * nt] = to;
-                        }
-                        const float inv = one_over<kWeightShift>(to);
-#pragma unroll
-                        for (int e = 0; e < kE; ++e) x[e] *= inv;
+                        for (int t = 0; t < kTiles; ++t) o[nt][t] *= alpha;
                     }
+                }
+                float psum = 0.f;
 #pragma unroll
-                    for (int hf = 0; hf < kHalves; ++hf)
+                for (int e = 0; e < kE; ++e) {
+                    x[e] = __builtin_amdgcn_exp2f(x[e] - m[nt]);
+                    psum += x[e];
+                    x[e] *= weight[e >> 2];
+                    // what hidden tokens hold stays out: no weight, whatever their scale
+                    if (masked) x[e] = (seen[nt] >> e) & 1 ? x[e] : 0.f;
+                }
+                lsum[nt] += psum;
+                if constexpr (kWide) {
+                    // the row's unit follows the largest weight times scale that it has seen, as m the largest score
+                    float most = x[0];
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            const float a = x[8 * hf + 2 * j], b = x[8 * hf + 2 * j + 1];
-                            const uint32_t hi = Mma<F16>::pack2(a, b);
-                            (&packed[nt][hf][0].x)[j] = hi;
-                            (&packed[nt][hf][1].x)[j] = f16_rest2(hi, a, b);
-                        }
-                };
+                    for (int e = 1; e < kE; ++e) most = fmaxf(most, x[e]);
+                    most = max_over_row_groups(most);
+                    const float was = my_units[16 * nt];
+                    const bool move = was != power_of_two_below(was) || was < kLeastUnit || most > was * (float)(1 << (int)kLazyLog2);
+                    const float to = move ? power_of_two_below(fmaxf(fmaxf(most, was), kLeastUnit)) : was;
+                    if (__builtin_amdgcn_ballot_w64(move) != 0) {
+                        const float ratio = was * one_over<0>(to);
+#pragma unroll
+                        for (int t = 0; t < kTiles; ++t) o[nt][t] *= ratio;
+                        my_units[16 * nt] = to;
+                    }
+                    const float inv = one_over<kWeightShift>(to);
+#pragma unroll
+                    for (int e = 0; e < kE; ++e) x[e] *= inv;
+                }
+            };
+            if constexpr (kByTile) {
+                // ---- S^T = K Q^T, row tile by row tile: the keys once in Q's type, P packed as soon as it is known -------
+                uint4 kop[kPages][kSteps];
+#pragma unroll
+                for (int mt = 0; mt < kPages; ++mt)
+#pragma unroll
+                    for (int s = 0; s < kSteps; ++s) {
+                        const uint4 raw = kreg[mt][s >> 1];
+                        kop[mt][s] = (s & 1) ? e4m3_operand<T>(raw.z, raw.w) : e4m3_operand<T>(raw.x, raw.y);
+                    }
+                float factor[kPages];
+#pragma unroll
+                for (int mt = 0; mt < kPages; ++mt) factor[mt] = ks[mt] * scale_log2;
+                __builtin_amdgcn_sched_barrier(0);
+                if (next) load_k(nb);
+                __builtin_amdgcn_sched_barrier(0);
+                find_weights();
 #pragma unroll
                 for (int nt = 0; nt < kNT; ++nt) {
                     if ((!kInner || kCount) && nt > 0 && nt >= tiles) break;
@@ -382,6 +376,15 @@ __global__ __launch_bounds__(256, (RT == 1 ? 3 : 2)) void attn_e4m3_kernel(
 #pragma unroll
                     for (int e = 0; e < kE; ++e) p[0][e] = acc[e >> 2][e & 3] * factor[e >> 2];
                     weigh(nt, p[0]);
+#pragma unroll
+                    for (int hf = 0; hf < kHalves; ++hf)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const float a = p[0][8 * hf + 2 * j], b = p[0][8 * hf + 2 * j + 1];
+                            const uint32_t hi = Mma<F16>::pack2(a, b);
+                            (&packed[nt][hf][0].x)[j] = hi;
+                            (&packed[nt][hf][1].x)[j] = f16_rest2(hi, a, b);
+                        }
                 }
             } else {
                 // ---- S^T = K Q^T ------------------------------------------------------------
@@ -410,100 +413,11 @@ __global__ __launch_bounds__(256, (RT == 1 ? 3 : 2)) void attn_e4m3_kernel(
                 if (next) load_k(nb);
                 __builtin_amdgcn_sched_barrier(0);
 
-                // ---- online softmax (per lane: row n16 of each row tile, kE of the tokens), in log2 units ----
-                float weight[kPages];
-                if constexpr (!kWide) {
-                    // the values' scales relative to the largest so far, which O is kept in units of
-                    float most_vs = vs[0];
-                    least_scale = fminf(least_scale, vs[0]);
-#pragma unroll
-                    for (int mt = 1; mt < kPages; ++mt) {
-                        most_vs = fmaxf(most_vs, vs[mt]);
-                        least_scale = fminf(least_scale, vs[mt]);
-                    }
-                    if (__builtin_expect(most_vs > vref, 0)) {
-                        const float up = __uint_as_float((__float_as_uint(most_vs) + 0x7fffffu) & 0x7f800000u), down = vref * one_over<0>(up);
-                        vref = up;
-                        vref_inv = one_over<kWeightShift>(up);
-#pragma unroll
-                        for (int nt = 0; nt < kNT; ++nt)
-#pragma unroll
-                            for (int t = 0; t < kTiles; ++t) o[nt][t] *= down;
-                    }
-                }
-#pragma unroll
-                for (int mt = 0; mt < kPages; ++mt) weight[mt] = vs[mt] * (kWide ? kUnitShift : vref_inv);
+                find_weights();
 #pragma unroll
                 for (int nt = 0; nt < kNT; ++nt) {
                     if ((!kInner || kCount) && nt > 0 && nt >= tiles) break;
-                    if (masked) {
-                        seen[nt] = 0;
-                        const unsigned long long am = kTree ? s_anc[16 * nt + n16] : 0ull;
-                        const int row = u.r0 + 16 * nt + n16, base = u.L - u.n;
-                        const int pos = row < u.rows ? base + row / G : -1, lim = min(pos, u.t1 - 1);
-#pragma unroll
-                        for (int e = 0; e < kE; ++e) {
-                            const int t = tb + 16 * (e >> 2) + g + 4 * (e & 3), rel = t - base;
-                            bool vis;
-                            if constexpr (kTree) vis = t < u.t1 && (rel < 0 ? pos >= 0 : ((am >> (rel & 63)) & 1ull) != 0);
-                            else vis = t <= lim;
-                            p[nt][e] = vis ? p[nt][e] : -INFINITY;
-                            seen[nt] |= vis ? 1u << e : 0u;
-                        }
-                    }
-                    if constexpr (RT > 2) __builtin_amdgcn_sched_barrier(0);
-                    float mx = p[nt][0];
-#pragma unroll
-                    for (int e = 1; e < kE; ++e) mx = fmaxf(mx, p[nt][e]);
-                    mx = max_over_row_groups(mx);
-                    // lazy reference: moves only when the block's maximum exceeds it by more than kLazyLog2
-                    const bool grow = mx > m[nt] + kLazyLog2;
-                    if (__builtin_expect(__builtin_amdgcn_ballot_w64(grow) != 0, 0)) {
-                        const float m_new = grow ? mx : m[nt];
-                        const float alpha = __builtin_amdgcn_exp2f(m[nt] - m_new);
-                        m[nt] = m_new;
-                        lsum[nt] *= alpha;
-                        if constexpr (kWide) {
-                            my_units[16 * nt] *= alpha;
-                        } else {
-#pragma unroll
-                            for (int t = 0; t < kTiles; ++t) o[nt][t] *= alpha;
-                        }
-                    }
-                    float psum = 0.f;
-#pragma unroll
-                    for (int e = 0; e < kE; ++e) {
-                        p[nt][e] = __builtin_amdgcn_exp2f(p[nt][e] - m[nt]);
-                        psum += p[nt][e];
-                        p[nt][e] *= weight[e >> 2];
-                        // what hidden tokens hold stays out: no weight, whatever their scale
-                        if (masked) p[nt][e] = (seen[nt] >> e) & 1 ? p[nt][e] : 0.f;
-                    }
-                    lsum[nt] += psum;
-                }
-                if constexpr (kWide) {
-                    // every row's unit follows the largest weight times scale that it has seen, as m the largest score
-#pragma unroll
-                    for (int nt = 0; nt < kNT; ++nt) {
-                        if (nt > 0 && nt >= tiles) break;
-                        if constexpr (RT > 2) __builtin_amdgcn_sched_barrier(0);
-                        float most = p[nt][0];
-#pragma unroll
-                        for (int e = 1; e < kE; ++e) most = fmaxf(most, p[nt][e]);
-                        most = max_over_row_groups(most);
-                        const float was = my_units[16 * nt];
-                        const bool move = was != power_of_two_below(was) || was < kLeastUnit || most > was * (float)(1 << (int)kLazyLog2);
-                        const float to = move ? power_of_two_below(fmaxf(fmaxf(most, was), kLeastUnit)) : was;
-                        if (__builtin_amdgcn_ballot_w64(move) != 0) {
-                            const float ratio = was * one_over<0>(to);
-#pragma unroll
-                            for (int t = 0; t < kTiles; ++t) o[nt][t] *= ratio;
-                            my_units[16 * nt] = to;
-                        }
-                        const float inv = one_over<kWeightShift>(to);
-#pragma unroll
-                        for (int e = 0; e < kE; ++e) p[nt][e] *= inv;
-                    }
+                    weigh(nt, p[nt]);
                 }
             }
 
