@@ -14,9 +14,10 @@
 //     out).  The lane then holds D / 16 whole operand columns: tile t of O^T has channel (D / 16) m + t in row m.
 // A block is 32 tokens of 128 channels or 64 of 64: 8 KB of K and V per wavefront, 32 registers.
 //
-// Bound: HBM where requests are many and rows few: 128 requests of 128-4096 tokens, 32/8 heads of 128, 562 MB in 95-98 us of the kernel, 5.8
-// TB/s; 64 of 8192-32768, 64/8 heads, 2.7 GB in 474-489 us, 5.6 TB/s (one row tile 435: up to 6.3).  The vector ALU where they are many: a score costs
-// about 10 instructions whatever it weighs, and with four row tiles (trees of 13 nodes, G = 4) there are 64 of them per token.
+// Bound: HBM where requests are many and rows few: 128 requests of 128-4096 tokens, 32/8 heads of 128, 562 MB, 102 us a call, 96 of them this
+// kernel, 5.8 TB/s; 64 of 8192-32768, 64/8 heads, 2.7 GB in 452 us with one row tile, 6.0 TB/s, 517 with three (which spill 47 registers).  The
+// vector ALU where rows are many: a score costs about 12 instructions whatever it weighs, and with four row tiles (trees of 13 nodes, G = 4:
+// 156 us for those 562 MB) there are 64 of them per token.
 #include <type_traits>
 
 #include "adaspec_internal.h"
@@ -51,14 +52,14 @@ __device__ __forceinline__ uint32_t e4m3_nans(uint32_t w) { return ((w & 0x7f7f7
 // they trail 1 by 2^kLazyLog2 at most.  Off by 2^-22 of themselves, or by 2^-25 (half a subnormal) where that is more, as little as the
 // fp32 sums they go into.  The first piece alone is off by up to 2^-12 and leaves that in the output wherever weights round alike.  MI355X, output in
 // fp32 against 64 bits, relative, one piece / two: 128 requests of 128-4096 tokens, 32/8 heads of 128, 1.8e-4 / 2.7e-7 (100.9 / 101.7
-// us), 64 trees of up to 13 nodes, 256-4096, 32/8 of 64, 1.8e-4 / 3.4e-7 (52.5 / 56.8); 64 of 8192-32768, 64/8 of 128, 495 / 509 us.
+// us), 64 trees of up to 13 nodes, 256-4096, 32/8 of 64, 1.8e-4 / 3.4e-7 (52.7 / 56.1); 64 of 8192-32768, 64/8 of 128, 495 / 517 us.
 // They are multiplied by their value's scale before that, relative to the largest scale so far, which O is kept in units of: a factor
 // per page.  That is sound where all scales are within kScalesApart of each other: 2^-25 of a unit, what a subnormal may be off by, is
 // then at most 2^-26 of the row's largest weighted scale.  A wavefront that has met scales further apart, which it knows at the end of its
 // blocks, takes them once more with a unit for every row, the largest weight times scale that this row has seen, so that neither a page
 // that is far louder (and perhaps hidden from the row) nor one that is far quieter costs the others their bits.  (To leave the inner
 // loop at the first such page instead, its keys kept or requested again, cost the usual case 3 % and 8 %.  128 requests of 128-4096 tokens,
-// 32/8 heads: 105 us, 167 with a page a thousand times as loud in each.)
+// 32/8 heads: 106 us, 170 with a page a thousand times as loud in each.)
 constexpr int kWeightShift = 7;
 constexpr float kScalesApart = 64.f;
 // (Units are powers of two: what is kept in them changes exactly.)  Units of rows times kUnitShift: the product of a scale and a weight up to
@@ -79,7 +80,6 @@ __global__ __launch_bounds__(256, (RT == 1 ? 3 : 2)) void attn_e4m3_kernel(
     int Hq, int Hkv, int max_pages_per_req, int max_rows, int n_row_groups, float scale_log2, int out_dtype, int cus, DirectArgs direct)
 {
     constexpr int kRows = 16 * RT;
-    constexpr bool kCount = RT > 3;                                 // tiles without rows are skipped at run time in the inner loop, too
     constexpr int kTokens = attn_e4m3_block(D), kPages = kTokens / 16;
     constexpr int kKLoads = D / 64;                                 // 16-byte pieces of a key per lane
     constexpr int kSteps = D / 32;                                  // products per 16 x 16 tile of scores
@@ -251,8 +251,8 @@ __global__ __launch_bounds__(256, (RT == 1 ? 3 : 2)) void attn_e4m3_kernel(
 
             // Two orders of the same work.  head_dim 64: row tile by row tile, with all keys in Q's type (32 registers) and P packed at once, so
             // that Q is read once per block, not once per page, and the scores of one tile are live, not of all: 64 requests of 256-4096
-            // tokens, trees of up to 13 nodes, 32/8 heads: 52.6 us against 60.9.  head_dim 128, whose O leaves no registers for that: page by
-            // page (the other way costs 64 requests of 8192-32768 tokens, 64/8 heads, 520 us against 495, trees of up to 13 nodes 168 against 155).
+            // tokens, trees of up to 13 nodes, 32/8 heads: 56.1 us against 61.1.  head_dim 128, whose O leaves no registers for that: page by
+            // page (the other way costs 64 requests of 8192-32768 tokens, 64/8 heads, 539 us against 517, trees of up to 13 nodes 160 against 156).
             float p[kByTile ? 1 : kNT][kE];
             uint4 packed[kByTile ? kNT : 1][kHalves][2];            // P as an operand, in two pieces
             uint32_t seen[kNT];                                     // masked: bit e = the row sees token e
@@ -365,7 +365,7 @@ __global__ __launch_bounds__(256, (RT == 1 ? 3 : 2)) void attn_e4m3_kernel(
                 find_weights();
 #pragma unroll
                 for (int nt = 0; nt < kNT; ++nt) {
-                    if ((!kInner || kCount) && nt > 0 && nt >= tiles) break;
+                    if (!kInner && nt > 0 && nt >= tiles) break;
                     f32x4 acc[kPages];
 #pragma unroll
                     for (int s = 0; s < kSteps; ++s) {
@@ -400,7 +400,7 @@ __global__ __launch_bounds__(256, (RT == 1 ? 3 : 2)) void attn_e4m3_kernel(
                     if constexpr (RT > 2) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                     for (int nt = 0; nt < kNT; ++nt) {
-                        if ((!kInner || kCount) && nt > 0 && nt >= tiles) break;
+                        if (!kInner && nt > 0 && nt >= tiles) break;
                         f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                         for (int s = 0; s < kSteps; ++s) acc = Mma<T>::run(kop[s], q_lds[(nt * kSteps + s) * 64 + lane], acc);
@@ -416,7 +416,7 @@ __global__ __launch_bounds__(256, (RT == 1 ? 3 : 2)) void attn_e4m3_kernel(
                 find_weights();
 #pragma unroll
                 for (int nt = 0; nt < kNT; ++nt) {
-                    if ((!kInner || kCount) && nt > 0 && nt >= tiles) break;
+                    if (!kInner && nt > 0 && nt >= tiles) break;
                     weigh(nt, p[nt]);
                 }
             }
@@ -447,7 +447,7 @@ __global__ __launch_bounds__(256, (RT == 1 ? 3 : 2)) void attn_e4m3_kernel(
                             const uint4 a = make_uint4(bad[0] | bad[1] << 16, bad[2] | bad[3] << 16, bad[4] | bad[5] << 16, bad[6] | bad[7] << 16);
 #pragma unroll
                             for (int nt = 0; nt < kNT; ++nt) {
-                                if ((!kInner || kCount) && nt > 0 && nt >= tiles) break;
+                                if (!kInner && nt > 0 && nt >= tiles) break;
                                 uint32_t see[8];
 #pragma unroll
                                 for (int e = 0; e < 8; ++e) see[e] = (seen[nt] >> (8 * hf + e)) & 1 ? 0x3f80u : 0u;
@@ -477,7 +477,7 @@ __global__ __launch_bounds__(256, (RT == 1 ? 3 : 2)) void attn_e4m3_kernel(
                 uint4 pop[kNT][2];
 #pragma unroll
                 for (int nt = 0; nt < kNT; ++nt) {
-                    if ((!kInner || kCount) && nt > 0 && nt >= tiles) break;
+                    if (!kInner && nt > 0 && nt >= tiles) break;
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         if constexpr (kByTile) {
@@ -509,7 +509,7 @@ __global__ __launch_bounds__(256, (RT == 1 ? 3 : 2)) void attn_e4m3_kernel(
                         const int t = 4 * w + 2 * up;
 #pragma unroll
                         for (int nt = 0; nt < kNT; ++nt) {
-                            if ((!kInner || kCount) && nt > 0 && nt >= tiles) break;
+                            if (!kInner && nt > 0 && nt >= tiles) break;
 #pragma unroll
                             for (int piece = 1; piece >= 0; --piece) {
                                 o[nt][t] = Mma<F16>::run(even, pop[nt][piece], o[nt][t]);
@@ -530,10 +530,11 @@ __global__ __launch_bounds__(256, (RT == 1 ? 3 : 2)) void attn_e4m3_kernel(
             auto inner = [&](auto tiles_tag) {
                 for (; bi + kWaves < u.nblk && bi < full; bi += kWaves) block(bi, std::true_type{}, tiles_tag, std::false_type{});
             };
-            // (A copy of the loop for every number of tiles; with four of them they crowd the instruction cache: 128 requests of 128-4096
-            // tokens, trees of up to 13 nodes, 32/8 heads: 152 us with one copy, whose tiles are counted at run time, 168 with four.
-            // Up to three: 100.4 us against 101.7 for the headline batch, 497 against 505 for 64 of 8192-32768, 64/8 heads)
-            if (kCount) inner(std::integral_constant<int, RT>{});
+            // (A copy of the loop for every number of tiles, so that none is looked at in it.  MI355X, us, with copies / one loop that skips tiles without
+            // rows: 128 requests of 128-4096 tokens, 32/8 heads of 128, 102.0 / 104.4, in trees of up to 13 nodes 156 / 187, 64 of 8192-32768, 64/8
+            // 517 / 529, of up to 8 rows 621 / 679; 64-channel trees 56.1 / 57.1.  Four tiles first: with that copy behind the others the
+            // compiler spills twice as many registers, and those trees take 192 and 73 us.)
+            if (RT == 4 && tiles > 3) inner(std::integral_constant<int, RT>{});
             else if (RT == 1 || tiles <= 1) inner(std::integral_constant<int, 1>{});
             else if (RT == 2 || tiles == 2) inner(std::integral_constant<int, RT < 2 ? 1 : 2>{});
             else inner(std::integral_constant<int, RT < 3 ? 1 : 3>{});
