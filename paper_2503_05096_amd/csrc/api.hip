@@ -179,9 +179,9 @@ AttnPlan make_attn_plan(const adaspec_attn_dims &d, AttnKind kind, bool tree)
         // A unit of so many tokens is half the bytes that it is in 16 bits, and the states of its parts, in fp32, are not: longer
         // splits.  How long follows from the lengths, which the plan kernel sees: tokens times kv heads over two units per compute
         // unit, as the next power of two.  MI355X, us, 32/8 heads of 128, splits of 1024 / 2048 / 4096 / 8192 / 16384 (that figure):
-        // 8 requests of 5000-10000 34.5 / 41.4 / 52.2 / 90.0 / 92.9 (937), 32 of 500-6000 54.8 / 49.2 / 53.4 / 63.2 / 63.2 (1624), 64 of
-        // 500-4000 76.8 / 67.1 / 56.5 / 56.8 (2249), 32 of 4000-20000 186 / 168 / 159 / 138 / 197 (6000), 64 of 8192-32768 600 / 550 /
-        // 496 / 467 / 488 (20480).  Longer than 8192 gains nothing.
+        // 8 requests of 5000-10000 34.6 / 41.3 / 45.3 / 73.4 / 87.8 (937), 32 of 500-6000 54.6 / 48.4 / 52.6 / 61.3 / 61.3 (1624), 64 of
+        // 500-4000 76.4 / 66.5 / 56.0 / 56.1 (2249), 32 of 4000-20000 185 / 167 / 156 / 136 / 172 (6000), 64 of 8192-32768, 64/8, 644 / 595 /
+        // 542 / 515 / 523 (20480).  Longer than 8192 gains nothing.
         if (pairs >= 512) p.split_tokens = 2 * p.split_tokens;
         p.split_most = kE4m3MostSplit;
     }
@@ -221,9 +221,9 @@ AttnPlan make_attn_plan(const adaspec_attn_dims &d, AttnKind kind, bool tree)
     }
     // Caches of 8 bits, few (request, kv head) pairs: as many parts of equal length as make two units per compute unit, one for a single
     // request (parts of two blocks per wavefront at least).  MI355X, us, 32/8 heads of 128, metadata first / 256 units / 512 / 768: 1 request of
-    // 60000 36.2 / 27.9 / 30.1 / 34.6, 4 of 10000-20000 35.7 / 32.0 / 30.9 / 35.7, 16 of 3000-8000 46.5 / 47.0 / 42.6 / 48.8, 16/2 heads, 16
-    // of 1000-8000 37.9 / 28.0 / 26.4 / 30.7, 64/8 heads, 4 of 6000-20000 55.2 / 46.4 / 37.5 / 41.8; with more pairs lengths differ too
-    // much for it: 32 of 4000-20000 140 / 201 / 170 / 174.
+    // 60000 38.6 / 28.4 / 30.6 / 36.0, 4 of 10000-20000 35.6 / 31.6 / 30.8 / 36.6, 16 of 3000-8000 45.5 / 44.8 / 42.3 / 48.6, 16/2 heads, 16
+    // of 1000-8000 39.9 / 28.3 / 26.6 / 30.9, 64/8 heads, 4 of 6000-20000 59.7 / 46.8 / 37.3 / 42.2; with more pairs lengths differ too
+    // much for it: 32 of 4000-20000 137 / 180 / 168 / 176.
     // The longest request of a batch may be alone with its length: its units, fewer the more requests there are, then keep everybody
     // waiting.  So more than two requests (whose longest has a unit for every compute unit) are cut like this only where a part of the
     // longest possible one is short, 32 tokens of 128 channels for each of its units, 2048 at least.  Equal parts / metadata first, 32/8 of 128: one

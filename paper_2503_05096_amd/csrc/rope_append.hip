@@ -10,8 +10,9 @@
 // decide together) and some of the kv heads with their query heads; cosines and sines of its rows are worked out once.
 //
 // Small calls are bound by latency: two memory round trips (lengths, rows), three into a cache of 8 bits (the page's scale), with
-// the angles worked out while the rows travel: 128 requests of up to 7 rows, 32/8 heads of 128, 6.7 us, into 8 bits 8.9.  Large ones by
-// HBM: 16 prompts of 100-4000 rows 168 us for 806 MB, 4.8 TB/s; into 8 bits, 64/8 heads, 256 for 1276 MB, 5.0 TB/s (a large copy: 5.07).
+// the angles worked out while the rows travel: 128 requests of up to 7 rows, 32/8 heads of 128, 6.8 us, into 8 bits 8.9, where a wavefront's second head
+// is requested when its first is written: one round trip more.  Large ones by HBM: 16 prompts of 100-4000 rows 169 us for 806 MB,
+// 4.8 TB/s; into 8 bits, 64/8 heads, 256 for 1276 MB, 5.0 TB/s (a large copy: 5.07).
 #include <type_traits>
 
 #include "adaspec_internal.h"
@@ -25,7 +26,9 @@ constexpr int kRopeThreads = 256;
 constexpr int kRopeRows = 16;
 static_assert(kRopeRows == kPageTokens, "a workgroup's rows are those of a page");
 constexpr int kRopeMaxHalf = 128;       // pairs of a head
-constexpr int kFewChunks = 8;           // MI355X, us: headline step into 8 bits, 2 chunks a request, 10.2 -> 9.4, but prompts of up to 250 257 -> 324
+// MI355X, us, into 8 bits, chunk by chunk / request by request: 128 requests of up to 7 rows (2 chunks) 9.5 / 8.9, 128 prompts of up to 100 (8)
+// 77 / 62, 64 of up to 250 (17) 68.5 / 82, 16 of up to 4000 (251) 243 / 304.
+constexpr int kFewChunks = 8;
 
 struct RopeArgs {
     const void *q, *k, *v;
@@ -468,10 +471,10 @@ hipError_t launch_rope_append(const void *q, const void *k, const void *v, const
     const int heads = k ? d.n_kv_heads : d.n_q_heads;
     // Heads per workgroup: enough for its angles to be shared (20 rows of heads per row; into 8 bits, where a wavefront takes a head's keys
     // or values, 2 kv heads, or 4 without shared ones), fewer where that leaves less than two workgroups per compute unit.
-    // MI355X, us, 1 / 2 / 4 / 8 kv heads of 32/8: 128 requests of up to 7 rows 6.9 / 6.3 / 7.3 / 9.8, into 8 bits 12.5 / 10.3 / 12.1 /
-    // 16.7; prompts of 32000 rows 189 / 195 / 168 / 177, into 8 bits (64/8) 306 / 258 / 264 / 275; 16 trees of up to 61 rows into 8
-    // bits 12.5 / 13.7 / 16.6 / 23.7 (8 bits: all of them when scratch memory still cost the small ones 1-4 us); query heads alone, 17400 rows
-    // of 32 86 / 56 / 50 / 51.
+    // MI355X, us, 1 / 2 / 4 / 8 kv heads of 32/8: 128 requests of up to 7 rows 7.4 / 6.8 / 7.9 / 10.7, into 8 bits 9.6 / 9.0 / 9.8 /
+    // 13.8; prompts of 32000 rows 184 / 190 / 169 / 177, into 8 bits 180 / 181 / 153 / 159, of 64/8 heads 307 / 256 / 264 / 274; 16 trees of
+    // up to 61 rows into 8 bits 8.8 / 10.3 / 13.1 / 21.0; without shared heads (32/32), 128 of up to 7 into 8 bits 28.8 / 20.6 / 17.6 / 17.9, without
+    // queries 18.1 / 12.9 / 10.9 / 12.1; query heads alone, 17400 rows of 32 94 / 60 / 51 / 52.
     const int shared = k && q ? d.n_q_heads / d.n_kv_heads : 1;
     a.heads = !k ? 4 : !fp8 ? 20 / (shared + 1) : shared > 1 ? 2 : 4;
     a.heads = a.heads < 1 ? 1 : a.heads > heads ? heads : a.heads;
