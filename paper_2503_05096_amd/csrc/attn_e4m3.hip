@@ -50,9 +50,10 @@ __device__ __forceinline__ uint32_t e4m3_nans(uint32_t w) { return ((w & 0x7f7f7
 
 // Softmax weights reach the matrix core as two f16, the nearest one and what it leaves: 22 bits, 2^kWeightShift larger: at most 2^15, as
 // they trail 1 by 2^kLazyLog2 at most.  Off by 2^-22 of themselves, or by 2^-25 (half a subnormal) where that is more, as little as the
-// fp32 sums they go into.  The first piece alone is off by up to 2^-12 and leaves that in the output wherever weights round alike.  MI355X, output in
+// fp32 sums they go into.  The first piece alone is off by up to 2^-11 and leaves that in the output wherever weights round alike.  MI355X, output in
 // fp32 against 64 bits, relative, one piece / two: 128 requests of 128-4096 tokens, 32/8 heads of 128, 1.8e-4 / 2.7e-7 (100.9 / 101.7
-// us), 64 trees of up to 13 nodes, 256-4096, 32/8 of 64, 1.8e-4 / 3.4e-7 (52.7 / 56.1); 64 of 8192-32768, 64/8 of 128, 495 / 517 us.
+// us), 64 trees of up to 13 nodes, 256-4096, 32/8 of 64, 1.8e-4 / 3.4e-7 (52.7 / 56.1); 64 of 8192-32768, 64/8 of 128, 495 / 517 us,
+// of 8 rows each, four full row tiles, 624 / 724.
 // They are multiplied by their value's scale before that, relative to the largest scale so far, which O is kept in units of: a factor
 // per page.  That is sound where all scales are within kScalesApart of each other: 2^-25 of a unit, what a subnormal may be off by, is
 // then at most 2^-26 of the row's largest weighted scale.  A wavefront that has met scales further apart, which it knows at the end of its

@@ -2,7 +2,7 @@
 
 Tolerance on the fp32 accumulator: 2e-5 for values of unit size, that of the other attention tests, where weights are fp32.  The weights
 are two f16, the second what the first leaves: off by half a step of 11 bits, 2^-11, of at most 2^-11 of them, 2^-22, and a mean of values by up to
-that times the mean of their magnitudes.  (One f16 alone would be off by up to 2^-12 of each weight.)"""
+that times the mean of their magnitudes.  (One f16 alone would be off by up to 2^-11 of each weight.)"""
 import numpy as np
 import pytest
 
